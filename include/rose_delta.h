@@ -475,6 +475,113 @@ rose_status rose_bw_probe_mixed_timed(const void *src_a, const void *src_b, void
  */
 rose_status rose_bw_probe_lines(void *dst, size_t bytes, uint32_t touched_per_2_32, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Operators at the two ends of a synchronisation.  They work on the tensors that an update carries:
+ * on the training side the embedding, its gradient, and the norm of all gradients, which decide what
+ * the next weights are; on the serving side matrices held in 4 bits, made from the shards that an
+ * update has been applied to.  Conventions as above: device memory is the caller's, calls queue work on
+ * `stream` and return, allocate nothing and may be captured into a graph; errors that the host can
+ * see are returned before anything is queued.  Sizes of zero are allowed where nothing is then read.
+ * Matrices are row-major with rows `stride` elements apart (stride >= columns; what lies between is
+ * neither read nor written); pointers need the alignment of their element type only, unless stated.
+ * Every result is a function of the inputs alone: two calls give the same bits.
+ * ---------------------------------------------------------------------------------------------
+ */
+typedef enum {
+    ROSE_DTYPE_BF16 = 0,
+    ROSE_DTYPE_F32 = 1
+} rose_dtype;
+
+/*
+ * Rows of an embedding, scaled:  out[i][:] = scale * table[tokens[i] - first_row][:]
+ * The table holds rows first_row .. first_row + rows - 1 of the vocabulary (ROSE_SPLIT_ROWS puts rows / tp
+ * of them on a shard).  A token outside (of another shard, or negative: padding) gives a row of zeros, so
+ * the shards' outputs add up to the whole embedding's.  The product is formed in fp32 and rounded once.
+ *   tokens       int32 or int64 (token_bytes 4 or 8)
+ * ROSE_ERR_ARG for null pointers, negative sizes, strides below cols, unknown types; ROSE_ERR_ALIGN for a
+ * pointer that is not aligned to its element; ROSE_ERR_UNSUPPORTED for 2^31 or more tokens or rows or columns.
+ */
+rose_status rose_embedding_lookup(const void *table, int32_t table_dtype, int64_t rows, int64_t cols, int64_t table_stride,
+                                  const void *tokens, int32_t token_bytes, int64_t n_tokens, int64_t first_row, float scale,
+                                  void *out, int32_t out_dtype, int64_t out_stride, void *stream);
+
+/*
+ * Its gradient:  grad[r][:] = scale * sum of dy[i][:] over the tokens i with tokens[i] - first_row == r
+ * (accumulate != 0: that is added to grad[r][:]; rows that no token names are then neither read nor written.
+ * accumulate == 0: they become zero).  The tokens are sorted by row, equal ones in their order, and the
+ * rows of dy that belong together are summed in fp32 in that order, in blocks of fixed size whose sums are then
+ * joined in order; scale and an accumulated gradient come in at the end, in fp32, before the one rounding.
+ *   workspace    rose_embedding_grad_workspace_bytes, 256-byte aligned; contents before the call do not
+ *                matter; calls that share one must be ordered on one stream
+ * Errors as rose_embedding_lookup; ROSE_ERR_ARG for a workspace that is too small.
+ */
+rose_status rose_embedding_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t n_tokens, size_t *bytes);
+rose_status rose_embedding_grad(const void *dy, int32_t dy_dtype, int64_t dy_stride, const void *tokens, int32_t token_bytes,
+                                int64_t n_tokens, int64_t first_row, float scale, void *grad, int32_t grad_dtype, int64_t rows,
+                                int64_t cols, int64_t grad_stride, int32_t accumulate, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
+ * The norm of many tensors together, and clipping by it.
+ *   grad_ptrs    DEVICE array of n_tensors device pointers, each aligned to its element.  A null pointer leaves its
+ *                tensor out: a rank that holds a replicated tensor which another rank counts passes null for it to
+ *                rose_grad_sum_squares (rose_plan_tensor_is_read says who sends, and may count, which).
+ *   offsets      DEVICE array of n_tensors + 1 int64: offsets[0] = 0, tensor t has offsets[t+1] - offsets[t] elements
+ *   total        offsets[n_tensors], for the host to size the launch by (a wrong value costs speed, nothing else)
+ *   workspace    ROSE_GRAD_WORKSPACE_BYTES, 256-byte aligned; contents before the call do not matter
+ * rose_grad_sum_squares   *sum (device, 8-byte aligned) = sum of all squares, formed and added in 64 bits: ranks that
+ *                         hold different tensors or shards add their sums up before they clip.
+ * rose_grad_clip          out = grad * min(1, max_norm / (norm + 1e-6)), norm = sqrt(*sum), rounded once to the
+ *                         gradients' type.  out_ptrs as grad_ptrs (null: leave out); entries may equal those of
+ *                         grad_ptrs, and where they do and nothing is to be scaled nothing is moved.  A norm that is
+ *                         infinite or NaN goes through the same formula (finite gradients become 0 or NaN): a program
+ *                         that skips such steps reads *norm.  *norm (device, 4-byte aligned, may be NULL) gets the norm.
+ * rose_grad_clip_norm     both, for one rank that holds everything: one launch less, the same bits.
+ * ROSE_ERR_ARG for null pointers, negative sizes, an unknown type, a max_norm that is negative or NaN, a workspace
+ * that is too small; ROSE_ERR_ALIGN for unaligned tables, sums or workspaces.
+ */
+#define ROSE_GRAD_WORKSPACE_BYTES 32768
+rose_status rose_grad_sum_squares(const void *const *grad_ptrs, const int64_t *offsets, int32_t n_tensors, int64_t total,
+                                  int32_t dtype, double *sum, void *workspace, size_t workspace_bytes, void *stream);
+rose_status rose_grad_clip(const void *const *grad_ptrs, const int64_t *offsets, int32_t n_tensors, int64_t total, int32_t dtype,
+                           void *const *out_ptrs, const double *sum, float max_norm, float *norm, void *stream);
+rose_status rose_grad_clip_norm(const void *const *grad_ptrs, const int64_t *offsets, int32_t n_tensors, int64_t total,
+                                int32_t dtype, void *const *out_ptrs, float max_norm, float *norm, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
+ * Matrices in microscaled 4-bit floating point (OCP Microscaling formats v1.0, MXFP4): each 32 consecutive
+ * elements of a row share a scale, a power of two; an element is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *   codes    [rows][ceil(cols / 32) * 16] bytes, 16-byte aligned: two elements a byte, the first in the low half,
+ *            code = sign << 3 | index of the magnitude; rows are filled up with zeros to whole blocks
+ *   scales   [rows][ceil(cols / 32)] bytes: exponent + 127; 255 says that the block is NaN
+ * rose_mx4_quantize     x (bf16 or fp32) -> codes, scales.  Exponent = floor(log2(largest magnitude)) - 2, at least
+ *                       -127; elements are divided by the scale and rounded to the nearest magnitude, ties to the
+ *                       even code, magnitudes above 6 to 6.  A block of zeros has exponent -127; a block that holds an
+ *                       infinity or a NaN has scale 255 and codes of zero.
+ * rose_mx4_dequantize   codes, scales -> out (bf16 or fp32), exact
+ * rose_mx4_matmul       out[i][j] = sum over k of a[i][k] * w[j][k]: a is m x k (activations), w is n x k (a stored
+ *                       [out, in] matrix), both quantised; products are exact, sums fp32, rounded once to out's type
+ * rose_mx4_linear       the same with a quantised on the way from x (m x k, bf16 or fp32).
+ *                       workspace: rose_mx4_linear_workspace_bytes (may be 0: then NULL is fine), 256-byte aligned;
+ *                       calls that share one must be ordered on one stream
+ * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too
+ * small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns.
+ */
+#define ROSE_MX4_BLOCK 32
+rose_status rose_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t *codes,
+                              uint8_t *scales, void *stream);
+rose_status rose_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out,
+                                int32_t dtype, int64_t stride, void *stream);
+rose_status rose_mx4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, const uint8_t *w_codes,
+                            const uint8_t *w_scales, int64_t n, int64_t k, void *out, int32_t out_dtype, int64_t out_stride,
+                            void *stream);
+rose_status rose_mx4_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t *bytes);
+rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m, int64_t x_stride, const uint8_t *w_codes,
+                            const uint8_t *w_scales, int64_t n, int64_t k, void *out, int32_t out_dtype, int64_t out_stride,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 const char *rose_status_str(rose_status s);
 
 #ifdef __cplusplus

@@ -10,7 +10,10 @@ __all__ = ["BF16", "FP32_RNE", "FUSED_ROWS", "REPLICATED", "SPLIT_COLS", "SPLIT_
            "Bucket", "Plan", "RoseError", "bucket_check", "bw_probe", "bw_probe_mixed", "bw_probe_lines", "delta_apply", "delta_encode",
            "delta_encode_refresh", "dense_copy", "ENCODE_ARITH", "ENCODE_REFRESH", "PAYLOAD_ARITH", "PAYLOAD_NEW",
            "delta_encode_ex", "delta_encode_static", "delta_apply_ex", "bucket_pack_ex", "bucket_pack", "object_apply",
-           "object_bytes", "object_check", "ptr_table", "shard_plan", "workspace", "binding"]
+           "object_bytes", "object_check", "ptr_table", "shard_plan", "workspace", "binding",
+           "embedding_lookup", "embedding_grad", "embedding_grad_workspace", "grad_sum_squares", "grad_clip", "grad_clip_norm",
+           "grad_workspace", "offset_table", "Mx4", "mx4_quantize", "mx4_dequantize", "mx4_matmul", "mx4_linear",
+           "mx4_linear_workspace"]
 
 
 def __getattr__(name):

@@ -15,9 +15,12 @@ ROSE_MAX_SECTIONS = 4
 REPLICATED, SPLIT_ROWS, SPLIT_COLS, FUSED_ROWS = 0, 1, 2, 3
 BF16, FP32_RNE = 0, 1
 OK, ERR_ARG, ERR_SHAPE, ERR_CAPACITY, ERR_ALIGN, ERR_HIP, ERR_UNSUPPORTED, ERR_SCRATCH = range(8)
+DTYPE_BF16, DTYPE_F32 = 0, 1
 LAYER_FIRST, LAYER_LAST = -1, -2
 TILE_ORDER_AUTO, TILE_ORDER_SPREAD, TILE_ORDER_NEIGHBOURS, TILE_ORDER_TIMED = 0, 1, 2, 3
 STATIC_SCRATCH_BYTES = 48 << 20
+GRAD_WORKSPACE_BYTES = 32768
+MX4_BLOCK = 32
 
 _LIB_PATH = os.environ.get("ROSE_DELTA_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)),
                                                             "librose_delta.so")
@@ -38,6 +41,7 @@ class CBucket(ctypes.Structure):
 
 
 _vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+_f32, _size = ctypes.c_float, ctypes.c_size_t
 _P = ctypes.POINTER
 _SIGS = {
     "rose_shard_plan_create": (_i32, [_P(TensorDesc), _i32, _i32, _P(_vp)]),
@@ -77,6 +81,18 @@ _SIGS = {
     "rose_bw_probe_mixed": (_i32, [_vp, _vp, _vp, ctypes.c_size_t, ctypes.c_size_t, _vp, _vp]),
     "rose_bw_probe_mixed_timed": (_i32, [_vp, _vp, _vp, ctypes.c_size_t, ctypes.c_size_t, _vp, _vp]),
     "rose_bw_probe_lines": (_i32, [_vp, ctypes.c_size_t, ctypes.c_uint32, _vp]),
+    "rose_embedding_lookup": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _i64, _i64, _f32, _vp, _i32, _i64, _vp]),
+    "rose_embedding_grad_workspace_bytes": (_i32, [_i64, _i64, _i64, _P(_size)]),
+    "rose_embedding_grad": (_i32, [_vp, _i32, _i64, _vp, _i32, _i64, _i64, _f32, _vp, _i32, _i64, _i64, _i64, _i32, _vp, _size,
+                                   _vp]),
+    "rose_grad_sum_squares": (_i32, [_vp, _vp, _i32, _i64, _i32, _vp, _vp, _size, _vp]),
+    "rose_grad_clip": (_i32, [_vp, _vp, _i32, _i64, _i32, _vp, _vp, _f32, _vp, _vp]),
+    "rose_grad_clip_norm": (_i32, [_vp, _vp, _i32, _i64, _i32, _vp, _f32, _vp, _vp, _size, _vp]),
+    "rose_mx4_quantize": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "rose_mx4_dequantize": (_i32, [_vp, _vp, _i64, _i64, _vp, _i32, _i64, _vp]),
+    "rose_mx4_matmul": (_i32, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i32, _i64, _vp]),
+    "rose_mx4_linear_workspace_bytes": (_i32, [_i64, _i64, _i64, _P(_size)]),
+    "rose_mx4_linear": (_i32, [_vp, _i32, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i32, _i64, _vp, _size, _vp]),
     "rose_status_str": (ctypes.c_char_p, [_i32]),
 }
 
@@ -364,3 +380,155 @@ def object_check(plan, obj, stream=None, with_payload=False):
                                   ctypes.byref(d), ctypes.byref(first), ctypes.byref(n), ctypes.byref(kind)),
            "object_check")
     return (d.value, first.value, n.value, kind.value) if with_payload else (d.value, first.value, n.value)
+
+
+# ---------------------------------------------------------------------------------------------------
+# operators at the two ends of a synchronisation
+# ---------------------------------------------------------------------------------------------------
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+
+
+def _dtype(dtype, what):
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise RoseError(ERR_ARG, "%s: %s" % (what, dtype))
+    return code
+
+
+def _matrix(t, what):
+    """-> (pointer, type, rows, columns, stride) of a matrix on the GPU whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or (t.size(1) > 1 and t.stride(1) != 1):
+        raise RoseError(ERR_SHAPE, "%s: a matrix on the GPU with contiguous rows is wanted" % what)
+    rows, cols = t.shape
+    return t.data_ptr(), _dtype(t.dtype, what), rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _tokens(t, what):
+    """-> (pointer, bytes of an id, how many)"""
+    if t.dim() != 1 or not t.is_cuda or not t.is_contiguous() or t.dtype not in (torch.int32, torch.int64):
+        raise RoseError(ERR_SHAPE, "%s: a contiguous list of int32 or int64 ids on the GPU is wanted" % what)
+    return t.data_ptr(), t.element_size(), t.numel()
+
+
+def _same(ok, what):
+    if not ok:
+        raise RoseError(ERR_SHAPE, what)
+
+
+def embedding_lookup(table, tokens, out, scale=1.0, first_row=0, stream=None):
+    """out[i] = scale * table[tokens[i] - first_row]; rows of zeros for tokens of other shards."""
+    tp, tt, rows, cols, ts = _matrix(table, "embedding_lookup")
+    ip, ib, n = _tokens(tokens, "embedding_lookup")
+    op, ot, n_out, o_cols, os_ = _matrix(out, "embedding_lookup")
+    _same(n_out == n and o_cols == cols, "embedding_lookup")
+    _check(_lib.rose_embedding_lookup(tp, tt, rows, cols, ts, ip, ib, n, first_row, scale, op, ot, os_, _stream(stream)),
+           "embedding_lookup")
+
+
+def embedding_grad_workspace(rows, cols, n_tokens, device="cuda"):
+    v = _size()
+    _check(_lib.rose_embedding_grad_workspace_bytes(rows, cols, n_tokens, ctypes.byref(v)), "embedding_grad_workspace")
+    return torch.empty(v.value, dtype=torch.uint8, device=device)
+
+
+def embedding_grad(dy, tokens, grad, ws, scale=1.0, first_row=0, accumulate=False, stream=None):
+    """grad[r] = scale * the sum of dy[i] over the tokens i of row first_row + r (accumulate: added to what is there)."""
+    dp, dt, n_dy, cols, ds = _matrix(dy, "embedding_grad")
+    ip, ib, n = _tokens(tokens, "embedding_grad")
+    gp, gt, rows, g_cols, gs = _matrix(grad, "embedding_grad")
+    _same(n_dy == n and g_cols == cols, "embedding_grad")
+    _check(_lib.rose_embedding_grad(dp, dt, ds, ip, ib, n, first_row, scale, gp, gt, rows, cols, gs, 1 if accumulate else 0,
+                                    ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "embedding_grad")
+
+
+def offset_table(numels, device="cuda"):
+    """Device array of where each tensor begins if all were laid end to end, and their total."""
+    at = [0]
+    for n in numels:
+        at.append(at[-1] + int(n))
+    return torch.tensor(at, dtype=torch.int64, device=device)
+
+
+def grad_workspace(device="cuda"):
+    return torch.empty(GRAD_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+
+def _grads(grad_tab, offsets, what):
+    _same(offsets.numel() == grad_tab.numel() + 1 and offsets.dtype == torch.int64 and grad_tab.dtype == torch.int64, what)
+    return grad_tab.data_ptr(), offsets.data_ptr(), grad_tab.numel()
+
+
+def grad_sum_squares(grad_tab, offsets, total, dtype, out, ws, stream=None):
+    """out (one float64): sum of the squares of all elements of the tensors of a pointer table; null pointers are left out."""
+    gp, fp, n = _grads(grad_tab, offsets, "grad_sum_squares")
+    _same(out.dtype == torch.float64 and out.numel() == 1, "grad_sum_squares")
+    _check(_lib.rose_grad_sum_squares(gp, fp, n, total, _dtype(dtype, "grad_sum_squares"), out.data_ptr(), ws.data_ptr(),
+                                      ws.numel() * ws.element_size(), _stream(stream)), "grad_sum_squares")
+
+
+def grad_clip(grad_tab, offsets, total, dtype, out_tab, sum_squares, max_norm, norm=None, stream=None):
+    """Scales the tensors down to a norm of max_norm, given the sum of all squares; out_tab may be grad_tab."""
+    gp, fp, n = _grads(grad_tab, offsets, "grad_clip")
+    _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and sum_squares.dtype == torch.float64 and
+          (norm is None or norm.dtype == torch.float32), "grad_clip")
+    _check(_lib.rose_grad_clip(gp, fp, n, total, _dtype(dtype, "grad_clip"), out_tab.data_ptr(), sum_squares.data_ptr(),
+                               max_norm, norm.data_ptr() if norm is not None else None, _stream(stream)), "grad_clip")
+
+
+def grad_clip_norm(grad_tab, offsets, total, dtype, out_tab, max_norm, norm, ws, stream=None):
+    """grad_sum_squares and grad_clip in one call, for a rank that holds everything."""
+    gp, fp, n = _grads(grad_tab, offsets, "grad_clip_norm")
+    _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and (norm is None or norm.dtype == torch.float32), "grad_clip_norm")
+    _check(_lib.rose_grad_clip_norm(gp, fp, n, total, _dtype(dtype, "grad_clip_norm"), out_tab.data_ptr(), max_norm,
+                                    norm.data_ptr() if norm is not None else None, ws.data_ptr(),
+                                    ws.numel() * ws.element_size(), _stream(stream)), "grad_clip_norm")
+
+
+class Mx4:
+    """A matrix in microscaled 4-bit floating point (caller-owned torch tensors; made here if not given)."""
+
+    def __init__(self, rows, cols, codes=None, scales=None, device="cuda"):
+        self.rows, self.cols = int(rows), int(cols)
+        blocks = -(-self.cols // MX4_BLOCK)
+        self.codes = torch.empty(self.rows, blocks * MX4_BLOCK // 2, dtype=torch.uint8, device=device) if codes is None else codes
+        self.scales = torch.empty(self.rows, blocks, dtype=torch.uint8, device=device) if scales is None else scales
+        for t, width in ((self.codes, blocks * MX4_BLOCK // 2), (self.scales, blocks)):
+            _same(t.dtype == torch.uint8 and tuple(t.shape) == (self.rows, width) and t.is_contiguous(), "Mx4")
+
+
+def mx4_quantize(x, out, stream=None):
+    """x (bf16 or float32) -> out, an Mx4 of the same shape"""
+    xp, xt, rows, cols, xs = _matrix(x, "mx4_quantize")
+    _same((out.rows, out.cols) == (rows, cols), "mx4_quantize")
+    _check(_lib.rose_mx4_quantize(xp, xt, rows, cols, xs, out.codes.data_ptr(), out.scales.data_ptr(), _stream(stream)),
+           "mx4_quantize")
+
+
+def mx4_dequantize(q, out, stream=None):
+    op, ot, rows, cols, os_ = _matrix(out, "mx4_dequantize")
+    _same((q.rows, q.cols) == (rows, cols), "mx4_dequantize")
+    _check(_lib.rose_mx4_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, op, ot, os_, _stream(stream)),
+           "mx4_dequantize")
+
+
+def mx4_matmul(a, w, out, stream=None):
+    """out = a @ w.T: a (m x k) and w (n x k, a stored [out, in] matrix) are Mx4"""
+    op, ot, m, n, os_ = _matrix(out, "mx4_matmul")
+    _same(a.cols == w.cols and (a.rows, w.rows) == (m, n), "mx4_matmul")
+    _check(_lib.rose_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), m, w.codes.data_ptr(), w.scales.data_ptr(), n, a.cols,
+                                op, ot, os_, _stream(stream)), "mx4_matmul")
+
+
+def mx4_linear_workspace(m, n, k, device="cuda"):
+    v = _size()
+    _check(_lib.rose_mx4_linear_workspace_bytes(m, n, k, ctypes.byref(v)), "mx4_linear_workspace")
+    return torch.empty(v.value, dtype=torch.uint8, device=device)
+
+
+def mx4_linear(x, w, out, ws, stream=None):
+    """out = x @ w.T: x (m x k, bf16 or float32) is quantised on the way in, w (n x k) is an Mx4"""
+    xp, xt, m, k, xs = _matrix(x, "mx4_linear")
+    op, ot, m_out, n, os_ = _matrix(out, "mx4_linear")
+    _same(m_out == m and w.cols == k and w.rows == n, "mx4_linear")
+    _check(_lib.rose_mx4_linear(xp, xt, m, xs, w.codes.data_ptr(), w.scales.data_ptr(), n, k, op, ot, os_, ws.data_ptr(),
+                                ws.numel() * ws.element_size(), _stream(stream)), "mx4_linear")

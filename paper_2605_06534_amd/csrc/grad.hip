@@ -1,0 +1,218 @@
+// The norm of many gradients together, and the gradients scaled by it.  Reads them once for the norm and once more to
+// scale them: HBM traffic bounds both.
+#include "ops_device.h"
+
+namespace rose {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kShare = 8192;                    // a workgroup's share of the elements is a multiple of this
+
+// The share of workgroup `index` of `count`, as positions in all tensors laid end to end.
+__device__ __forceinline__ void share_of(int64_t total, int64_t index, int64_t count, int64_t &from, int64_t &to) {
+    const int64_t per = ((total + count - 1) / count + kShare - 1) / kShare * kShare;
+    from = index * per < total ? index * per : total;
+    to = from + per < total ? from + per : total;
+}
+
+// the tensor that holds position `at`: the last one that begins at or before it
+__device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, int64_t at) {
+    int32_t lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int32_t mid = (lo + hi + 1) / 2;
+        if (offsets[mid] <= at) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double squares(const float (&f)[8]) {
+    double s = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fma((double)f[e], (double)f[e], s);
+    return s;
+}
+
+// sum over the workgroup, the same in every thread
+__device__ __forceinline__ double sum_over(double v, double (&waves)[kThreads / 64]) {
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) v += waves[w];
+    __syncthreads();
+    return v;
+}
+
+// Elements in front of the first 16-byte boundary of p, at most n
+template <class T>
+__device__ __forceinline__ int64_t head_of(const T *p, int64_t n) {
+    const int64_t h = (int64_t)((-(uint64_t)p & 15) / sizeof(T));
+    return h < n ? h : n;
+}
+
+template <class T>
+__device__ __forceinline__ double squares_of(const T *p, int64_t n) {
+    constexpr int kAhead = 4;
+    double s = 0;
+    const int64_t head = head_of(p, n), vectors = (n - head) / 8, tail = head + vectors * 8;
+    if (threadIdx.x < head) {
+        const double f = to_f32(p[threadIdx.x]);
+        s = fma(f, f, s);
+    }
+    if (threadIdx.x < n - tail) {
+        const double f = to_f32(p[tail + threadIdx.x]);
+        s = fma(f, f, s);
+    }
+    const T *body = p + head;
+    int64_t i = threadIdx.x;
+    for (; i + (kAhead - 1) * kThreads < vectors; i += kAhead * kThreads) {
+        Raw8<T> raw[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) load8(body + (i + u * kThreads) * 8, raw[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float f[8];
+            widen8(raw[u], f);
+            s += squares(f);
+        }
+    }
+    for (; i < vectors; i += kThreads) {
+        Raw8<T> raw;
+        float f[8];
+        load8(body + i * 8, raw);
+        widen8(raw, f);
+        s += squares(f);
+    }
+    return s;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradArgs a) {
+    __shared__ double waves[kThreads / 64];
+    int64_t from, to;
+    share_of(a.offsets[a.n_tensors], blockIdx.x, gridDim.x, from, to);
+    double s = 0;
+    if (from < to)
+        for (int32_t t = tensor_at(a.offsets, a.n_tensors, from); t < a.n_tensors && a.offsets[t] < to; ++t) {
+            const int64_t base = a.offsets[t], end = a.offsets[t + 1];
+            const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
+            const T *p = static_cast<const T *>(a.grad_ptrs[t]);
+            if (p && lo < hi) s += squares_of(p + (lo - base), hi - lo);
+        }
+    s = sum_over(s, waves);
+    if (threadIdx.x == 0) a.partials[blockIdx.x] = s;
+}
+
+// all partial sums, in one order whoever adds them
+__device__ __forceinline__ double sum_partials(const GradArgs &a, double (&waves)[kThreads / 64]) {
+    double s = 0;
+    for (int i = threadIdx.x; i < a.n_partials; i += kThreads) s += a.partials[i];
+    return sum_over(s, waves);
+}
+
+__global__ __launch_bounds__(kThreads) void grad_sum_kernel(GradArgs a) {
+    __shared__ double waves[kThreads / 64];
+    const double s = sum_partials(a, waves);
+    if (threadIdx.x == 0) *a.sum = s;
+}
+
+template <class T>
+__device__ __forceinline__ void scale_into(const T *p, T *q, int64_t n, float factor) {
+    constexpr int kAhead = 4;
+    const int64_t head = head_of(q, n), vectors = (n - head) / 8, tail = head + vectors * 8;
+    if (threadIdx.x < head) q[threadIdx.x] = from_f32<T>(to_f32(p[threadIdx.x]) * factor);
+    if (threadIdx.x < n - tail) q[tail + threadIdx.x] = from_f32<T>(to_f32(p[tail + threadIdx.x]) * factor);
+    p += head;
+    q += head;
+    int64_t i = threadIdx.x;
+    for (; i + (kAhead - 1) * kThreads < vectors; i += kAhead * kThreads) {
+        Raw8<T> raw[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) load8(p + (i + u * kThreads) * 8, raw[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float f[8];
+            widen8(raw[u], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] *= factor;
+            store8(q + (i + u * kThreads) * 8, f);
+        }
+    }
+    for (; i < vectors; i += kThreads) {
+        Raw8<T> raw;
+        float f[8];
+        load8(p + i * 8, raw);
+        widen8(raw, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= factor;
+        store8(q + i * 8, f);
+    }
+}
+
+template <class T, bool FROM_PARTIALS>
+__global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
+    __shared__ double waves[kThreads / 64];
+    const float norm = (float)sqrt(FROM_PARTIALS ? sum_partials(a, waves) : *a.sum);
+    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
+    const float ratio = a.max_norm / (norm + 1e-6f);
+    const float factor = ratio >= 1.f ? 1.f : ratio;        // (a NaN stays one)
+    int64_t from, to;
+    share_of(a.offsets[a.n_tensors], blockIdx.x, gridDim.x, from, to);
+    if (from >= to) return;
+    for (int32_t t = tensor_at(a.offsets, a.n_tensors, from); t < a.n_tensors && a.offsets[t] < to; ++t) {
+        const int64_t base = a.offsets[t], end = a.offsets[t + 1];
+        const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
+        const T *p = static_cast<const T *>(a.grad_ptrs[t]);
+        T *q = static_cast<T *>(a.out_ptrs[t]);
+        if (!p || !q || lo >= hi || (p == q && factor == 1.f)) continue;
+        scale_into(p + (lo - base), q + (lo - base), hi - lo, factor);
+    }
+}
+
+int workgroups(int64_t total) {
+    const int64_t shares = (total + kShare - 1) / kShare;
+    return (int)(shares < 1 ? 1 : shares > 2048 ? 2048 : shares);
+}
+
+}  // namespace
+
+static_assert(kGradPartials >= 2048, "the workspace holds a partial sum of each workgroup");
+
+static int squares(GradArgs &a, int64_t total, bool f32, hipStream_t st) {
+    a.n_partials = workgroups(total);
+    if (f32) hipLaunchKernelGGL(grad_squares_kernel<float>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL(grad_squares_kernel<bf16_t>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
+    return (int)hipGetLastError();
+}
+
+int launch_grad_sum_squares(const GradArgs &args, int64_t total, bool f32, void *stream) {
+    GradArgs a = args;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (int e = squares(a, total, f32, st)) return e;
+    hipLaunchKernelGGL(grad_sum_kernel, dim3(1), dim3(kThreads), 0, st, a);
+    return (int)hipGetLastError();
+}
+
+int launch_grad_clip(const GradArgs &a, int64_t total, bool f32, void *stream) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid(workgroups(total)), block(kThreads);
+    if (f32) hipLaunchKernelGGL((grad_clip_kernel<float, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((grad_clip_kernel<bf16_t, false>), grid, block, 0, st, a);
+    return (int)hipGetLastError();
+}
+
+int launch_grad_clip_norm(const GradArgs &args, int64_t total, bool f32, void *stream) {
+    GradArgs a = args;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (int e = squares(a, total, f32, st)) return e;
+    const dim3 grid(workgroups(total)), block(kThreads);
+    if (f32) hipLaunchKernelGGL((grad_clip_kernel<float, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((grad_clip_kernel<bf16_t, true>), grid, block, 0, st, a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace rose
