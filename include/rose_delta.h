@@ -567,7 +567,7 @@ rose_status rose_grad_clip_norm(const void *const *grad_ptrs, const int64_t *off
  *                       workspace: rose_mx4_linear_workspace_bytes (may be 0: then NULL is fine), 256-byte aligned;
  *                       calls that share one must be ordered on one stream
  * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too
- * small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns.
+ * small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, or products with k >= 2^24.
  */
 #define ROSE_MX4_BLOCK 32
 rose_status rose_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t *codes,

@@ -1,5 +1,6 @@
 """MI355X-native sparse weight-delta synchronisation (ROSE, Sec. 4.2): shard_plan, delta_encode,
-delta_apply and helpers, implemented in librose_delta.so (HIP, gfx950) and bound with ctypes.
+delta_apply and helpers, and operators at the two ends of a synchronisation (embedding, gradient
+norm, 4-bit matrices), implemented in librose_delta.so (HIP, gfx950) and bound with ctypes.
 
 The names of `binding` are served from here on first use, so that `paper_2605_06534_amd.build`
 can be run while the library is missing or stale; any other use loads the library and fails
@@ -15,9 +16,14 @@ __all__ = ["BF16", "FP32_RNE", "FUSED_ROWS", "REPLICATED", "SPLIT_COLS", "SPLIT_
            "grad_workspace", "offset_table", "Mx4", "mx4_quantize", "mx4_dequantize", "mx4_matmul", "mx4_linear",
            "mx4_linear_workspace"]
 
+_names = frozenset(__all__)
+_binding = None
+
 
 def __getattr__(name):
-    if name in __all__:
-        binding = importlib.import_module(__name__ + ".binding")
-        return binding if name == "binding" else getattr(binding, name)
+    global _binding
+    if name in _names:
+        if _binding is None:
+            _binding = importlib.import_module(__name__ + ".binding")
+        return _binding if name == "binding" else getattr(_binding, name)
     raise AttributeError("module %r has no attribute %r" % (__name__, name))

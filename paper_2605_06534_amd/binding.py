@@ -123,8 +123,9 @@ def _check(status, what):
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+        # (the current stream's handle itself: torch.cuda.current_stream() makes an object for it first, 3 us a call)
+        return _vp(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+    return _vp(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
 class Plan:

@@ -1,4 +1,6 @@
 // Matrices in microscaled 4-bit floating point: quantisation, its inverse, and products on the matrix cores.
+#include <type_traits>
+
 #include "ops_device.h"
 
 namespace rose {
@@ -89,40 +91,379 @@ __global__ __launch_bounds__(kThreads) void mx4_dequantize_kernel(QuantArgs a, T
 // products
 // -------------------------------------------------------------------------------------------------
 // v_mfma_scale_f32_16x16x128: lane l holds, of either operand, row l % 16 and block l / 16 of the four blocks of 32 that
-// one instruction takes (16 bytes and a scale), and of the result column l % 16, rows 4 * (l / 16) .. + 3.  With the
-// weights as the first operand a lane ends up with four neighbouring outputs of one row of the activations.
+// one instruction takes (16 bytes and a scale, byte S of a word), and of the result column l % 16, rows 4 * (l / 16) .. + 3.
+// With the weights as the first operand a lane ends up with four neighbouring outputs of one row of the activations.
+template <int S>
 __device__ __forceinline__ f32x4 product(u32x4 w, uint32_t w_scale, u32x4 a, uint32_t a_scale, f32x4 c) {
     const i32x8 wv = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
     const i32x8 av = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av, c, 4, 4, 0, (int)w_scale, 0, (int)a_scale);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av, c, 4, 4, S, (int)w_scale, S, (int)a_scale);
 }
 
-// One wave: 16 rows of the weights by 16 of the activations.
-template <class OT>
-__global__ __launch_bounds__(kThreads) void mx4_product_kernel(Mx4ProductArgs a, int64_t blocks, int64_t n_tiles, int64_t tiles) {
-    const int64_t tile = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (tile >= tiles) return;
-    const int lane = threadIdx.x & 63, of16 = lane & 15, quarter = lane >> 4;
-    const int64_t m0 = tile / n_tiles * 16, n0 = (tile - tile / n_tiles * n_tiles) * 16;
-    const int64_t w_row = n0 + of16 < a.n ? n0 + of16 : a.n - 1, a_row = m0 + of16 < a.m ? m0 + of16 : a.m - 1;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t b = quarter; b - quarter < blocks; b += 4) {
-        u32x4 wv = {0, 0, 0, 0}, av = {0, 0, 0, 0};
-        uint32_t ws = kOneScale, as = kOneScale;
-        if (b < blocks) {
-            wv = reinterpret_cast<const u32x4 *>(a.w_codes)[w_row * blocks + b];
-            av = reinterpret_cast<const u32x4 *>(a.a_codes)[a_row * blocks + b];
-            ws = a.w_scales[w_row * blocks + b];
-            as = a.a_scales[a_row * blocks + b];
-        }
-        sum = product(wv, ws, av, as, sum);
-    }
-    const int64_t row = m0 + of16, col = n0 + quarter * 4;
-    if (row >= a.m) return;
-    OT *q = static_cast<OT *>(a.out) + row * a.out_stride + col;
+// ---- products of many rows: tiles in LDS ----
+//
+// A workgroup forms BN x BM outputs (BN rows of the weights, BM of the activations), a wave FN x FM fragments of 16 x 16 of
+// them.  Codes go from memory to LDS by loads that write there themselves, 256 elements of every row (128 bytes: a whole
+// line, which halves the requests that the L2 sees against 64) at a time, a slot ahead of the one that is multiplied; the
+// waves copy fragments to registers half a slot ahead of the multiplications.  So one barrier a slot does: behind it,
+// everybody has read the whole of slot d, whose place then takes slot d + 2, and slot d + 1 has come.
+// A row's sixteen-byte parts are permuted within the 128 bytes by bits of the row number so that the eight rows that eight
+// lanes read together lie in eight different groups of LDS banks.
+// Scales go through registers: sixteen of a row (two slots) a thread, turned around so that a lane finds the four that it
+// needs for its quarter of four instructions in one word, of which the instruction picks a byte.
+// 16384 x 6912 x 5120: 380 us, 3050 TFLOP/s (the simplest kernel: 7480 us); 4096 x 4096 x 4096: 40 us, 3460.  What bounds
+// it: without the loads from memory the same loop takes 310 us, without the multiplications 260, and 50 of either are
+// the stores, which nothing overlaps where one workgroup fills a CU.
+constexpr uint32_t kOutside = 0xFFFFF000u;      // an offset behind every resource: such loads give zeros
+
+__device__ __forceinline__ u32x4 resource_of(const uint8_t *p, int64_t bytes) {
+    const uint64_t at = (uint64_t)p;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xFFFFu),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes < (int64_t)kOutside ? (uint32_t)bytes : kOutside), 0x00020000u};
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
+template <class T>
+__device__ __forceinline__ T from_lds(uint32_t at) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) T *>(at);
+}
+
+// 16 bytes a lane from a resource to LDS, lane after lane from `to` on.  Written in assembly because the compiler, told of a
+// load that writes LDS, waits for it before every read of LDS; here the kernel waits (load_wait) where it has to.
+__device__ __forceinline__ void load_to_lds(uint32_t to, u32x4 resource, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(resource) : "memory");
+}
+// until at most LEFT of this wave's loads are away, and for its LDS operations; then for the other waves
+template <int LEFT>
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// 4 x 4 bytes, columns for rows
+__device__ __forceinline__ u32x4 turned(u32x4 d) {
+    const uint32_t a = __builtin_amdgcn_perm(d[1], d[0], 0x05010400), b = __builtin_amdgcn_perm(d[1], d[0], 0x07030602);
+    const uint32_t c = __builtin_amdgcn_perm(d[3], d[2], 0x05010400), e = __builtin_amdgcn_perm(d[3], d[2], 0x07030602);
+    return u32x4{__builtin_amdgcn_perm(c, a, 0x05040100), __builtin_amdgcn_perm(c, a, 0x07060302),
+                 __builtin_amdgcn_perm(e, b, 0x05040100), __builtin_amdgcn_perm(e, b, 0x07060302)};
+}
+
+// Sixteen scales from block `from` on of a row of nb; blocks behind its end have a scale of one (their codes are zeros).
+__device__ __forceinline__ u32x4 scales_at(const uint8_t *row, int from, int nb) {
+    if (from + 16 <= nb) return *reinterpret_cast<const u32x4_any *>(row + from);
+    uint64_t part[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (col + i < a.n) q[i] = from_f32<OT>(sum[i]);
+    for (int half = 0; half < 2; ++half) {
+        uint64_t v = 0;
+#pragma unroll 1
+        for (int i = 8 * half + 7; i >= 8 * half; --i) v = v << 8 | (from + i < nb ? row[from + i] : kOneScale);
+        part[half] = v;
+    }
+    return u32x4{(uint32_t)part[0], (uint32_t)(part[0] >> 32), (uint32_t)part[1], (uint32_t)(part[1] >> 32)};
+}
+// The same without a branch, for rows of 16 blocks at least: the last sixteen, shifted.  (A branch in the main loop makes
+// the compiler move all sums between register files on either side of it.)  Of shorter rows nothing is left: `row` is then
+// any address with 16 bytes behind it.
+__device__ __forceinline__ u32x4 scales_at_no_branch(const uint8_t *row, int from, int nb) {
+    constexpr uint64_t kOnes = 0x7F7F7F7F7F7F7F7Full;
+    static_assert(kOneScale == 0x7F, "");
+    const int at = nb < 16 ? 0 : from + 16 <= nb ? from : nb - 16, cut = (from - at) * 8, bits = cut & 63;
+    const u32x4 v = *reinterpret_cast<const u32x4_any *>(row + at);
+    const uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+    const uint64_t lo_cut = bits ? lo >> bits | hi << (64 - bits) : lo, hi_cut = bits ? hi >> bits | kOnes << (64 - bits) : hi;
+    const uint64_t low = from >= nb ? kOnes : cut >= 64 ? hi_cut : lo_cut, high = from >= nb || cut >= 64 ? kOnes : hi_cut;
+    return u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+}
+
+// Which tile a workgroup takes: workgroups i, i + 8, ... run on one XCD, whose L2 is its own, so it gets a stretch of
+// neighbouring tiles, in groups of kGroup rows of tiles that share their weights.
+__device__ __forceinline__ void tile_of(int n_tiles, int m_tiles, int &nt, int &mt) {
+    constexpr int kGroup = 8;
+    const int total = n_tiles * m_tiles, xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int per = (total + 7) / 8, full = total & 7 ? total & 7 : 8;      // the first `full` XCDs have `per` tiles, others one less
+    const int tile = xcd < full ? xcd * per + at : full * per + (xcd - full) * (per - 1) + at;
+    const int group = tile / (kGroup * n_tiles), first = group * kGroup, rows = m_tiles - first < kGroup ? m_tiles - first : kGroup;
+    const int in_group = tile - first * n_tiles;
+    mt = first + in_group % rows;
+    nt = in_group / rows;
+}
+
+template <class OT, int BN, int BM, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArgs a, int nb, int n_tiles, int m_tiles) {
+    constexpr int kThr = 64 * WN * WM, FN = BN / WN / 16, FM = BM / WM / 16, kRows = BN + BM;
+    constexpr int kPer = kThr / 8;                      // rows that one load of all threads takes
+    constexpr int kLoadsW = BN / kPer, kLoads = kRows / kPer;
+    constexpr uint32_t kSlot = kRows * 128, kScaleSlot = kRows * 16;
+    static_assert(BN % kPer == 0 && BM % kPer == 0 && kPer % 16 == 0 && FN % 2 == 0 && kRows == kThr, "a row of scales a thread");
+    __shared__ __attribute__((aligned(1024))) uint8_t codes[2][kSlot];
+    __shared__ __attribute__((aligned(16))) u32x4 scales[2][kRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), of16 = lane & 15, quarter = lane >> 4;
+    const int wn = wave % WN, wm = wave / WN;
+    int nt, mt;
+    tile_of(n_tiles, m_tiles, nt, mt);
+    const int64_t n0 = (int64_t)nt * BN, m0 = (int64_t)mt * BM, row_bytes = (int64_t)nb * 16;
+
+    // what this thread loads: 16 bytes of rows my, my + kPer, ... of either matrix; rows behind the last give zeros
+    const u32x4 w_res = resource_of(a.w_codes + n0 * row_bytes, (a.n - n0) * row_bytes);
+    const u32x4 x_res = resource_of(a.a_codes + m0 * row_bytes, (a.m - m0) * row_bytes);
+    const int my = tid >> 3;
+    const int w_part = (tid & 7) ^ ((my & 3) | ((my >> 3) & 1) << 2), x_part = (tid & 7) ^ (my & 7);
+    const uint32_t w_off = (uint32_t)my * (uint32_t)row_bytes + w_part * 16, x_off = (uint32_t)my * (uint32_t)row_bytes + x_part * 16;
+    const uint32_t hop = kPer * (uint32_t)row_bytes;
+    const uint32_t codes0 = lds_address(codes), scales0 = lds_address(scales);
+    auto ask = [&](int d, int slot, int j) {
+        const bool is_w = j < kLoadsW, inside = d * 8 + (is_w ? w_part : x_part) < nb;
+        const uint32_t off = is_w ? w_off + j * hop : x_off + (j - kLoadsW) * hop;
+        load_to_lds(codes0 + slot * kSlot + j * kThr * 16 + wave * 1024, is_w ? w_res : x_res, inside ? off + d * 128 : kOutside);
+    };
+    const int64_t s_row = tid < BN ? (n0 + tid < a.n ? n0 + tid : a.n - 1) : (m0 + tid - BN < a.m ? m0 + tid - BN : a.m - 1);
+    const uint8_t *my_scales = (tid < BN ? a.w_scales : a.a_scales) + s_row * nb;
+    const uint8_t *later_scales = nb < 16 ? a.w_codes : my_scales;
+
+    // what this lane multiplies: of fragments 2p and 2p + 1 of the weights rows 8 * (of16 / 4) + 0..3 and + 4..7 of 32, so
+    // that it ends up with eight neighbouring outputs
+    const int w_row = wn * (FN * 16) + (of16 >> 2) * 8 + (of16 & 3), x_row = BN + wm * (FM * 16) + of16;
+    const uint32_t w_at = codes0 + w_row * 128 + (quarter ^ ((of16 & 3) | ((of16 >> 2) & 1) << 2)) * 16;
+    const uint32_t x_at = codes0 + x_row * 128 + (quarter ^ (of16 & 7)) * 16;
+    const uint32_t ws_at = scales0 + w_row * 16 + quarter * 4, xs_at = scales0 + x_row * 16 + quarter * 4;
+    u32x4 w[2][FN], x[FM], more_scales;
+    uint32_t ws[FN], xs[FM];
+    auto get_w = [&](int slot, int half, u32x4 (&to)[FN]) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i) to[i] = from_lds<u32x4>((w_at ^ (half * 64)) + slot * kSlot + (i >> 1) * 4096 + (i & 1) * 512);
+    };
+    auto get_x = [&](int slot, int half, int j) { x[j] = from_lds<u32x4>((x_at ^ (half * 64)) + slot * kSlot + j * 2048); };
+    auto get_scales = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i) ws[i] = from_lds<uint32_t>(ws_at + slot * kScaleSlot + (i >> 1) * 512 + (i & 1) * 64);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) xs[j] = from_lds<uint32_t>(xs_at + slot * kScaleSlot + j * 256);
+    };
+    f32x4 sum[FN][FM];
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    more_scales = scales_at(my_scales, 16, nb);
+    scales[0][tid] = turned(scales_at(my_scales, 0, nb));
+    scales[1][tid] = turned(more_scales);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) ask(0, 0, j);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) ask(1, 1, j);
+    wait_and_meet<kLoads>();
+    get_w(0, 0, w[0]);
+#pragma unroll
+    for (int j = 0; j < FM; ++j) get_x(0, 0, j);
+    get_scales(0);
+
+    // One slot of 256 elements, d, in place P = d & 1: its first half while the second comes from LDS, then the second
+    // while the next slot's first half does.
+    int d = 0;
+    const int slots = (nb + 7) / 8;
+    auto one_slot = [&](auto place) {
+        constexpr int P = decltype(place)::value;
+        asm volatile("" : "+s"(d));                     // (offsets are formed where they are used, not kept in registers)
+        get_w(P, 1, w[1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P>(w[0][i], ws[i], x[j], xs[j], sum[i][j]);
+            get_x(P, 1, j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wait_and_meet<0>();
+        const int pair = d >> 1;                        // scales come for pairs of slots
+        if (P == 0) scales[(pair + 1) & 1][tid] = turned(more_scales);
+        get_w(P ^ 1, 0, w[0]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P + 1>(w[1][i], ws[i], x[j], xs[j], sum[i][j]);
+            get_x(P ^ 1, 0, j);
+#pragma unroll
+            for (int l = j * kLoads / FM; l < (j + 1) * kLoads / FM; ++l) ask(d + 2, P, l);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (P == 1) {
+            more_scales = scales_at_no_branch(later_scales, (pair + 2) * 16, nb);
+            get_scales((pair + 1) & 1);
+        }
+        ++d;
+    };
+    // (two slots a turn: one behind the last is zeros)
+    do {
+        one_slot(std::integral_constant<int, 0>{});
+        one_slot(std::integral_constant<int, 1>{});
+    } while (d < slots);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // (loads may still be on their way to LDS)
+
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        const int64_t row = m0 + wm * (FM * 16) + j * 16 + of16;
+        if (row >= a.m) continue;
+#pragma unroll
+        for (int i = 0; i < FN; i += 2) {
+            const int64_t col = n0 + wn * (FN * 16) + i * 16 + quarter * 8;
+            OT *q = static_cast<OT *>(a.out) + row * a.out_stride + col;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[e] = sum[i][j][e];
+                f[e + 4] = sum[i + 1][j][e];
+            }
+            if (col + 8 <= a.n) store8(q, f);
+            else if (col < a.n) store8(q, (int)(a.n - col), f);
+        }
+    }
+}
+
+// ---- products of few rows: the weights go by once ----
+//
+// A workgroup takes NT * 16 rows of the weights and all of the activations (MT * 16 rows at most); its waves divide the
+// columns among them, 256 at a time, and their sums are added up through LDS in their order.  Nothing is shared before
+// that, so the weights go from memory to registers, a lane's two blocks (32 bytes) of a row next to each other, the next
+// ones while the last are multiplied.  With BF16 the wave quantises the activations that it needs by itself: up to 16 rows
+// that costs less than a launch of its own.
+struct Blocks2 {                                // a lane's two blocks of one row
+    u32x4 code[2];
+    uint32_t scale;                             // one byte each
+};
+__device__ __forceinline__ void get_blocks(const uint8_t *codes, const uint8_t *scales, int64_t row, int b, int nb, Blocks2 &r) {
+    typedef uint16_t __attribute__((aligned(1))) u16_any;
+    const u32x4 *p = reinterpret_cast<const u32x4 *>(codes) + row * nb + b;
+    const uint8_t *s = scales + row * nb + b;
+    if (b + 2 <= nb) {
+        r.code[0] = p[0];
+        r.code[1] = p[1];
+        r.scale = *reinterpret_cast<const u16_any *>(s);
+    } else {
+        r.code[0] = b < nb ? p[0] : u32x4{0, 0, 0, 0};
+        r.code[1] = u32x4{0, 0, 0, 0};
+        r.scale = (b < nb ? s[0] : kOneScale) | kOneScale << 8;
+    }
+}
+struct Values2 {                                // the same before quantisation: 64 bf16
+    u32x4 v[8];
+};
+__device__ __forceinline__ void get_values(const bf16_t *row, int64_t col, int64_t cols, Values2 &r) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        Raw8<bf16_t> raw;
+        zero8(raw);
+        if (row && col + 8 * i + 8 <= cols) load8(row + col + 8 * i, raw);
+        else if (row && col + 8 * i < cols) load8(row + col + 8 * i, (int)(cols - col - 8 * i), raw);
+        r.v[i] = raw.v;
+    }
+}
+__device__ __forceinline__ void quantise(const Values2 &x, Blocks2 &r) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    r.scale = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x.v[4 * k + i / 4][i % 4] & 0x7FFF7FFFu));
+        const uint32_t scale = scale_of((uint32_t)(top[0] > top[1] ? top[0] : top[1]) << 16);
+        const float by = scale_value(scale);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair[4] = {x.v[4 * k + i][0], x.v[4 * k + i][1], x.v[4 * k + i][2], x.v[4 * k + i][3]};
+            uint32_t c = 0;
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[0]), by, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[1]), by, 1);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[2]), by, 2);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[3]), by, 3);
+            r.code[k][i] = scale == kNanScale ? 0 : c;
+        }
+        r.scale |= scale << (8 * k);
+    }
+}
+
+template <class OT, int MT, int NT, bool BF16>
+__global__ __launch_bounds__(1024) void mx4_few_kernel(Mx4ProductArgs a, int nb) {
+    extern __shared__ f32x4 sums[];             // [wave][tile][lane]
+    const int lane = threadIdx.x & 63, of16 = lane & 15, quarter = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int64_t n0 = (int64_t)blockIdx.x * (NT * 16);
+    int64_t w_row[NT], x_row[MT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) w_row[i] = n0 + i * 16 + of16 < a.n ? n0 + i * 16 + of16 : a.n - 1;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) x_row[j] = j * 16 + of16 < a.m ? j * 16 + of16 : a.m - 1;
+    f32x4 sum[NT][MT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bf16_t *values = BF16 && of16 < a.m ? static_cast<const bf16_t *>(a.x) + of16 * a.x_stride : nullptr;
+    Blocks2 w[2][NT], x[2][MT];
+    Values2 xv[2];
+    auto get = [&](int step, int buf) {
+        const int b = step * 8 + quarter * 2;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) get_blocks(a.w_codes, a.w_scales, w_row[i], b, nb, w[buf][i]);
+        if constexpr (BF16) get_values(values, (int64_t)b * ROSE_MX4_BLOCK, a.k, xv[buf]);
+        else
+#pragma unroll
+            for (int j = 0; j < MT; ++j) get_blocks(a.a_codes, a.a_scales, x_row[j], b, nb, x[buf][j]);
+    };
+    auto multiply = [&](int buf) {
+        if constexpr (BF16) quantise(xv[buf], x[buf][0]);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                sum[i][j] = product<0>(w[buf][i].code[0], w[buf][i].scale, x[buf][j].code[0], x[buf][j].scale, sum[i][j]);
+                sum[i][j] = product<1>(w[buf][i].code[1], w[buf][i].scale, x[buf][j].code[1], x[buf][j].scale, sum[i][j]);
+            }
+    };
+    const int steps = (nb + 7) / 8;
+    int step = wave;
+    if (step < steps) get(step, 0);
+    while (step < steps) {
+        if (step + waves < steps) get(step + waves, 1);
+        multiply(0);
+        step += waves;
+        if (step >= steps) break;
+        if (step + waves < steps) get(step + waves, 0);
+        multiply(1);
+        step += waves;
+    }
+    if (waves > 1) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) sums[(wave * (NT * MT) + i * MT + j) * 64 + lane] = sum[i][j];
+        __syncthreads();
+    }
+    // tiles in turn to the waves: four neighbouring outputs a lane
+#pragma unroll
+    for (int t = 0; t < NT * MT; ++t) {
+        if (t % waves != wave) continue;
+        f32x4 s = sum[t / MT][t % MT];
+        if (waves > 1) {
+            s = sums[t * 64 + lane];
+            for (int v = 1; v < waves; ++v) s += sums[(v * (NT * MT) + t) * 64 + lane];
+        }
+        const int64_t row = (t % MT) * 16 + of16, col = n0 + (t / MT) * 16 + quarter * 4;
+        if (row >= a.m) continue;
+        OT *q = static_cast<OT *>(a.out) + row * a.out_stride + col;
+        typedef uint64_t __attribute__((aligned(2))) u64_any;
+        if (col + 4 > a.n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < a.n) q[e] = from_f32<OT>(s[e]);
+        } else if constexpr (sizeof(OT) == 4) *reinterpret_cast<f32x4_any *>(q) = s;
+        else *reinterpret_cast<u64_any *>(q) = (uint64_t)pack_bf16(s[2], s[3]) << 32 | pack_bf16(s[0], s[1]);
+    }
 }
 
 int64_t blocks_of(int64_t cols) { return (cols + ROSE_MX4_BLOCK - 1) / ROSE_MX4_BLOCK; }
@@ -153,16 +494,41 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
     return (int)hipGetLastError();
 }
 
-bool mx4_product_takes_bf16(int64_t) { return false; }
+bool mx4_product_takes_bf16(int64_t m) { return m <= 16; }
+
+template <int MT, int NT, bool BF16>
+static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
+    const int64_t groups = (a.n + NT * 16 - 1) / (NT * 16), steps = (blocks_of(a.k) + 7) / 8;
+    // waves a workgroup: about sixteen for every CU together, two steps each at least
+    int waves = 1;
+    while (waves < 16 && groups * waves < 4096 && waves * 4 <= steps) waves *= 2;
+    const dim3 grid((unsigned)groups), block(64 * waves);
+    const size_t lds = waves > 1 ? (size_t)waves * NT * MT * 1024 : 0;
+    if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, lds, st, a, (int)blocks_of(a.k));
+    else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, lds, st, a, (int)blocks_of(a.k));
+    return (int)hipGetLastError();
+}
+
+template <int BN, int BM, int WN, int WM>
+static int launch_tiles(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
+    const int64_t n_tiles = (a.n + BN - 1) / BN, m_tiles = (a.m + BM - 1) / BM;
+    if (n_tiles * m_tiles > 0x7FFFFFFF / 8) return (int)hipErrorInvalidValue;
+    const dim3 grid((unsigned)(n_tiles * m_tiles)), block(64 * WN * WM);
+    if (out_f32) hipLaunchKernelGGL((mx4_tile_kernel<float, BN, BM, WN, WM>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
+    else hipLaunchKernelGGL((mx4_tile_kernel<bf16_t, BN, BM, WN, WM>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
+    return (int)hipGetLastError();
+}
 
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.m == 0 || a.n == 0) return 0;
-    const int64_t n_tiles = (a.n + 15) / 16, tiles = n_tiles * ((a.m + 15) / 16), grid = (tiles + kThreads / 64 - 1) / (kThreads / 64);
-    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    if (out_f32) hipLaunchKernelGGL(mx4_product_kernel<float>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, blocks_of(a.k), n_tiles, tiles);
-    else hipLaunchKernelGGL(mx4_product_kernel<bf16_t>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, blocks_of(a.k), n_tiles, tiles);
-    return (int)hipGetLastError();
+    if (a.m <= 16) return a.x ? launch_few<1, 1, true>(a, out_f32, st) : launch_few<1, 1, false>(a, out_f32, st);
+    if (a.m <= 32) return launch_few<2, 1, false>(a, out_f32, st);
+    if (a.m <= 64) return launch_few<4, 1, false>(a, out_f32, st);
+    // 256 x 256 tiles move half of what 128 x 128 ones do but fill a CU each; the smaller ones, two a CU, where there are few
+    // (256 x 19008 x 5120: 38.5 us with the large ones, 28.8 with the small; 4096 x 4096 x 4096: 39.8 and 48.7).
+    const int64_t large = ((a.n + 255) / 256) * ((a.m + 255) / 256);
+    return large >= 192 ? launch_tiles<256, 256, 4, 2>(a, out_f32, st) : launch_tiles<128, 128, 2, 2>(a, out_f32, st);
 }
 
 }  // namespace rose

@@ -43,6 +43,10 @@ rose_status check_mx4(const void *codes, const void *scales, int64_t rows, int64
     return aligned(codes, 16) ? ROSE_OK : ROSE_ERR_ALIGN;
 }
 
+// What a product can address: a tile of 256 rows within 32 bits of bytes.
+constexpr int64_t kMostProductCols = (int64_t)1 << 24;
+rose_status check_product_cols(int64_t k) { return k < kMostProductCols ? ROSE_OK : ROSE_ERR_UNSUPPORTED; }
+
 rose_status status_of(int hip_error) { return hip_error == 0 ? ROSE_OK : ROSE_ERR_HIP; }
 
 int64_t blocks_of(int64_t cols) { return (cols + ROSE_MX4_BLOCK - 1) / ROSE_MX4_BLOCK; }
@@ -142,6 +146,7 @@ extern "C" rose_status rose_mx4_matmul(const uint8_t *a_codes, const uint8_t *a_
                                        int64_t out_stride, void *stream) {
     ROSE_CHECK(check_mx4(a_codes, a_scales, m, k));
     ROSE_CHECK(check_mx4(w_codes, w_scales, n, k));
+    ROSE_CHECK(check_product_cols(k));
     ROSE_CHECK(check_matrix(out, out_dtype, m, n, out_stride));
     rose::Mx4ProductArgs a = {nullptr, 0, a_codes, a_scales, w_codes, w_scales, out, m, n, k, out_stride};
     return status_of(rose::launch_mx4_product(a, out_dtype == ROSE_DTYPE_F32, stream));
@@ -159,6 +164,7 @@ extern "C" rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m
                                        int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream) {
     ROSE_CHECK(check_matrix(x, x_dtype, m, k, x_stride));
     ROSE_CHECK(check_mx4(w_codes, w_scales, n, k));
+    ROSE_CHECK(check_product_cols(k));
     ROSE_CHECK(check_matrix(out, out_dtype, m, n, out_stride));
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, linear_workspace(m, k)));
     rose::Mx4ProductArgs a = {nullptr, 0, nullptr, nullptr, w_codes, w_scales, out, m, n, k, out_stride};
