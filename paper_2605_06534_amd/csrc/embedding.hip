@@ -9,11 +9,12 @@ namespace {
 constexpr int kLookupThreads = 256;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
-constexpr int kSmallItems = 16;                 // items a thread of the one-workgroup sort takes at most
+constexpr int kSmallBits = 5;                   // digits of the one-workgroup sort
+constexpr int kSmallItems = 16;                 // tokens a thread of it takes at most
 constexpr int64_t kSmallTokens = (int64_t)kSortThreads * kSmallItems;
 constexpr int kTileItems = 2, kTile = kSortThreads * kTileItems;   // tokens that a workgroup of the large sort takes at a time
 constexpr int kMostTiles = 256;
-constexpr int kRun = 32;                        // sorted tokens that are summed in one go
+constexpr int64_t kShortestRun = 32;            // sorted tokens that are summed in one go
 
 // row of the table that a token names, rows if none
 __device__ __forceinline__ uint32_t row_of(const Tokens &t, int64_t i) {
@@ -26,15 +27,13 @@ __device__ __forceinline__ uint32_t row_of(const Tokens &t, int64_t i) {
 // lookup
 // -------------------------------------------------------------------------------------------------
 // A row goes to 1 << log_lanes lanes, eight columns each; R rows a lane, all of them asked for before the first is used.
-template <class TT, class OT, int R>
+template <class TT, class OT, int R, bool NARROW>
 __global__ __launch_bounds__(kLookupThreads) void embedding_lookup_kernel(LookupArgs a, int log_lanes, uint32_t chunks) {
     const uint32_t group = blockIdx.x / chunks, chunk = blockIdx.x - group * chunks;
     const int lane = threadIdx.x & ((1 << log_lanes) - 1), sub = threadIdx.x >> log_lanes;
     const int per = kLookupThreads >> log_lanes;
-    const int64_t col = ((int64_t)chunk * kLookupThreads + lane) * 8;
-    if (col >= a.cols) return;
-    const int here = (int)(a.cols - col < 8 ? a.cols - col : 8);
-    const TT *table = static_cast<const TT *>(a.table) + col;
+    const Columns<NARROW> col(((int64_t)chunk * kLookupThreads + lane) * 8, a.cols);
+    if (!col.n) return;
     const int64_t i0 = (int64_t)group * (R * per) + sub;
     uint32_t row[R];
 #pragma unroll
@@ -43,11 +42,7 @@ __global__ __launch_bounds__(kLookupThreads) void embedding_lookup_kernel(Lookup
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         zero8(raw[r]);
-        if (row[r] < a.tokens.rows) {
-            const TT *p = table + (int64_t)row[r] * a.table_stride;
-            if (here == 8) load8(p, raw[r]);
-            else load8(p, here, raw[r]);
-        }
+        if (row[r] < a.tokens.rows) col.load(static_cast<const TT *>(a.table) + (int64_t)row[r] * a.table_stride, raw[r]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -57,9 +52,7 @@ __global__ __launch_bounds__(kLookupThreads) void embedding_lookup_kernel(Lookup
         // (zeros stay zeros under any scale: of another shard, not 0 * inf)
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = row[r] < a.tokens.rows ? f[e] * a.scale : 0.f;
-        OT *q = static_cast<OT *>(a.out) + (i0 + r * per) * a.out_stride + col;
-        if (here == 8) store8(q, f);
-        else store8(q, here, f);
+        col.store(static_cast<OT *>(a.out) + (i0 + r * per) * a.out_stride, f);
     }
 }
 
@@ -154,60 +147,105 @@ struct SortArgs {
     uint32_t *counts;                           // large sort: [pass][tile][bin]
     int32_t bits, passes, width;                // bits of a row number, passes of `width` bits
     int32_t tiles, subtiles;                    // tiles of subtiles * kTile tokens
+    int32_t place_bits;                         // small sort: bits of a token's number, below those of its row
     Fill fill;
 };
 
-// Up to kSmallTokens tokens: one workgroup holds them all.
+// Up to kSmallTokens tokens: one workgroup holds them all, row and token of each in one word.  A thread has ITEMS neighbouring
+// ones; it counts their digits in counters of its own (16 bits, two threads' in a word), which an item's rank comes from, and
+// prefix sums over all threads of a digit, then over the digits, say where its items go.  (Ranks from ballots over the waves, as
+// below: 35 us for 8191 tokens and 15 bits; the vector instructions of one CU bound that.)
 template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SortArgs a) {
-    __shared__ SortShared s;
-    __shared__ uint32_t keys[kSortThreads * ITEMS], places[kSortThreads * ITEMS];
+    constexpr int kFew = 1 << kSmallBits;
+    __shared__ __attribute__((aligned(16))) uint16_t counts[kFew][kSortThreads];
+    __shared__ __attribute__((aligned(16))) uint32_t items[kSortThreads * ITEMS];
+    __shared__ uint32_t totals[kFew];
     if (blockIdx.x > 0) {
         fill_zeros(a.fill, blockIdx.x - 1);
         return;
     }
-    const int n = (int)a.tokens.n, wave = threadIdx.x >> 6;
-    const int first = wave * 64 * ITEMS + (threadIdx.x & 63);
-    uint32_t key[ITEMS], place[ITEMS], digit[ITEMS], rank[ITEMS];
-    bool valid[ITEMS];
+    const int n = (int)a.tokens.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = threadIdx.x * ITEMS;
+    // (what is behind the last token has the largest key there is and stays behind)
+    for (int i = threadIdx.x; i < kSortThreads * ITEMS; i += kSortThreads)
+        items[i] = i < n ? row_of(a.tokens, i) << a.place_bits | (uint32_t)i : 0xFFFFFFFFu;
+    __syncthreads();
+    uint32_t item[ITEMS], rank[ITEMS];
+    auto load = [&] {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        place[i] = first + 64 * i;
-        valid[i] = (int)place[i] < n;
-        key[i] = valid[i] ? row_of(a.tokens, place[i]) : 0;
-    }
-    for (int pass = 0; pass < a.passes; ++pass) {
-        clear_counts(s);
-        __syncthreads();
+        for (int i = 0; i < ITEMS; i += ITEMS < 4 ? 1 : 4) {
+            if constexpr (ITEMS < 4) item[i] = items[first + i];
+            else {
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(items + first + i);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) digit[i] = (key[i] >> (pass * a.width)) & ((1u << a.width) - 1);
-        rank_items(s, digit, valid, a.width, rank);
-        __syncthreads();
-        const uint32_t total = threadIdx.x < kBins ? scan_waves(s, threadIdx.x) : 0;
-        const uint32_t start = exclusive_scan(s, total);
-        if (threadIdx.x < kBins) s.start[threadIdx.x] = start;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-            if (valid[i]) {
-                const uint32_t to = s.start[digit[i]] + s.before[wave][digit[i]] + rank[i];
-                keys[to] = key[i];
-                places[to] = place[i];
+                for (int e = 0; e < 4; ++e) item[i + e] = v[e];
             }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-            if (valid[i]) {
-                key[i] = keys[first + 64 * i];
-                place[i] = places[first + 64 * i];
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-        if (valid[i]) {
-            a.keys[0][first + 64 * i] = key[i];
-            a.places[0][first + 64 * i] = place[i];
         }
+    };
+    load();
+    for (int shift = a.place_bits; shift < a.place_bits + a.bits; shift += kSmallBits) {
+        u32x4 *clear = reinterpret_cast<u32x4 *>(counts);
+        for (int i = threadIdx.x; i < (int)(sizeof counts / 16); i += kSortThreads) clear[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        const int half = 16 * (threadIdx.x & 1);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            uint32_t *counter = reinterpret_cast<uint32_t *>(&counts[(item[i] >> shift) & (kFew - 1)][threadIdx.x & ~1]);
+            rank[i] = (atomicAdd(counter, 1u << half) >> half) & 0xFFFFu;
+        }
+        __syncthreads();
+        // a digit a wave at a time: eight threads' counts a lane, and the other half of the threads behind them
+        for (int digit = wave; digit < kFew; digit += kSortWaves) {
+            uint32_t before = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 *at = reinterpret_cast<u32x4 *>(&counts[digit][h * 512 + lane * 8]);
+                const u32x4 c = *at;
+                uint32_t sums[8], sum = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sums[e] = sum;
+                    sum += (c[e / 2] >> (16 * (e & 1))) & 0xFFFFu;
+                }
+                uint32_t up_to = sum;
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const uint32_t up = __shfl_up(up_to, d);
+                    if (lane >= d) up_to += up;
+                }
+                const uint32_t base = before + up_to - sum;
+                u32x4 out;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = (base + sums[2 * e]) | (base + sums[2 * e + 1]) << 16;
+                *at = out;
+                before += __shfl(up_to, 63);
+            }
+            if (lane == 0) totals[digit] = before;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const uint32_t total = lane < kFew ? totals[lane] : 0;
+            uint32_t up_to = total;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const uint32_t up = __shfl_up(up_to, d);
+                if (lane >= d) up_to += up;
+            }
+            if (lane < kFew) totals[lane] = up_to - total;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int digit = (item[i] >> shift) & (kFew - 1);
+            items[totals[digit] + counts[digit][threadIdx.x] + rank[i]] = item[i];
+        }
+        __syncthreads();
+        load();
+    }
+    for (int i = threadIdx.x; i < n; i += kSortThreads) {
+        a.keys[0][i] = items[i] >> a.place_bits;
+        a.places[0][i] = items[i] & ((1u << a.place_bits) - 1);
+    }
 }
 
 // More: how often each digit of the first pass comes in each tile; the counts of later passes become zero.
@@ -242,6 +280,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(SortArgs a, int
     uint32_t *keys_out = a.keys[pass & 1], *places_out = a.places[pass & 1];
     uint32_t total = 0, before = 0;
     if (threadIdx.x < kBins)
+#pragma unroll 16
         for (int t = 0; t < a.tiles; ++t) {
             const uint32_t c = counts[(int64_t)t * kBins + threadIdx.x];
             total += c;
@@ -291,115 +330,171 @@ struct SumArgs {
     const void *dy;
     void *grad;
     float *parts;                               // [block][2][parts_stride]: sums of runs that begin before the block, behind it
-    int64_t parts_stride;
-    uint32_t chunks;
+    int64_t parts_stride, run;                  // run: tokens of a block
+    uint32_t chunks;                            // a row's columns go to this many waves ...
+    int32_t lanes;                              // ... of so many lanes
     float scale;
     int32_t accumulate;
 };
 
-template <class GT>
-__device__ __forceinline__ void write_grad(const SumArgs &a, uint32_t row, int64_t col, int here, float (&sum)[8]) {
-    GT *p = static_cast<GT *>(a.grad) + (int64_t)row * a.grad_stride + col;
-    float old[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.accumulate) {
-        Raw8<GT> r;
-        if (here == 8) load8(p, r);
-        else load8(p, here, r);
-        widen8(r, old);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = old[e] + sum[e] * a.scale;
-    if (here == 8) store8(p, sum);
-    else store8(p, here, sum);
-}
-
-// kRun sorted tokens and up to eight columns a lane.  A row whose tokens all lie in the block is finished here; what
-// crosses the block's ends is left for join_kernel.
-template <class DT, class GT>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a) {
-    constexpr int kAhead = 8;
-    const uint32_t block = blockIdx.x / a.chunks, chunk = blockIdx.x - block * a.chunks;
-    const int64_t from = (int64_t)block * kRun, to = from + kRun < a.n ? from + kRun : a.n;
-    const int64_t col = ((int64_t)chunk * blockDim.x + threadIdx.x) * 8;
-    if (a.keys[from] >= a.rows || col >= a.cols) return;
-    const int here = (int)(a.cols - col < 8 ? a.cols - col : 8);
-    const DT *dy = static_cast<const DT *>(a.dy) + col;
-    float *parts = a.parts + (int64_t)block * 2 * a.parts_stride + col;
-    bool open = from > 0 && a.keys[from - 1] == a.keys[from];       // the run began before the block
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t j0 = from; j0 < to; j0 += kAhead) {
-        uint32_t key[kAhead + 1];
-        Raw8<DT> raw[kAhead];
-#pragma unroll
-        for (int u = 0; u <= kAhead; ++u) key[u] = j0 + u < a.n ? a.keys[j0 + u] : 0xFFFFFFFFu;
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (j0 + u < to && key[u] < a.rows) {
-                const DT *p = dy + (int64_t)a.places[j0 + u] * a.dy_stride;
-                if (here == 8) load8(p, raw[u]);
-                else load8(p, here, raw[u]);
-            }
+// A block of sorted tokens and eight columns a lane, one wave a workgroup.  A row whose tokens all lie in the block is
+// finished here; what crosses the block's ends is left for the join.  Rows come kAhead at a time, the next ones asked for before
+// the last are added, and with them (ADD) what is in the gradient of the rows that end among them: a load where a run ends would
+// wait for all that were asked for before it, stores included.
+template <class DT, class GT, bool NARROW, bool ADD>
+__global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
+    constexpr int kAhead = ADD ? 4 : 8;
+    constexpr int kWindow = 32;
+    // Workgroups i, i + 8, ... run on one XCD; all columns of a block go to one.  (With each column of waves on an XCD of its own,
+    // as where there are eight of them, an XCD reads the same kilobyte of every row: a quarter of its L2's channels.)
+    const uint32_t turn = blockIdx.x >> 3, chunk = turn % a.chunks;
+    const int64_t block = (int64_t)(turn / a.chunks) * 8 + (blockIdx.x & 7);
+    if (block * a.run >= a.n) return;
+    const int lane = threadIdx.x;
+    const int64_t from = block * a.run, to = from + a.run < a.n ? from + a.run : a.n;
+    const uint32_t first_key = a.keys[from], first_place = a.places[from], last_key = from > 0 ? a.keys[from - 1] : 0xFFFFFFFFu;
+    if (first_key >= a.rows) return;
+    const int64_t lane_of_row = (int64_t)chunk * a.lanes + lane;
+    const Columns<NARROW> col(lane < a.lanes ? lane_of_row * 8 : a.cols, a.cols);
+    float *parts = a.parts + block * 2 * a.parts_stride;
+    // Rows and tokens of 64 positions from a window's first on, a lane each: read from there without another trip to memory.
+    // Positions behind the block name its first token, so that loads need no condition.
+    uint32_t keys, places, next_keys, next_places;
+    auto look = [&](int64_t j) {
+        next_keys = j + lane < a.n ? a.keys[j + lane] : 0xFFFFFFFFu;
+        next_places = j + lane < to ? a.places[j + lane] : first_place;
+    };
+    auto key_at = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane(keys, i); };
+    Raw8<DT> raw[2][kAhead];
+    Raw8<GT> old[2][ADD ? kAhead : 1];
+    auto get = [&](int64_t window, int i0, int which) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (j0 + u >= to || key[u] >= a.rows) return;
+            col.load(static_cast<const DT *>(a.dy) + (int64_t)(uint32_t)__builtin_amdgcn_readlane(places, i0 + u) * a.dy_stride, raw[which][u]);
+            if constexpr (ADD) {
+                const uint32_t key = key_at(i0 + u);
+                if (key < a.rows && key_at(i0 + u + 1) != key && window + i0 + u < to)
+                    col.load(static_cast<const GT *>(a.grad) + (int64_t)key * a.grad_stride, old[which][u]);
+            }
+        }
+    };
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    bool open = last_key == first_key;                  // the run began before the block
+    auto add = [&](int64_t window, int i0, int which) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t j = window + i0 + u;
+            const uint32_t key = key_at(i0 + u);
+            if (j >= to || key >= a.rows) return false;
             float f[8];
-            widen8(raw[u], f);
+            widen8(raw[which][u], f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += f[e];
-            const bool ends = key[u + 1] != key[u], last = j0 + u + 1 == to;
-            if (ends && !open) write_grad<GT>(a, key[u], col, here, sum);
-            else if (ends || last) store8(parts + (open ? 0 : a.parts_stride), sum);
+            const bool ends = key_at(i0 + u + 1) != key;
+            if (ends && !open) {
+                if constexpr (ADD) {
+                    widen8(old[which][u], f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] = f[e] + sum[e] * a.scale;
+                } else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] *= a.scale;
+                col.store(static_cast<GT *>(a.grad) + (int64_t)key * a.grad_stride, sum);
+            } else if (ends || j + 1 == to) col.store(parts + (open ? 0 : a.parts_stride), sum);
             if (ends) {
                 open = false;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] = 0.f;
             }
         }
+        return true;
+    };
+    look(from);
+    keys = next_keys;
+    places = next_places;
+    get(from, 0, 0);
+    for (int64_t window = from; window < to; window += kWindow) {
+        look(window + kWindow);
+        for (int i = 0; i < kWindow; i += 2 * kAhead) {
+            get(window, i + kAhead, 1);
+            if (!add(window, i, 0)) return;
+            get(window, i + 2 * kAhead, 0);
+            if (!add(window, i + kAhead, 1)) return;
+        }
+        keys = next_keys;
+        places = next_places;
     }
 }
 
-// A run that crosses the end of the block it begins in: the sums of its parts, one after the other; the waves take every
-// fourth, and their sums are added in order.  Four columns a lane.
+// A run that crosses the end of the block it begins in: the sums of its parts.  Four columns a lane; where there are few
+// parts each of the four waves adds those of its own 256 columns, where there are many the waves take every fourth part and
+// their sums are added in order, 256 columns after the other.
 template <class GT>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, uint32_t chunks) {
     __shared__ f32x4 sums[4][64];
     const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x - block * chunks;
-    const int64_t from = (int64_t)block * kRun, next = from + kRun;
-    const uint32_t key = a.keys[next];
-    if (key >= a.rows || a.keys[next - 1] != key || (from > 0 && a.keys[from - 1] == key)) return;
-    int64_t lo = next, hi = a.n;                 // the run ends in front of the first other row from lo on
+    const int64_t from = (int64_t)block * a.run, next = from + a.run;
+    const uint32_t key = a.keys[next], in_front = a.keys[next - 1], before = from > 0 ? a.keys[from - 1] : 0xFFFFFFFFu;
+    if (key >= a.rows || in_front != key || before == key) return;
+    // the run ends in front of the first other row: looked for block by block (in most cases the next one), then by halves
+    int64_t lo = next, hi = a.n, step = a.run;
+    while (lo + step < a.n && a.keys[lo + step] == key) {
+        lo += step;
+        step *= 2;
+    }
+    if (lo + step < hi) hi = lo + step;
     while (lo < hi) {
         const int64_t mid = lo + (hi - lo) / 2;
         if (a.keys[mid] == key) lo = mid + 1;
         else hi = mid;
     }
-    const int64_t last = (lo - 1) / kRun;
+    const int64_t last = (lo - 1) / a.run;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = ((int64_t)chunk * 64 + lane) * 4;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (col < a.cols) {
+    auto add = [&](int64_t col, int64_t first, int64_t hop) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         const float *parts = a.parts + col;
-        for (int64_t b = block + wave; b <= last; b += 4)
+#pragma unroll 4
+        for (int64_t b = block + first; b <= last; b += hop)
             sum += *reinterpret_cast<const f32x4 *>(parts + (2 * b + (b == block ? 1 : 0)) * a.parts_stride);
-    }
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave > 0 || col >= a.cols) return;
-    sum = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
-    GT *p = static_cast<GT *>(a.grad) + (int64_t)key * a.grad_stride + col;
+        return sum;
+    };
+    auto write = [&](int64_t col, f32x4 sum) {
+        GT *p = static_cast<GT *>(a.grad) + (int64_t)key * a.grad_stride + col;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (col + e < a.cols) p[e] = from_f32<GT>((a.accumulate ? to_f32(p[e]) : 0.f) + sum[e] * a.scale);
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.cols) p[e] = from_f32<GT>((a.accumulate ? to_f32(p[e]) : 0.f) + sum[e] * a.scale);
+    };
+    const int64_t first_col = (int64_t)chunk * 1024;
+    if (last - block < 16) {
+        const int64_t col = first_col + wave * 256 + lane * 4;
+        if (col < a.cols) write(col, add(col, 0, 1));
+        return;
+    }
+    for (int64_t c = first_col; c < first_col + 1024 && c < a.cols; c += 256) {
+        const int64_t col = c + lane * 4;
+        if (col < a.cols) sums[wave][lane] = add(col, wave, 4);
+        __syncthreads();
+        if (wave == 0 && col < a.cols) write(col, ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane]);
+        __syncthreads();
+    }
 }
 
 // where things lie in the workspace
 struct GradLayout {
-    int64_t blocks, parts_stride;
+    int64_t run, blocks, parts_stride;
     int32_t tiles, subtiles;
     bool small;
     size_t keys[2], places[2], counts, parts, total;
 };
-GradLayout grad_layout(int64_t cols, int64_t n) {
+int bits_of(int64_t v) {
+    int bits = 1;
+    while (v >> bits) ++bits;
+    return bits;
+}
+// one workgroup sorts: all tokens in its LDS, row (the number of rows is one too: that of no row) and token in 32 bits; a
+// word of ones is none of them
+bool small_sort(int64_t rows, int64_t n) { return n <= kSmallTokens && bits_of(rows) + bits_of(n) <= 32; }
+GradLayout grad_layout(int64_t rows, int64_t cols, int64_t n) {
     GradLayout l = {};
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -407,7 +502,7 @@ GradLayout grad_layout(int64_t cols, int64_t n) {
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    l.small = n <= kSmallTokens;
+    l.small = small_sort(rows, n);
     for (int i = 0; i < (l.small ? 1 : 2); ++i) {
         l.keys[i] = take((size_t)n * 4);
         l.places[i] = take((size_t)n * 4);
@@ -417,7 +512,11 @@ GradLayout grad_layout(int64_t cols, int64_t n) {
         l.tiles = (int32_t)((n + (int64_t)l.subtiles * kTile - 1) / ((int64_t)l.subtiles * kTile));
         l.counts = take((size_t)4 * l.tiles * kBins * 4);
     }
-    l.blocks = (n + kRun - 1) / kRun;
+    // blocks as short as fill the chip, but no shorter: each leaves parts of two runs to be joined
+    const int64_t waves = (cols + 511) / 512;
+    l.run = kShortestRun;
+    while (l.run * 8192 < n * waves && l.run < 4096) l.run *= 2;
+    l.blocks = (n + l.run - 1) / l.run;
     l.parts_stride = (cols + 7) / 8 * 8;
     l.parts = take(l.blocks > 1 ? (size_t)l.blocks * 2 * (size_t)l.parts_stride * 4 : 0);
     l.total = at;
@@ -426,7 +525,7 @@ GradLayout grad_layout(int64_t cols, int64_t n) {
 
 }  // namespace
 
-size_t embedding_grad_workspace(int64_t, int64_t cols, int64_t n_tokens) { return grad_layout(cols, n_tokens).total; }
+size_t embedding_grad_workspace(int64_t rows, int64_t cols, int64_t n_tokens) { return grad_layout(rows, cols, n_tokens).total; }
 
 int launch_embedding_lookup(const LookupArgs &a, bool table_f32, bool out_f32, void *stream) {
     if (a.tokens.n == 0 || a.cols == 0) return 0;
@@ -434,18 +533,19 @@ int launch_embedding_lookup(const LookupArgs &a, bool table_f32, bool out_f32, v
     int log_lanes = 2;
     while (log_lanes < 8 && ((int64_t)8 << log_lanes) < a.cols) ++log_lanes;
     const int64_t chunks = (a.cols + kLookupThreads * 8 - 1) / (kLookupThreads * 8), per = kLookupThreads >> log_lanes;
-    const bool many = (a.tokens.n / per) * chunks >= 8192;       // enough for every CU also at four rows a lane
+    const bool many = a.cols >= 8 && (a.tokens.n / per) * chunks >= 8192;       // enough for every CU also at four rows a lane
     const int64_t groups = (a.tokens.n + per * (many ? 4 : 1) - 1) / (per * (many ? 4 : 1));
     if (groups * chunks > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
     const dim3 grid((unsigned)(groups * chunks)), block(kLookupThreads);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, log_lanes, (uint32_t)chunks); };
-    if (many) {
-        if (table_f32) out_f32 ? go(embedding_lookup_kernel<float, float, 4>) : go(embedding_lookup_kernel<float, bf16_t, 4>);
-        else out_f32 ? go(embedding_lookup_kernel<bf16_t, float, 4>) : go(embedding_lookup_kernel<bf16_t, bf16_t, 4>);
-    } else {
-        if (table_f32) out_f32 ? go(embedding_lookup_kernel<float, float, 1>) : go(embedding_lookup_kernel<float, bf16_t, 1>);
-        else out_f32 ? go(embedding_lookup_kernel<bf16_t, float, 1>) : go(embedding_lookup_kernel<bf16_t, bf16_t, 1>);
-    }
+    auto of_types = [&](auto t, auto o) {
+        using TT = decltype(t);
+        using OT = decltype(o);
+        if (a.cols < 8) go(embedding_lookup_kernel<TT, OT, 1, true>);
+        else many ? go(embedding_lookup_kernel<TT, OT, 4, false>) : go(embedding_lookup_kernel<TT, OT, 1, false>);
+    };
+    if (table_f32) out_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
+    else out_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
     return (int)hipGetLastError();
 }
 
@@ -453,7 +553,7 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t n = a.tokens.n, rows = a.tokens.rows;
     if (rows == 0 || a.cols == 0 || (n == 0 && a.accumulate)) return 0;
-    const GradLayout l = grad_layout(a.cols, n);
+    const GradLayout l = grad_layout(rows, a.cols, n);
     SortArgs s = {};
     s.tokens = a.tokens;
     for (int i = 0; i < 2; ++i) {
@@ -461,8 +561,8 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
         s.places[i] = reinterpret_cast<uint32_t *>(a.workspace + l.places[i]);
     }
     s.counts = reinterpret_cast<uint32_t *>(a.workspace + l.counts);
-    s.bits = 1;
-    while (rows >> s.bits) ++s.bits;             // the number of rows itself is a key: that of no row
+    s.bits = bits_of(rows);
+    s.place_bits = bits_of(n);
     s.passes = (s.bits + kDigitBits - 1) / kDigitBits;
     s.width = (s.bits + s.passes - 1) / s.passes;
     s.tiles = l.tiles;
@@ -506,15 +606,26 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     u.parts_stride = l.parts_stride;
     u.scale = a.scale;
     u.accumulate = a.accumulate;
-    const int64_t lanes = (a.cols + 7) / 8, threads = lanes >= 256 ? 256 : (lanes + 63) / 64 * 64;
-    const int64_t chunks = (lanes + threads - 1) / threads, join_chunks = (a.cols + 255) / 256;
+    u.run = l.run;
+    // waves of as many lanes as another, and none of a single one, which would share columns with another wave (see Columns)
+    const int64_t vectors = (a.cols + 7) / 8;
+    int64_t chunks = (vectors + 63) / 64, lanes = (vectors + chunks - 1) / chunks;
+    while (vectors > 1 && vectors % lanes == 1) --lanes;
+    chunks = (vectors + lanes - 1) / lanes;
+    const int64_t join_chunks = (a.cols + 1023) / 1024;
+    u.lanes = (int32_t)lanes;
     u.chunks = (uint32_t)chunks;
-    if (l.blocks * chunks > 0x7FFFFFFF || l.blocks * join_chunks > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    auto sum = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(l.blocks * chunks)), dim3((unsigned)threads), 0, st, u);
+    const int64_t grid = (l.blocks + 7) / 8 * 8 * chunks;
+    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64), 0, st, u); };
+    auto of_types = [&](auto d, auto g) {
+        using DT = decltype(d);
+        using GT = decltype(g);
+        if (a.cols < 8) a.accumulate ? sum(embedding_sum_kernel<DT, GT, true, true>) : sum(embedding_sum_kernel<DT, GT, true, false>);
+        else a.accumulate ? sum(embedding_sum_kernel<DT, GT, false, true>) : sum(embedding_sum_kernel<DT, GT, false, false>);
     };
-    if (dy_f32) grad_f32 ? sum(embedding_sum_kernel<float, float>) : sum(embedding_sum_kernel<float, bf16_t>);
-    else grad_f32 ? sum(embedding_sum_kernel<bf16_t, float>) : sum(embedding_sum_kernel<bf16_t, bf16_t>);
+    if (dy_f32) grad_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
+    else grad_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
     if (l.blocks > 1) {
         auto join = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((l.blocks - 1) * join_chunks)), dim3(256), 0, st, u, (uint32_t)join_chunks);

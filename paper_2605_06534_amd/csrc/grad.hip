@@ -7,24 +7,36 @@ namespace rose {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kShare = 8192;                    // a workgroup's share of the elements is a multiple of this
+constexpr int kWorkgroups = 2048;                // at most: eight a CU
+constexpr int64_t kSmallPiece = 8192, kLargePiece = 32768;
 
-// The share of workgroup `index` of `count`, as positions in all tensors laid end to end.
-__device__ __forceinline__ void share_of(int64_t total, int64_t index, int64_t count, int64_t &from, int64_t &to) {
-    const int64_t per = ((total + count - 1) / count + kShare - 1) / kShare * kShare;
-    from = index * per < total ? index * per : total;
-    to = from + per < total ? from + per : total;
+// All tensors laid end to end are cut into pieces, which the workgroups take in turn.
+__device__ __forceinline__ int64_t piece_of(int64_t total) {
+    return total <= kWorkgroups * kSmallPiece ? kSmallPiece : kLargePiece;
 }
 
-// the tensor that holds position `at`: the last one that begins at or before it
+// The tensor that holds position `at`: the last one that begins at or before it, 64 candidates at a time.
 __device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, int64_t at) {
-    int32_t lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int32_t mid = (lo + hi + 1) / 2;
-        if (offsets[mid] <= at) lo = mid;
-        else hi = mid - 1;
+    const int lane = threadIdx.x & 63;
+    int32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int32_t step = (hi - lo + 63) / 64, mine = lo + lane * step;
+        const uint64_t begun = __ballot(mine < hi && offsets[mine] <= at);
+        lo += (64 - __clzll((long long)begun) - 1) * step;           // (the first of them has begun, and so have all before the last)
+        hi = lo + step < hi ? lo + step : hi;
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Calls f(tensor, first element, number) for the stretch of every tensor that lies in [from, to).
+template <class F>
+__device__ __forceinline__ void for_stretches(const GradArgs &a, int64_t from, int64_t to, F f) {
+    for (int32_t t = tensor_at(a.offsets, a.n_tensors, from); t < a.n_tensors; ++t) {
+        const int64_t base = a.offsets[t], end = a.offsets[t + 1];
+        if (base >= to) return;
+        const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
+        if (lo < hi) f(t, lo - base, hi - lo);
+    }
 }
 
 __device__ __forceinline__ double squares(const float (&f)[8]) {
@@ -93,16 +105,13 @@ __device__ __forceinline__ double squares_of(const T *p, int64_t n) {
 template <class T>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradArgs a) {
     __shared__ double waves[kThreads / 64];
-    int64_t from, to;
-    share_of(a.offsets[a.n_tensors], blockIdx.x, gridDim.x, from, to);
+    const int64_t total = a.offsets[a.n_tensors], piece = piece_of(total);
     double s = 0;
-    if (from < to)
-        for (int32_t t = tensor_at(a.offsets, a.n_tensors, from); t < a.n_tensors && a.offsets[t] < to; ++t) {
-            const int64_t base = a.offsets[t], end = a.offsets[t + 1];
-            const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
+    for (int64_t from = blockIdx.x * piece; from < total; from += gridDim.x * piece)
+        for_stretches(a, from, from + piece < total ? from + piece : total, [&](int32_t t, int64_t first, int64_t n) {
             const T *p = static_cast<const T *>(a.grad_ptrs[t]);
-            if (p && lo < hi) s += squares_of(p + (lo - base), hi - lo);
-        }
+            if (p) s += squares_of(p + first, n);
+        });
     s = sum_over(s, waves);
     if (threadIdx.x == 0) a.partials[blockIdx.x] = s;
 }
@@ -160,27 +169,23 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
     const float ratio = a.max_norm / (norm + 1e-6f);
     const float factor = ratio >= 1.f ? 1.f : ratio;        // (a NaN stays one)
-    int64_t from, to;
-    share_of(a.offsets[a.n_tensors], blockIdx.x, gridDim.x, from, to);
-    if (from >= to) return;
-    for (int32_t t = tensor_at(a.offsets, a.n_tensors, from); t < a.n_tensors && a.offsets[t] < to; ++t) {
-        const int64_t base = a.offsets[t], end = a.offsets[t + 1];
-        const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
-        const T *p = static_cast<const T *>(a.grad_ptrs[t]);
-        T *q = static_cast<T *>(a.out_ptrs[t]);
-        if (!p || !q || lo >= hi || (p == q && factor == 1.f)) continue;
-        scale_into(p + (lo - base), q + (lo - base), hi - lo, factor);
-    }
+    const int64_t total = a.offsets[a.n_tensors], piece = piece_of(total);
+    for (int64_t from = blockIdx.x * piece; from < total; from += gridDim.x * piece)
+        for_stretches(a, from, from + piece < total ? from + piece : total, [&](int32_t t, int64_t first, int64_t n) {
+            const T *p = static_cast<const T *>(a.grad_ptrs[t]);
+            T *q = static_cast<T *>(a.out_ptrs[t]);
+            if (p && q && !(p == q && factor == 1.f)) scale_into(p + first, q + first, n, factor);
+        });
 }
 
 int workgroups(int64_t total) {
-    const int64_t shares = (total + kShare - 1) / kShare;
-    return (int)(shares < 1 ? 1 : shares > 2048 ? 2048 : shares);
+    const int64_t pieces = (total + kSmallPiece - 1) / kSmallPiece;
+    return (int)(pieces < 1 ? 1 : pieces > kWorkgroups ? kWorkgroups : pieces);
 }
 
 }  // namespace
 
-static_assert(kGradPartials >= 2048, "the workspace holds a partial sum of each workgroup");
+static_assert(kGradPartials >= kWorkgroups, "the workspace holds a partial sum of each workgroup");
 
 static int squares(GradArgs &a, int64_t total, bool f32, hipStream_t st) {
     a.n_partials = workgroups(total);

@@ -31,16 +31,9 @@ struct QuantArgs {
     int64_t rows, cols, stride, blocks, units;  // blocks a row; units = rows * blocks * 4, one lane each
 };
 
+// Codes of a lane's eight values and the scale of the block that it shares with three neighbours (all four call it).
 template <class T>
-__global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
-    const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (unit >= a.units) return;                // (whole blocks: the four lanes of one go together)
-    const int64_t row = unit / (a.blocks * 4), in_row = unit - row * (a.blocks * 4), col = in_row * 8;
-    const T *p = static_cast<const T *>(a.x) + row * a.stride + col;
-    Raw8<T> raw;
-    zero8(raw);
-    if (col + 8 <= a.cols) load8(p, raw);
-    else if (col < a.cols) load8(p, (int)(a.cols - col), raw);
+__device__ __forceinline__ uint32_t quantised(const Raw8<T> &raw, uint32_t &scale) {
     float f[8];
     widen8(raw, f);
     uint32_t top = 0;
@@ -53,16 +46,28 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
     top = other > top ? other : top;
     other = __shfl_xor(top, 2);
     top = other > top ? other : top;
-    const uint32_t scale = scale_of(top);
+    scale = scale_of(top);
     const float by = scale_value(scale);
     uint32_t codes = 0;
-    if (scale != kNanScale) {
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], by, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], by, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], by, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], by, 3);
-    }
-    reinterpret_cast<uint32_t *>(a.codes)[unit] = codes;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], by, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], by, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], by, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], by, 3);
+    return scale == kNanScale ? 0 : codes;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
+    const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (unit >= a.units) return;                // (whole blocks: the four lanes of one go together)
+    const int64_t row = unit / (a.blocks * 4), in_row = unit - row * (a.blocks * 4), col = in_row * 8;
+    const T *p = static_cast<const T *>(a.x) + row * a.stride + col;
+    Raw8<T> raw;
+    zero8(raw);
+    if (col + 8 <= a.cols) load8(p, raw);
+    else if (col < a.cols) load8(p, (int)(a.cols - col), raw);
+    uint32_t scale;
+    reinterpret_cast<uint32_t *>(a.codes)[unit] = quantised(raw, scale);
     if ((unit & 3) == 0) a.scales[unit >> 2] = (uint8_t)scale;
 }
 
@@ -129,6 +134,11 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) {
 template <class T>
 __device__ __forceinline__ T from_lds(uint32_t at) {
     return *reinterpret_cast<const __attribute__((address_space(3))) T *>(at);
+}
+
+template <class T>
+__device__ __forceinline__ void put_lds(uint32_t at, T v) {
+    *reinterpret_cast<__attribute__((address_space(3))) T *>(at) = v;
 }
 
 // 16 bytes a lane from a resource to LDS, lane after lane from `to` on.  Written in assembly because the compiler, told of a
@@ -328,120 +338,153 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 // ---- products of few rows: the weights go by once ----
 //
 // A workgroup takes NT * 16 rows of the weights and all of the activations (MT * 16 rows at most); its waves divide the
-// columns among them, 256 at a time, and their sums are added up through LDS in their order.  Nothing is shared before
-// that, so the weights go from memory to registers, a lane's two blocks (32 bytes) of a row next to each other, the next
-// ones while the last are multiplied.  With BF16 the wave quantises the activations that it needs by itself: up to 16 rows
-// that costs less than a launch of its own.
-struct Blocks2 {                                // a lane's two blocks of one row
-    u32x4 code[2];
-    uint32_t scale;                             // one byte each
-};
-__device__ __forceinline__ void get_blocks(const uint8_t *codes, const uint8_t *scales, int64_t row, int b, int nb, Blocks2 &r) {
-    typedef uint16_t __attribute__((aligned(1))) u16_any;
-    const u32x4 *p = reinterpret_cast<const u32x4 *>(codes) + row * nb + b;
-    const uint8_t *s = scales + row * nb + b;
-    if (b + 2 <= nb) {
-        r.code[0] = p[0];
-        r.code[1] = p[1];
-        r.scale = *reinterpret_cast<const u16_any *>(s);
-    } else {
-        r.code[0] = b < nb ? p[0] : u32x4{0, 0, 0, 0};
-        r.code[1] = u32x4{0, 0, 0, 0};
-        r.scale = (b < nb ? s[0] : kOneScale) | kOneScale << 8;
-    }
-}
-struct Values2 {                                // the same before quantisation: 64 bf16
-    u32x4 v[8];
-};
-__device__ __forceinline__ void get_values(const bf16_t *row, int64_t col, int64_t cols, Values2 &r) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        Raw8<bf16_t> raw;
-        zero8(raw);
-        if (row && col + 8 * i + 8 <= cols) load8(row + col + 8 * i, raw);
-        else if (row && col + 8 * i < cols) load8(row + col + 8 * i, (int)(cols - col - 8 * i), raw);
-        r.v[i] = raw.v;
-    }
-}
-__device__ __forceinline__ void quantise(const Values2 &x, Blocks2 &r) {
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    r.scale = 0;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        u16x2 top = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x.v[4 * k + i / 4][i % 4] & 0x7FFF7FFFu));
-        const uint32_t scale = scale_of((uint32_t)(top[0] > top[1] ? top[0] : top[1]) << 16);
-        const float by = scale_value(scale);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t pair[4] = {x.v[4 * k + i][0], x.v[4 * k + i][1], x.v[4 * k + i][2], x.v[4 * k + i][3]};
-            uint32_t c = 0;
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[0]), by, 0);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[1]), by, 1);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[2]), by, 2);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[3]), by, 3);
-            r.code[k][i] = scale == kNanScale ? 0 : c;
-        }
-        r.scale |= scale << (8 * k);
-    }
+// columns among them and their sums are added up through LDS in their order.  The weights are read once, so all there is to do is
+// to keep enough of them on the way: each wave has a ring of its own in LDS that loads fill (as above) and that it alone
+// reads, without barriers.  (Loads straight to registers, each lane its row's: 64 lines an instruction where eight lanes of
+// a row next to each other make 8; 6912 x 5120 took 10.1 us that way.)
+// With BF16 the wave quantises the activations that it needs by itself, a chunk of columns ahead of the multiplications.
+typedef uint64_t __attribute__((aligned(2))) u64_any2;
+
+constexpr int kRing = 3;                        // steps of 256 columns on the way
+constexpr int kChunk = 4;                       // steps whose scales (and activations, BF16) are made ready together
+constexpr int kBf16Rows = 4;                    // rows of activations that a product quantises itself
+constexpr int kScaleRow = kChunk * 8 + 16;      // bytes of LDS for a row's scales of a chunk (and a gap: other banks for other rows)
+
+// bytes of LDS that a wave needs
+template <int MT, int NT, bool BF16>
+constexpr size_t few_lds(int64_t m) {
+    return BF16 ? kRing * NT * 2048 + NT * 16 * kScaleRow + (size_t)m * (kChunk * 128 + kScaleRow)
+                : kRing * (NT + MT) * 2048 + (NT + MT) * 16 * kScaleRow;
 }
 
 template <class OT, int MT, int NT, bool BF16>
-__global__ __launch_bounds__(1024) void mx4_few_kernel(Mx4ProductArgs a, int nb) {
-    extern __shared__ f32x4 sums[];             // [wave][tile][lane]
+__global__ __launch_bounds__(512) void mx4_few_kernel(Mx4ProductArgs a, int nb, int steps_each, uint32_t wave_lds) {
+    extern __shared__ __attribute__((aligned(128))) uint8_t lds[];
+    constexpr int kTiles = BF16 ? NT : NT + MT; // tiles of 16 rows in a step of the ring
+    constexpr uint32_t kStep = kTiles * 2048;
     const int lane = threadIdx.x & 63, of16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int64_t n0 = (int64_t)blockIdx.x * (NT * 16);
-    int64_t w_row[NT], x_row[MT];
+    const int64_t n0 = (int64_t)blockIdx.x * (NT * 16), row_bytes = (int64_t)nb * 16;
+    const int steps = (nb + 7) / 8, m = (int)a.m;
+    const uint32_t ring = lds_address(lds) + wave * wave_lds, w_scales = ring + kRing * kStep, x_scales = w_scales + NT * 16 * kScaleRow;
+    const uint32_t x_codes = x_scales + m * kScaleRow;         // BF16 only
+    // rows behind the last give zeros
+    const u32x4 w_res = resource_of(a.w_codes + n0 * row_bytes, (a.n - n0) * row_bytes);
+    const u32x4 x_res = BF16 ? w_res : resource_of(a.a_codes, a.m * row_bytes);
+    const int part = (lane & 7) ^ (lane >> 3);
+    const uint32_t off = (uint32_t)(lane >> 3) * (uint32_t)row_bytes + part * 16;
+    auto ask = [&](int step, int slot) {
+        const bool inside = step * 8 + part < nb;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) w_row[i] = n0 + i * 16 + of16 < a.n ? n0 + i * 16 + of16 : a.n - 1;
-#pragma unroll
-    for (int j = 0; j < MT; ++j) x_row[j] = j * 16 + of16 < a.m ? j * 16 + of16 : a.m - 1;
+        for (int t = 0; t < 2 * kTiles; ++t) {
+            const bool is_w = t < 2 * NT;
+            const uint32_t at = off + (uint32_t)(is_w ? t : t - 2 * NT) * 8 * (uint32_t)row_bytes + step * 128;
+            load_to_lds(ring + slot * kStep + t * 1024, is_w ? w_res : x_res, inside ? at : kOutside);
+        }
+    };
     f32x4 sum[NT][MT];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const bf16_t *values = BF16 && of16 < a.m ? static_cast<const bf16_t *>(a.x) + of16 * a.x_stride : nullptr;
-    Blocks2 w[2][NT], x[2][MT];
-    Values2 xv[2];
-    auto get = [&](int step, int buf) {
-        const int b = step * 8 + quarter * 2;
+
+    const int from = wave * steps_each, to = from + steps_each < steps ? from + steps_each : steps;
+    for (int chunk = from; chunk < to; chunk += kChunk) {
+        const int end = chunk + kChunk < to ? chunk + kChunk : to;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) get_blocks(a.w_codes, a.w_scales, w_row[i], b, nb, w[buf][i]);
-        if constexpr (BF16) get_values(values, (int64_t)b * ROSE_MX4_BLOCK, a.k, xv[buf]);
-        else
+        for (int i = 0; i < kRing; ++i)
+            if (chunk + i < end) ask(chunk + i, i);
+        // scales: two lanes a row, sixteen blocks each
+        const int s_row = lane >> 1, s_from = chunk * 8 + (lane & 1) * 16;
 #pragma unroll
-            for (int j = 0; j < MT; ++j) get_blocks(a.a_codes, a.a_scales, x_row[j], b, nb, x[buf][j]);
-    };
-    auto multiply = [&](int buf) {
-        if constexpr (BF16) quantise(xv[buf], x[buf][0]);
+        for (int t = 0; t < NT * 16; t += 32) {
+            const int64_t row = n0 + t + s_row < a.n ? n0 + t + s_row : a.n - 1;
+            if (t + s_row < NT * 16) put_lds(w_scales + (t + s_row) * kScaleRow + (lane & 1) * 16, turned(scales_at(a.w_scales + row * nb, s_from, nb)));
+        }
+        if constexpr (!BF16) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                sum[i][j] = product<0>(w[buf][i].code[0], w[buf][i].scale, x[buf][j].code[0], x[buf][j].scale, sum[i][j]);
-                sum[i][j] = product<1>(w[buf][i].code[1], w[buf][i].scale, x[buf][j].code[1], x[buf][j].scale, sum[i][j]);
+            for (int t = 0; t < MT * 16; t += 32) {
+                const int64_t row = t + s_row < a.m ? t + s_row : a.m - 1;
+                if (t + s_row < MT * 16) put_lds(x_scales + (t + s_row) * kScaleRow + (lane & 1) * 16, turned(scales_at(a.a_scales + row * nb, s_from, nb)));
             }
-    };
-    const int steps = (nb + 7) / 8;
-    int step = wave;
-    if (step < steps) get(step, 0);
-    while (step < steps) {
-        if (step + waves < steps) get(step + waves, 1);
-        multiply(0);
-        step += waves;
-        if (step >= steps) break;
-        if (step + waves < steps) get(step + waves, 0);
-        multiply(1);
-        step += waves;
+        } else {
+            // eight values a lane, four lanes a block, two steps a wave at a time; a few rows asked for together
+            for (int r0 = 0; r0 < m; r0 += kBf16Rows) {
+                Raw8<bf16_t> raw[kBf16Rows][kChunk / 2];
+#pragma unroll
+                for (int r = 0; r < kBf16Rows; ++r)
+#pragma unroll
+                    for (int h = 0; h < kChunk / 2; ++h) {
+                        const int64_t col = (int64_t)chunk * 256 + h * 512 + lane * 8;
+                        const bf16_t *p = static_cast<const bf16_t *>(a.x) + (int64_t)(r0 + r) * a.x_stride + col;
+                        zero8(raw[r][h]);
+                        if (r0 + r < m) {
+                            if (col + 8 <= a.k) load8(p, raw[r][h]);
+                            else if (col < a.k) load8(p, (int)(a.k - col), raw[r][h]);
+                        }
+                    }
+#pragma unroll
+                for (int r = 0; r < kBf16Rows; ++r) {
+                    if (r0 + r >= m) break;
+#pragma unroll
+                    for (int h = 0; h < kChunk / 2; ++h) {
+                        uint32_t scale;
+                        const uint32_t code = quantised(raw[r][h], scale);
+                        const int unit = h * 64 + lane, block = unit >> 2, step = block >> 3, in_step = block & 7;
+                        put_lds(x_codes + (r0 + r) * (kChunk * 128) + step * 128 + ((in_step ^ ((r0 + r) & 7)) * 16) + (unit & 3) * 4, code);
+                        if ((unit & 3) == 0)
+                            put_lds(x_scales + (r0 + r) * kScaleRow + (step >> 1) * 16 + (in_step & 3) * 4 + (step & 1) * 2 + (in_step >> 2), (uint8_t)scale);
+                    }
+                }
+            }
+        }
+        asm volatile("" ::: "memory");
+        const int x_row = of16 < m ? of16 : m - 1;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            if (chunk + i >= end) break;
+            // (of the loads that came since, those of kRing - 1 steps may be away; near the end there are fewer)
+            if (i > 0) {
+                if (chunk + i + kRing - 1 < end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRing - 1) * 2 * kTiles) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const uint32_t slot = ring + (i % kRing) * kStep;
+            uint32_t ws[NT], xs[MT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) ws[t] = from_lds<uint32_t>(w_scales + (t * 16 + of16) * kScaleRow + (i >> 1) * 16 + quarter * 4);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                xs[t] = from_lds<uint32_t>(x_scales + (BF16 ? x_row : t * 16 + of16) * kScaleRow + (i >> 1) * 16 + quarter * 4);
+            u32x4 w[2][NT], x[2][MT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) w[h][t] = from_lds<u32x4>(slot + t * 2048 + of16 * 128 + ((h * 4 + quarter) ^ (of16 & 7)) * 16);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    x[h][t] = BF16 ? from_lds<u32x4>(x_codes + x_row * (kChunk * 128) + i * 128 + ((h * 4 + quarter) ^ (x_row & 7)) * 16)
+                                   : from_lds<u32x4>(slot + (NT + t) * 2048 + of16 * 128 + ((h * 4 + quarter) ^ (of16 & 7)) * 16);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    if (i & 1) {
+                        sum[t][j] = product<2>(w[0][t], ws[t], x[0][j], xs[j], sum[t][j]);
+                        sum[t][j] = product<3>(w[1][t], ws[t], x[1][j], xs[j], sum[t][j]);
+                    } else {
+                        sum[t][j] = product<0>(w[0][t], ws[t], x[0][j], xs[j], sum[t][j]);
+                        sum[t][j] = product<1>(w[1][t], ws[t], x[1][j], xs[j], sum[t][j]);
+                    }
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the slot has been read)
+            if (chunk + i + kRing < end) ask(chunk + i + kRing, i % kRing);
+        }
     }
     if (waves > 1) {
+        // (each wave's sums where its ring was: nothing of it is on the way any more)
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int j = 0; j < MT; ++j) sums[(wave * (NT * MT) + i * MT + j) * 64 + lane] = sum[i][j];
+        for (int t = 0; t < NT * MT; ++t) put_lds(ring + (t * 64 + lane) * 16, sum[t / MT][t % MT]);
         __syncthreads();
     }
     // tiles in turn to the waves: four neighbouring outputs a lane
@@ -450,19 +493,19 @@ __global__ __launch_bounds__(1024) void mx4_few_kernel(Mx4ProductArgs a, int nb)
         if (t % waves != wave) continue;
         f32x4 s = sum[t / MT][t % MT];
         if (waves > 1) {
-            s = sums[t * 64 + lane];
-            for (int v = 1; v < waves; ++v) s += sums[(v * (NT * MT) + t) * 64 + lane];
+            const uint32_t at = lds_address(lds) + (t * 64 + lane) * 16;
+            s = from_lds<f32x4>(at);
+            for (int v = 1; v < waves; ++v) s += from_lds<f32x4>(at + v * wave_lds);
         }
         const int64_t row = (t % MT) * 16 + of16, col = n0 + (t / MT) * 16 + quarter * 4;
         if (row >= a.m) continue;
         OT *q = static_cast<OT *>(a.out) + row * a.out_stride + col;
-        typedef uint64_t __attribute__((aligned(2))) u64_any;
         if (col + 4 > a.n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (col + e < a.n) q[e] = from_f32<OT>(s[e]);
         } else if constexpr (sizeof(OT) == 4) *reinterpret_cast<f32x4_any *>(q) = s;
-        else *reinterpret_cast<u64_any *>(q) = (uint64_t)pack_bf16(s[2], s[3]) << 32 | pack_bf16(s[0], s[1]);
+        else *reinterpret_cast<u64_any2 *>(q) = (uint64_t)pack_bf16(s[2], s[3]) << 32 | pack_bf16(s[0], s[1]);
     }
 }
 
@@ -494,18 +537,22 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
     return (int)hipGetLastError();
 }
 
-bool mx4_product_takes_bf16(int64_t m) { return m <= 16; }
+bool mx4_product_takes_bf16(int64_t m) { return m <= kBf16Rows; }
 
 template <int MT, int NT, bool BF16>
 static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     const int64_t groups = (a.n + NT * 16 - 1) / (NT * 16), steps = (blocks_of(a.k) + 7) / 8;
-    // waves a workgroup: about sixteen for every CU together, two steps each at least
-    int waves = 1;
-    while (waves < 16 && groups * waves < 4096 && waves * 4 <= steps) waves *= 2;
-    const dim3 grid((unsigned)groups), block(64 * waves);
-    const size_t lds = waves > 1 ? (size_t)waves * NT * MT * 1024 : 0;
-    if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, lds, st, a, (int)blocks_of(a.k));
-    else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, lds, st, a, (int)blocks_of(a.k));
+    const size_t wave_lds = (few_lds<MT, NT, BF16>(a.m) + 127) / 128 * 128;
+    // as many waves as make about eight for every CU together, with as many steps each as another, and their rings in 72 KB
+    int64_t waves = (2048 + groups - 1) / groups;
+    const int64_t fit = (int64_t)((72 << 10) / wave_lds);
+    waves = waves > 8 ? 8 : waves;
+    waves = waves > fit ? fit : waves;
+    const int64_t each = steps > waves ? (steps + waves - 1) / waves : 1;
+    waves = steps > 0 ? (steps + each - 1) / each : 1;
+    const dim3 grid((unsigned)groups), block((unsigned)(64 * waves));
+    if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
+    else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
     return (int)hipGetLastError();
 }
 
@@ -522,9 +569,12 @@ static int launch_tiles(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.m == 0 || a.n == 0) return 0;
+    // (every workgroup reads all activations: with many of them and of their rows 32 rows of the weights share a reading;
+    // 64 x 19008 x 5120: 17.8 us against 32.5, 47 x 4099 x 4096: 10.2 against 6.8)
+    const bool wide = a.n >= 8192;
     if (a.m <= 16) return a.x ? launch_few<1, 1, true>(a, out_f32, st) : launch_few<1, 1, false>(a, out_f32, st);
-    if (a.m <= 32) return launch_few<2, 1, false>(a, out_f32, st);
-    if (a.m <= 64) return launch_few<4, 1, false>(a, out_f32, st);
+    if (a.m <= 32) return wide ? launch_few<2, 2, false>(a, out_f32, st) : launch_few<2, 1, false>(a, out_f32, st);
+    if (a.m <= 64) return wide ? launch_few<4, 2, false>(a, out_f32, st) : launch_few<4, 1, false>(a, out_f32, st);
     // 256 x 256 tiles move half of what 128 x 128 ones do but fill a CU each; the smaller ones, two a CU, where there are few
     // (256 x 19008 x 5120: 38.5 us with the large ones, 28.8 with the small; 4096 x 4096 x 4096: 39.8 and 48.7).
     const int64_t large = ((a.n + 255) / 256) * ((a.m + 255) / 256);

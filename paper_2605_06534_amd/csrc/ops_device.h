@@ -101,4 +101,28 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&f)[8]) {
         if (i < n) p[i] = from_f32<T>(f[i]);
 }
 
+// Eight columns a lane of rows that need not be multiples of eight: the last lane's vector is moved back to end with the
+// row, so that every load and store is a whole vector without a branch around it.  What that lane shares with the one before it
+// both form from the same values in the same order and write alike; a kernel that reads what it writes keeps the two in
+// one wave.  Rows of fewer than eight columns (NARROW) go element by element.
+template <bool NARROW>
+struct Columns {
+    int64_t at;                                 // first column of the vector
+    int n;                                      // elements of it; 0: this lane has none
+    __device__ __forceinline__ Columns(int64_t col, int64_t cols) {
+        at = NARROW ? 0 : col + 8 <= cols ? col : cols - 8;
+        n = col >= cols ? 0 : NARROW ? (int)cols : 8;
+    }
+    template <class T>
+    __device__ __forceinline__ void load(const T *row, Raw8<T> &r) const {
+        if (NARROW) load8(row + at, n, r);
+        else load8(row + at, r);
+    }
+    template <class T>
+    __device__ __forceinline__ void store(T *row, const float (&f)[8]) const {
+        if (NARROW) store8(row + at, n, f);
+        else if (n) store8(row + at, f);
+    }
+};
+
 }  // namespace rose
