@@ -8,12 +8,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWorkgroups = 2048;                // at most: eight a CU
-constexpr int64_t kSmallPiece = 8192, kLargePiece = 32768;
-
 // All tensors laid end to end are cut into pieces, which the workgroups take in turn.
-__device__ __forceinline__ int64_t piece_of(int64_t total) {
-    return total <= kWorkgroups * kSmallPiece ? kSmallPiece : kLargePiece;
-}
+constexpr int64_t kSmallPiece = 8192, kLargePiece = 32768;
+int64_t piece_of(int64_t total) { return total <= kWorkgroups * kSmallPiece ? kSmallPiece : kLargePiece; }
 
 // The tensor that holds position `at`: the last one that begins at or before it, 64 candidates at a time.
 __device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, int64_t at) {
@@ -28,14 +25,20 @@ __device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, 
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Calls f(tensor, first element, number) for the stretch of every tensor that lies in [from, to).
+// Calls f(tensor, first element, number) for every stretch of a tensor in this workgroup's pieces.
 template <class F>
-__device__ __forceinline__ void for_stretches(const GradArgs &a, int64_t from, int64_t to, F f) {
-    for (int32_t t = tensor_at(a.offsets, a.n_tensors, from); t < a.n_tensors; ++t) {
-        const int64_t base = a.offsets[t], end = a.offsets[t + 1];
-        if (base >= to) return;
-        const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
-        if (lo < hi) f(t, lo - base, hi - lo);
+__device__ __forceinline__ void for_stretches(const GradArgs &a, F f) {
+    for (int64_t from = blockIdx.x * a.piece;; from += gridDim.x * a.piece) {
+        // (the tensor is looked for before the end is known: one trip to memory less in front of the first element)
+        int32_t t = tensor_at(a.offsets, a.n_tensors, from);
+        const int64_t total = a.offsets[a.n_tensors], to = from + a.piece < total ? from + a.piece : total;
+        if (from >= total) return;
+        for (; t < a.n_tensors; ++t) {
+            const int64_t base = a.offsets[t], end = a.offsets[t + 1];
+            if (base >= to) break;
+            const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
+            if (lo < hi) f(t, lo - base, hi - lo);
+        }
     }
 }
 
@@ -71,14 +74,6 @@ __device__ __forceinline__ double squares_of(const T *p, int64_t n) {
     constexpr int kAhead = 4;
     double s = 0;
     const int64_t head = head_of(p, n), vectors = (n - head) / 8, tail = head + vectors * 8;
-    if (threadIdx.x < head) {
-        const double f = to_f32(p[threadIdx.x]);
-        s = fma(f, f, s);
-    }
-    if (threadIdx.x < n - tail) {
-        const double f = to_f32(p[tail + threadIdx.x]);
-        s = fma(f, f, s);
-    }
     const T *body = p + head;
     int64_t i = threadIdx.x;
     for (; i + (kAhead - 1) * kThreads < vectors; i += kAhead * kThreads) {
@@ -99,19 +94,26 @@ __device__ __forceinline__ double squares_of(const T *p, int64_t n) {
         widen8(raw, f);
         s += squares(f);
     }
+    // (what is in front of the first vector and behind the last)
+    if (threadIdx.x < head) {
+        const double f = to_f32(p[threadIdx.x]);
+        s = fma(f, f, s);
+    }
+    if (threadIdx.x < n - tail) {
+        const double f = to_f32(p[tail + threadIdx.x]);
+        s = fma(f, f, s);
+    }
     return s;
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradArgs a) {
     __shared__ double waves[kThreads / 64];
-    const int64_t total = a.offsets[a.n_tensors], piece = piece_of(total);
     double s = 0;
-    for (int64_t from = blockIdx.x * piece; from < total; from += gridDim.x * piece)
-        for_stretches(a, from, from + piece < total ? from + piece : total, [&](int32_t t, int64_t first, int64_t n) {
-            const T *p = static_cast<const T *>(a.grad_ptrs[t]);
-            if (p) s += squares_of(p + first, n);
-        });
+    for_stretches(a, [&](int32_t t, int64_t first, int64_t n) {
+        const T *p = static_cast<const T *>(a.grad_ptrs[t]);
+        if (p) s += squares_of(p + first, n);
+    });
     s = sum_over(s, waves);
     if (threadIdx.x == 0) a.partials[blockIdx.x] = s;
 }
@@ -129,53 +131,77 @@ __global__ __launch_bounds__(kThreads) void grad_sum_kernel(GradArgs a) {
     if (threadIdx.x == 0) *a.sum = s;
 }
 
+// The first kAhead vectors of a stretch that this thread scales, asked for before the factor is known.
+constexpr int kAhead = 4;
 template <class T>
-__device__ __forceinline__ void scale_into(const T *p, T *q, int64_t n, float factor) {
-    constexpr int kAhead = 4;
+struct Begun {
+    Raw8<T> raw[kAhead];
+};
+template <class T>
+__device__ __forceinline__ void begin(const T *p, const T *q, int64_t n, Begun<T> &b) {
+    const int64_t head = head_of(q, n), vectors = (n - head) / 8;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int64_t i = threadIdx.x + u * kThreads;
+        if (i < vectors) load8(p + head + i * 8, b.raw[u]);
+    }
+}
+template <class T>
+__device__ __forceinline__ void scale_into(const T *p, T *q, int64_t n, float factor, const Begun<T> &begun) {
     const int64_t head = head_of(q, n), vectors = (n - head) / 8, tail = head + vectors * 8;
-    if (threadIdx.x < head) q[threadIdx.x] = from_f32<T>(to_f32(p[threadIdx.x]) * factor);
-    if (threadIdx.x < n - tail) q[tail + threadIdx.x] = from_f32<T>(to_f32(p[tail + threadIdx.x]) * factor);
+    const T *from = p;
+    T *to = q;
     p += head;
     q += head;
-    int64_t i = threadIdx.x;
+    auto put = [&](int64_t i, const Raw8<T> &raw) {
+        float f[8];
+        widen8(raw, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= factor;
+        store8(q + i * 8, f);
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (threadIdx.x + u * kThreads < vectors) put(threadIdx.x + u * kThreads, begun.raw[u]);
+    int64_t i = threadIdx.x + kAhead * kThreads;
     for (; i + (kAhead - 1) * kThreads < vectors; i += kAhead * kThreads) {
         Raw8<T> raw[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) load8(p + (i + u * kThreads) * 8, raw[u]);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            float f[8];
-            widen8(raw[u], f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] *= factor;
-            store8(q + (i + u * kThreads) * 8, f);
-        }
+        for (int u = 0; u < kAhead; ++u) put(i + u * kThreads, raw[u]);
     }
     for (; i < vectors; i += kThreads) {
         Raw8<T> raw;
-        float f[8];
         load8(p + i * 8, raw);
-        widen8(raw, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= factor;
-        store8(q + i * 8, f);
+        put(i, raw);
     }
+    if (threadIdx.x < head) to[threadIdx.x] = from_f32<T>(to_f32(from[threadIdx.x]) * factor);
+    if (threadIdx.x < n - tail) to[tail + threadIdx.x] = from_f32<T>(to_f32(from[tail + threadIdx.x]) * factor);
 }
 
 template <class T, bool FROM_PARTIALS>
 __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
     __shared__ double waves[kThreads / 64];
-    const float norm = (float)sqrt(FROM_PARTIALS ? sum_partials(a, waves) : *a.sum);
-    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
-    const float ratio = a.max_norm / (norm + 1e-6f);
-    const float factor = ratio >= 1.f ? 1.f : ratio;        // (a NaN stays one)
-    const int64_t total = a.offsets[a.n_tensors], piece = piece_of(total);
-    for (int64_t from = blockIdx.x * piece; from < total; from += gridDim.x * piece)
-        for_stretches(a, from, from + piece < total ? from + piece : total, [&](int32_t t, int64_t first, int64_t n) {
-            const T *p = static_cast<const T *>(a.grad_ptrs[t]);
-            T *q = static_cast<T *>(a.out_ptrs[t]);
-            if (p && q && !(p == q && factor == 1.f)) scale_into(p + first, q + first, n, factor);
-        });
+    float factor = 0.f;
+    bool known = false;
+    auto find_factor = [&] {
+        const float norm = (float)sqrt(FROM_PARTIALS ? sum_partials(a, waves) : *a.sum);
+        if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
+        const float ratio = a.max_norm / (norm + 1e-6f);
+        factor = ratio >= 1.f ? 1.f : ratio;                // (a NaN stays one)
+        known = true;
+    };
+    for_stretches(a, [&](int32_t t, int64_t first, int64_t n) {
+        const T *p = static_cast<const T *>(a.grad_ptrs[t]);
+        T *q = static_cast<T *>(a.out_ptrs[t]);
+        const bool any = p && q;
+        Begun<T> begun;
+        if (any) begin(p + first, q + first, n, begun);
+        if (!known) find_factor();
+        if (any && !(p == q && factor == 1.f)) scale_into(p + first, q + first, n, factor, begun);
+    });
+    if (!known) find_factor();
 }
 
 int workgroups(int64_t total) {
@@ -188,6 +214,7 @@ int workgroups(int64_t total) {
 static_assert(kGradPartials >= kWorkgroups, "the workspace holds a partial sum of each workgroup");
 
 static int squares(GradArgs &a, int64_t total, bool f32, hipStream_t st) {
+    a.piece = piece_of(total);
     a.n_partials = workgroups(total);
     if (f32) hipLaunchKernelGGL(grad_squares_kernel<float>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL(grad_squares_kernel<bf16_t>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
@@ -202,7 +229,9 @@ int launch_grad_sum_squares(const GradArgs &args, int64_t total, bool f32, void 
     return (int)hipGetLastError();
 }
 
-int launch_grad_clip(const GradArgs &a, int64_t total, bool f32, void *stream) {
+int launch_grad_clip(const GradArgs &args, int64_t total, bool f32, void *stream) {
+    GradArgs a = args;
+    a.piece = piece_of(total);
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid(workgroups(total)), block(kThreads);
     if (f32) hipLaunchKernelGGL((grad_clip_kernel<float, false>), grid, block, 0, st, a);

@@ -22,74 +22,162 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
 __device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_float(scale ? scale << 23 : 0x00400000u); }
 
 // -------------------------------------------------------------------------------------------------
-// quantisation: four lanes a block, eight elements each
+// quantisation: four lanes a block, eight elements each, kUnits times eight a lane
 // -------------------------------------------------------------------------------------------------
+constexpr int kUnits = 4;
+
 struct QuantArgs {
-    const void *x;                              // or the output of the inverse
+    const void *x;                              // the matrix, of which ...
+    void *out;                                  // ... or into which
     const uint8_t *codes_in, *scales_in;
     uint8_t *codes, *scales;
-    int64_t rows, cols, stride, blocks, units;  // blocks a row; units = rows * blocks * 4, one lane each
+    int64_t rows, cols, stride, units;          // units: eights of all rows, filled up to whole blocks
+    uint32_t row_units, by_row_units;           // of a row; 2^32 over that, rounded up
 };
 
+// Row and column of this lane's u-th eight.  A workgroup's kThreads * kUnits of them begin in one row; where rows are shorter the
+// quotient of two numbers below 2048 comes from a product with the reciprocal (exact: off by less than 2048 / 2^32).
+struct Place {
+    int64_t row;
+    uint32_t in_row;
+    bool inside;
+};
+__device__ __forceinline__ Place place_of(const QuantArgs &a, int u) {
+    const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnits), row0 = first / a.row_units;
+    const int64_t unit = first + u * kThreads + threadIdx.x;
+    const uint32_t from_row0 = (uint32_t)(unit - row0 * a.row_units);
+    const uint32_t rows = a.row_units >= kThreads * kUnits ? (from_row0 >= a.row_units ? 1u : 0u) : __umulhi(from_row0, a.by_row_units);
+    return Place{row0 + rows, from_row0 - rows * a.row_units, unit < a.units};
+}
+
+// the elements from the k-th on, zeros behind them
+__device__ __forceinline__ void drop(Raw8<bf16_t> &r, int k) {
+    const u32x4 zeros = {0, 0, 0, 0};
+    if (k >= 8) r.v = zeros;
+    if (k & 4) r.v = u32x4{r.v[2], r.v[3], 0, 0};
+    if (k & 2) r.v = u32x4{r.v[1], r.v[2], r.v[3], 0};
+    if (k & 1) r.v = u32x4{r.v[0] >> 16 | r.v[1] << 16, r.v[1] >> 16 | r.v[2] << 16, r.v[2] >> 16 | r.v[3] << 16, r.v[3] >> 16};
+}
+__device__ __forceinline__ void drop(Raw8<float> &r, int k) {
+    const f32x4 zeros = {0.f, 0.f, 0.f, 0.f};
+    if (k >= 8) r.lo = r.hi = zeros;
+    if (k & 4) {
+        r.lo = r.hi;
+        r.hi = zeros;
+    }
+    if (k & 2) {
+        r.lo = f32x4{r.lo[2], r.lo[3], r.hi[0], r.hi[1]};
+        r.hi = f32x4{r.hi[2], r.hi[3], 0.f, 0.f};
+    }
+    if (k & 1) {
+        r.lo = f32x4{r.lo[1], r.lo[2], r.lo[3], r.hi[0]};
+        r.hi = f32x4{r.hi[1], r.hi[2], r.hi[3], 0.f};
+    }
+}
+
+// Largest magnitude of eight elements, as an fp32 pattern
+__device__ __forceinline__ uint32_t largest(const Raw8<bf16_t> &r) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)(r.v[i] & 0x7FFF7FFFu)));
+    return (uint32_t)(top[0] > top[1] ? top[0] : top[1]) << 16;
+}
+__device__ __forceinline__ uint32_t largest(const Raw8<float> &r) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = __float_as_uint(r.lo[i]) & 0x7FFFFFFFu, hi = __float_as_uint(r.hi[i]) & 0x7FFFFFFFu;
+        top = lo > top ? lo : top;
+        top = hi > top ? hi : top;
+    }
+    return top;
+}
+// Their codes: the conversions divide by the scale and round to the nearest, ties to even, at most 6.
+__device__ __forceinline__ uint32_t codes_of(const Raw8<bf16_t> &r, float by) {
+    const uint32_t pair[4] = {r.v[0], r.v[1], r.v[2], r.v[3]};
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[0]), by, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[1]), by, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[2]), by, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[3]), by, 3);
+}
+__device__ __forceinline__ uint32_t codes_of(const Raw8<float> &r, float by) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.lo[0], r.lo[1], by, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.lo[2], r.lo[3], by, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.hi[0], r.hi[1], by, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.hi[2], r.hi[3], by, 3);
+}
 // Codes of a lane's eight values and the scale of the block that it shares with three neighbours (all four call it).
 template <class T>
 __device__ __forceinline__ uint32_t quantised(const Raw8<T> &raw, uint32_t &scale) {
-    float f[8];
-    widen8(raw, f);
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t m = __float_as_uint(f[e]) & 0x7FFFFFFFu;
-        top = m > top ? m : top;
-    }
-    uint32_t other = __shfl_xor(top, 1);
+    uint32_t top = largest(raw), other = __builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true);      // lane ^ 1
     top = other > top ? other : top;
-    other = __shfl_xor(top, 2);
+    other = __builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true);                                   // lane ^ 2
     top = other > top ? other : top;
     scale = scale_of(top);
-    const float by = scale_value(scale);
-    uint32_t codes = 0;
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], by, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], by, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], by, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], by, 3);
+    const uint32_t codes = codes_of(raw, scale_value(scale));
     return scale == kNanScale ? 0 : codes;
 }
 
-template <class T>
+template <class T, bool NARROW>
 __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
-    const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (unit >= a.units) return;                // (whole blocks: the four lanes of one go together)
-    const int64_t row = unit / (a.blocks * 4), in_row = unit - row * (a.blocks * 4), col = in_row * 8;
-    const T *p = static_cast<const T *>(a.x) + row * a.stride + col;
-    Raw8<T> raw;
-    zero8(raw);
-    if (col + 8 <= a.cols) load8(p, raw);
-    else if (col < a.cols) load8(p, (int)(a.cols - col), raw);
-    uint32_t scale;
-    reinterpret_cast<uint32_t *>(a.codes)[unit] = quantised(raw, scale);
-    if ((unit & 3) == 0) a.scales[unit >> 2] = (uint8_t)scale;
+    Raw8<T> raw[kUnits];
+    int behind[kUnits];                         // rows that end inside an eight: the last whole one, moved
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const Place p = place_of(a, u);
+        const int64_t col = (int64_t)p.in_row * 8, at = col + 8 <= a.cols ? col : a.cols - 8;
+        const T *row = static_cast<const T *>(a.x) + (p.inside ? p.row : 0) * a.stride;
+        behind[u] = 0;
+        if (NARROW) load8(row, p.in_row == 0 ? (int)a.cols : 0, raw[u]);
+        else {
+            load8(row + at, raw[u]);
+            behind[u] = (int)(col - at < 8 ? col - at : 8);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int64_t unit = ((int64_t)blockIdx.x * kUnits + u) * kThreads + threadIdx.x;
+        if (behind[u]) drop(raw[u], behind[u]);
+        uint32_t scale;
+        const uint32_t codes = quantised(raw[u], scale);
+        if (unit >= a.units) return;            // (whole blocks: the four lanes of one go together)
+        reinterpret_cast<uint32_t *>(a.codes)[unit] = codes;
+        if ((unit & 3) == 0) a.scales[unit >> 2] = (uint8_t)scale;
+    }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void mx4_dequantize_kernel(QuantArgs a, T *out) {
-    const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (unit >= a.units) return;
-    const int64_t row = unit / (a.blocks * 4), in_row = unit - row * (a.blocks * 4), col = in_row * 8;
-    if (col >= a.cols) return;
-    const uint32_t codes = reinterpret_cast<const uint32_t *>(a.codes_in)[unit], scale = a.scales_in[unit >> 2];
-    const float by = scale == kNanScale ? __uint_as_float(0x7FC00000u) : scale_value(scale);
-    float f[8];
+// two values of a byte of codes
+__device__ __forceinline__ void expand(uint32_t codes, float by, bool nan, float (&f)[8]) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 1);
+    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 3);
+    const float v[8] = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t c = codes >> (4 * e), i = c & 7;
-        // magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6
-        const float m = i < 2 ? 0.5f * i : __uint_as_float((126 + (i >> 1)) << 23 | (i & 1) << 22);
-        f[e] = (c & 8 ? -m : m) * by;
+    for (int e = 0; e < 8; ++e) f[e] = nan ? __uint_as_float(0x7FC00000u) : v[e];
+}
+
+template <class T, bool NARROW>
+__global__ __launch_bounds__(kThreads) void mx4_dequantize_kernel(QuantArgs a) {
+    uint32_t codes[kUnits], scale[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int64_t unit = ((int64_t)blockIdx.x * kUnits + u) * kThreads + threadIdx.x, at = unit < a.units ? unit : 0;
+        codes[u] = reinterpret_cast<const uint32_t *>(a.codes_in)[at];
+        scale[u] = a.scales_in[at >> 2];
     }
-    T *q = out + row * a.stride + col;
-    if (col + 8 <= a.cols) store8(q, f);
-    else store8(q, (int)(a.cols - col), f);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const Place p = place_of(a, u);
+        const int64_t col = (int64_t)p.in_row * 8;
+        if (!p.inside || col >= a.cols) continue;
+        float f[8];
+        expand(codes[u], scale_value(scale[u]), scale[u] == kNanScale, f);
+        T *q = static_cast<T *>(a.out) + p.row * a.stride + col;
+        if (!NARROW && col + 8 <= a.cols) store8(q, f);
+        else store8(q, (int)(a.cols - col), f);
+    }
 }
 
 // -------------------------------------------------------------------------------------------------
@@ -175,14 +263,17 @@ __device__ __forceinline__ u32x4 scales_at(const uint8_t *row, int from, int nb)
     }
     return u32x4{(uint32_t)part[0], (uint32_t)(part[0] >> 32), (uint32_t)part[1], (uint32_t)(part[1] >> 32)};
 }
-// The same without a branch, for rows of 16 blocks at least: the last sixteen, shifted.  (A branch in the main loop makes
-// the compiler move all sums between register files on either side of it.)  Of shorter rows nothing is left: `row` is then
-// any address with 16 bytes behind it.
-__device__ __forceinline__ u32x4 scales_at_no_branch(const uint8_t *row, int from, int nb) {
+// The same in two steps, load and cut, without a branch, for rows of 16 blocks at least: the last sixteen, shifted.  (A branch
+// in the main loop makes the compiler move all sums between register files on either side of it, and a value that is worked on
+// where it is loaded makes it wait there for all loads.)  Of shorter rows nothing is left: `row` is then any address with 16
+// bytes behind it.
+__device__ __forceinline__ u32x4 load_scales(const uint8_t *row, int from, int nb) {
+    return *reinterpret_cast<const u32x4_any *>(row + (nb < 16 ? 0 : from + 16 <= nb ? from : nb - 16));
+}
+__device__ __forceinline__ u32x4 cut_scales(u32x4 v, int from, int nb) {
     constexpr uint64_t kOnes = 0x7F7F7F7F7F7F7F7Full;
     static_assert(kOneScale == 0x7F, "");
-    const int at = nb < 16 ? 0 : from + 16 <= nb ? from : nb - 16, cut = (from - at) * 8, bits = cut & 63;
-    const u32x4 v = *reinterpret_cast<const u32x4_any *>(row + at);
+    const int cut = from + 16 <= nb ? 0 : (from + 16 - nb) * 8, bits = cut & 63;       // what is in front of `from` goes
     const uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
     const uint64_t lo_cut = bits ? lo >> bits | hi << (64 - bits) : lo, hi_cut = bits ? hi >> bits | kOnes << (64 - bits) : hi;
     const uint64_t low = from >= nb ? kOnes : cut >= 64 ? hi_cut : lo_cut, high = from >= nb || cut >= 64 ? kOnes : hi_cut;
@@ -259,9 +350,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 #pragma unroll
         for (int j = 0; j < FM; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    more_scales = scales_at(my_scales, 16, nb);
     scales[0][tid] = turned(scales_at(my_scales, 0, nb));
-    scales[1][tid] = turned(more_scales);
+    more_scales = load_scales(later_scales, 16, nb);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) ask(0, 0, j);
 #pragma unroll
@@ -290,7 +380,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
         }
         wait_and_meet<0>();
         const int pair = d >> 1;                        // scales come for pairs of slots
-        if (P == 0) scales[(pair + 1) & 1][tid] = turned(more_scales);
+        if (P == 0) scales[(pair + 1) & 1][tid] = turned(cut_scales(more_scales, (pair + 1) * 16, nb));
         get_w(P ^ 1, 0, w[0]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -303,7 +393,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
             __builtin_amdgcn_sched_barrier(0);
         }
         if (P == 1) {
-            more_scales = scales_at_no_branch(later_scales, (pair + 2) * 16, nb);
+            more_scales = load_scales(later_scales, (pair + 2) * 16, nb);
             get_scales((pair + 1) & 1);
         }
         ++d;
@@ -513,28 +603,32 @@ int64_t blocks_of(int64_t cols) { return (cols + ROSE_MX4_BLOCK - 1) / ROSE_MX4_
 
 }  // namespace
 
+template <class Kernel>
+static int launch_quant(QuantArgs a, Kernel kernel, hipStream_t st) {
+    const int64_t row_units = blocks_of(a.cols) * 4, grid = (a.rows * row_units + kThreads * kUnits - 1) / (kThreads * kUnits);
+    if (grid == 0) return 0;
+    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    a.units = a.rows * row_units;
+    a.row_units = (uint32_t)row_units;
+    a.by_row_units = (uint32_t)(((1ull << 32) + row_units - 1) / row_units);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+    return (int)hipGetLastError();
+}
+
 int launch_mx4_quantize(const void *x, bool f32, int64_t rows, int64_t cols, int64_t stride, uint8_t *codes, uint8_t *scales,
                         void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    QuantArgs a = {x, nullptr, nullptr, codes, scales, rows, cols, stride, blocks_of(cols), rows * blocks_of(cols) * 4};
-    if (a.units == 0) return 0;
-    const int64_t grid = (a.units + kThreads - 1) / kThreads;
-    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    if (f32) hipLaunchKernelGGL(mx4_quantize_kernel<float>, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL(mx4_quantize_kernel<bf16_t>, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
-    return (int)hipGetLastError();
+    const QuantArgs a = {x, nullptr, nullptr, nullptr, codes, scales, rows, cols, stride, 0, 0, 0};
+    if (cols < 8) return f32 ? launch_quant(a, mx4_quantize_kernel<float, true>, st) : launch_quant(a, mx4_quantize_kernel<bf16_t, true>, st);
+    return f32 ? launch_quant(a, mx4_quantize_kernel<float, false>, st) : launch_quant(a, mx4_quantize_kernel<bf16_t, false>, st);
 }
 
 int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out, bool f32,
                           int64_t stride, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    QuantArgs a = {nullptr, codes, scales, nullptr, nullptr, rows, cols, stride, blocks_of(cols), rows * blocks_of(cols) * 4};
-    if (a.units == 0) return 0;
-    const int64_t grid = (a.units + kThreads - 1) / kThreads;
-    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    if (f32) hipLaunchKernelGGL(mx4_dequantize_kernel<float>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, static_cast<float *>(out));
-    else hipLaunchKernelGGL(mx4_dequantize_kernel<bf16_t>, dim3((unsigned)grid), dim3(kThreads), 0, st, a, static_cast<bf16_t *>(out));
-    return (int)hipGetLastError();
+    const QuantArgs a = {nullptr, out, codes, scales, nullptr, nullptr, rows, cols, stride, 0, 0, 0};
+    if (cols < 8) return f32 ? launch_quant(a, mx4_dequantize_kernel<float, true>, st) : launch_quant(a, mx4_dequantize_kernel<bf16_t, true>, st);
+    return f32 ? launch_quant(a, mx4_dequantize_kernel<float, false>, st) : launch_quant(a, mx4_dequantize_kernel<bf16_t, false>, st);
 }
 
 bool mx4_product_takes_bf16(int64_t m) { return m <= kBf16Rows; }

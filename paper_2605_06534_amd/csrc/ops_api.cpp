@@ -102,7 +102,7 @@ extern "C" rose_status rose_grad_sum_squares(const void *const *grad_ptrs, const
     if (!sum) return ROSE_ERR_ARG;
     if (!aligned(sum, 8)) return ROSE_ERR_ALIGN;
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, ROSE_GRAD_WORKSPACE_BYTES));
-    rose::GradArgs a = {grad_ptrs, nullptr, offsets, n_tensors, static_cast<double *>(workspace), 0, sum, 0.f, nullptr};
+    rose::GradArgs a = {grad_ptrs, nullptr, offsets, n_tensors, 0, static_cast<double *>(workspace), 0, sum, 0.f, nullptr};
     return status_of(rose::launch_grad_sum_squares(a, total, dtype == ROSE_DTYPE_F32, stream));
 }
 
@@ -112,7 +112,7 @@ extern "C" rose_status rose_grad_clip(const void *const *grad_ptrs, const int64_
     ROSE_CHECK(check_grads(grad_ptrs, offsets, n_tensors, total, dtype));
     if (!out_ptrs || !sum || !(max_norm >= 0.f)) return ROSE_ERR_ARG;
     if (!aligned(out_ptrs, 8) || !aligned(sum, 8) || !aligned(norm, 4)) return ROSE_ERR_ALIGN;
-    rose::GradArgs a = {grad_ptrs, out_ptrs, offsets, n_tensors, nullptr, 0, const_cast<double *>(sum), max_norm, norm};
+    rose::GradArgs a = {grad_ptrs, out_ptrs, offsets, n_tensors, 0, nullptr, 0, const_cast<double *>(sum), max_norm, norm};
     return status_of(rose::launch_grad_clip(a, total, dtype == ROSE_DTYPE_F32, stream));
 }
 
@@ -123,7 +123,7 @@ extern "C" rose_status rose_grad_clip_norm(const void *const *grad_ptrs, const i
     if (!out_ptrs || !(max_norm >= 0.f)) return ROSE_ERR_ARG;
     if (!aligned(out_ptrs, 8) || !aligned(norm, 4)) return ROSE_ERR_ALIGN;
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, ROSE_GRAD_WORKSPACE_BYTES));
-    rose::GradArgs a = {grad_ptrs, out_ptrs, offsets, n_tensors, static_cast<double *>(workspace), 0, nullptr, max_norm, norm};
+    rose::GradArgs a = {grad_ptrs, out_ptrs, offsets, n_tensors, 0, static_cast<double *>(workspace), 0, nullptr, max_norm, norm};
     return status_of(rose::launch_grad_clip_norm(a, total, dtype == ROSE_DTYPE_F32, stream));
 }
 

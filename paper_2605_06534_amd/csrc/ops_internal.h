@@ -43,6 +43,7 @@ struct GradArgs {
     void *const *out_ptrs;
     const int64_t *offsets;
     int32_t n_tensors;
+    int64_t piece;                      // elements that a workgroup takes at a time
     double *partials;                   // sum of squares of each workgroup
     int32_t n_partials;
     double *sum;
