@@ -14,6 +14,7 @@ constexpr int kSmallItems = 16;                 // tokens a thread of it takes a
 constexpr int64_t kSmallTokens = (int64_t)kSortThreads * kSmallItems;
 constexpr int kTileItems = 2, kTile = kSortThreads * kTileItems;   // tokens that a workgroup of the large sort takes at a time
 constexpr int kMostTiles = 256;
+constexpr int64_t kBlindBytes = 128 << 20;       // of a gradient that is filled with zeros while one workgroup sorts
 constexpr int64_t kShortestRun = 32;            // sorted tokens that are summed in one go
 
 // row of the table that a token names, rows if none
@@ -26,33 +27,36 @@ __device__ __forceinline__ uint32_t row_of(const Tokens &t, int64_t i) {
 // -------------------------------------------------------------------------------------------------
 // lookup
 // -------------------------------------------------------------------------------------------------
-// A row goes to 1 << log_lanes lanes, eight columns each; R rows a lane, all of them asked for before the first is used.
+// R vectors of 16 bytes of the output a lane.  It asks for its tokens, then for their rows, before it uses the first.
+template <class OT> constexpr int kLookupWidth = 16 / sizeof(OT);
 template <class TT, class OT, int R, bool NARROW>
-__global__ __launch_bounds__(kLookupThreads) void embedding_lookup_kernel(LookupArgs a, int log_lanes, uint32_t chunks) {
-    const uint32_t group = blockIdx.x / chunks, chunk = blockIdx.x - group * chunks;
-    const int lane = threadIdx.x & ((1 << log_lanes) - 1), sub = threadIdx.x >> log_lanes;
-    const int per = kLookupThreads >> log_lanes;
-    const Columns<NARROW> col(((int64_t)chunk * kLookupThreads + lane) * 8, a.cols);
-    if (!col.n) return;
-    const int64_t i0 = (int64_t)group * (R * per) + sub;
-    uint32_t row[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) row[r] = i0 + r * per < a.tokens.n ? row_of(a.tokens, i0 + r * per) : (uint32_t)a.tokens.rows;
-    Raw8<TT> raw[R];
+__global__ __launch_bounds__(kLookupThreads) void embedding_lookup_kernel(LookupArgs a, Rows rows) {
+    constexpr int W = kLookupWidth<OT>;
+    const Group<kLookupThreads * R> group(rows);
+    int64_t i[R];
+    uint32_t vector[R], row[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        zero8(raw[r]);
+        group.place(rows, r * kLookupThreads + threadIdx.x, i[r], vector[r]);
+        row[r] = i[r] < a.tokens.n ? row_of(a.tokens, i[r]) : (uint32_t)a.tokens.rows;
+    }
+    Raw<TT, W> raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        zero(raw[r]);
+        const Columns<NARROW, W> col((int64_t)vector[r] * W, a.cols);
         if (row[r] < a.tokens.rows) col.load(static_cast<const TT *>(a.table) + (int64_t)row[r] * a.table_stride, raw[r]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        if (i0 + r * per >= a.tokens.n) return;
-        float f[8];
-        widen8(raw[r], f);
+        if (i[r] >= a.tokens.n) return;
+        const Columns<NARROW, W> col((int64_t)vector[r] * W, a.cols);
+        float f[W];
+        widen(raw[r], f);
         // (zeros stay zeros under any scale: of another shard, not 0 * inf)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = row[r] < a.tokens.rows ? f[e] * a.scale : 0.f;
-        col.store(static_cast<OT *>(a.out) + (i0 + r * per) * a.out_stride, f);
+        for (int e = 0; e < W; ++e) f[e] = row[r] < a.tokens.rows ? f[e] * a.scale : 0.f;
+        col.template store<true>(static_cast<OT *>(a.out) + i[r] * a.out_stride, f);
     }
 }
 
@@ -134,7 +138,7 @@ __device__ __forceinline__ void fill_zeros(const Fill &f, int64_t worker) {
         char *p = f.at + row * f.stride_bytes + from;
         const int64_t n = f.row_bytes - from < kPiece ? f.row_bytes - from : kPiece;
         for (int64_t i = (int64_t)threadIdx.x * 16; i < n; i += (int64_t)kSortThreads * 16) {
-            if (i + 16 <= n) *reinterpret_cast<u32x4_any *>(p + i) = u32x4{0, 0, 0, 0};
+            if (i + 16 <= n) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4_any *>(p + i));
             else
                 for (int64_t j = i; j < n; j += 2) *reinterpret_cast<uint16_t *>(p + j) = 0;
         }
@@ -331,19 +335,51 @@ struct SumArgs {
     void *grad;
     float *parts;                               // [block][2][parts_stride]: sums of runs that begin before the block, behind it
     int64_t parts_stride, run;                  // run: tokens of a block
+    int64_t fill_rows;                          // the rows below this one that no token names become zero here
+    uint32_t join_groups;                       // workgroups that join
     uint32_t chunks;                            // a row's columns go to this many waves ...
     int32_t lanes;                              // ... of so many lanes
     float scale;
     int32_t accumulate;
 };
 
+// Zeros for those of eight rows that no token names: each row is looked for among the sorted tokens by eight lanes.
+constexpr int kFillRows = 8;
+template <class GT>
+__device__ __forceinline__ void fill_unnamed(const SumArgs &a, uint32_t group) {
+    const int lane = threadIdx.x & 63, sub = lane & 7;
+    const int64_t first = (int64_t)group * kFillRows, row = first + (lane >> 3);
+    int64_t lo = 0, hi = a.n;                            // the first token of this row or a later one is at lo .. hi
+    while (__ballot(lo < hi)) {
+        const int64_t step = (hi - lo + 7) / 8, mine = lo + (sub + 1) * step - 1;
+        const bool before = mine < hi && a.keys[mine] < row;
+        const int64_t below = __popcll((__ballot(before) >> (lane & 56)) & 0xFF);
+        const int64_t end = lo + (below + 1) * step - 1;
+        lo += below * step;
+        hi = end < hi ? end : hi;
+        lo = lo < hi ? lo : hi;
+    }
+    const uint64_t named = __ballot(lo < a.n && a.keys[lo < a.n ? lo : 0] == row);
+    for (int r = 0; r < kFillRows && first + r < a.fill_rows; ++r) {
+        if (named >> (8 * r) & 1) continue;
+        GT *p = static_cast<GT *>(a.grad) + (first + r) * a.grad_stride;
+        constexpr int kLane = 16 / sizeof(GT);           // elements of 16 bytes
+        for (int64_t c = (int64_t)lane * kLane; c < a.cols; c += 64 * kLane) {
+            if (c + kLane <= a.cols) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4_any *>(p + c));
+            else
+                for (int64_t e = c; e < a.cols; ++e) p[e] = from_f32<GT>(0.f);
+        }
+    }
+}
+
 // A block of sorted tokens and eight columns a lane, one wave a workgroup.  A row whose tokens all lie in the block is
 // finished here; what crosses the block's ends is left for the join.  Rows come kAhead at a time, the next ones asked for before
 // the last are added, and with them (ADD) what is in the gradient of the rows that end among them: a load where a run ends would
-// wait for all that were asked for before it, stores included.
+// wait for all that were asked for before it, stores included.  (ADD: two at a time, four take registers that waves could use:
+// 65536 tokens of 5120 columns 272 us, 295.)
 template <class DT, class GT, bool NARROW, bool ADD>
 __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
-    constexpr int kAhead = ADD ? 4 : 8;
+    constexpr int kAhead = ADD ? 2 : 8;
     constexpr int kWindow = 32;
     // Workgroups i, i + 8, ... run on one XCD; all columns of a block go to one.  (With each column of waves on an XCD of its own,
     // as where there are eight of them, an XCD reads the same kilobyte of every row: a quarter of its L2's channels.)
@@ -370,7 +406,7 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
     auto get = [&](int64_t window, int i0, int which) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            col.load(static_cast<const DT *>(a.dy) + (int64_t)(uint32_t)__builtin_amdgcn_readlane(places, i0 + u) * a.dy_stride, raw[which][u]);
+            col.template load<sizeof(DT) == 2>(static_cast<const DT *>(a.dy) + (int64_t)(uint32_t)__builtin_amdgcn_readlane(places, i0 + u) * a.dy_stride, raw[which][u]);
             if constexpr (ADD) {
                 const uint32_t key = key_at(i0 + u);
                 if (key < a.rows && key_at(i0 + u + 1) != key && window + i0 + u < to)
@@ -387,13 +423,13 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
             const uint32_t key = key_at(i0 + u);
             if (j >= to || key >= a.rows) return false;
             float f[8];
-            widen8(raw[which][u], f);
+            widen(raw[which][u], f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += f[e];
             const bool ends = key_at(i0 + u + 1) != key;
             if (ends && !open) {
                 if constexpr (ADD) {
-                    widen8(old[which][u], f);
+                    widen(old[which][u], f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[e] = f[e] + sum[e] * a.scale;
                 } else
@@ -429,27 +465,27 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
 // A run that crosses the end of the block it begins in: the sums of its parts.  Four columns a lane; where there are few
 // parts each of the four waves adds those of its own 256 columns, where there are many the waves take every fourth part and
 // their sums are added in order, 256 columns after the other.
+// The workgroups behind these write zeros to rows that no token names.
 template <class GT>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, uint32_t chunks) {
     __shared__ f32x4 sums[4][64];
+    if (blockIdx.x >= a.join_groups) {
+        fill_unnamed<GT>(a, (blockIdx.x - a.join_groups) * 4 + (threadIdx.x >> 6));
+        return;
+    }
     const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x - block * chunks;
     const int64_t from = (int64_t)block * a.run, next = from + a.run;
     const uint32_t key = a.keys[next], in_front = a.keys[next - 1], before = from > 0 ? a.keys[from - 1] : 0xFFFFFFFFu;
     if (key >= a.rows || in_front != key || before == key) return;
-    // the run ends in front of the first other row: looked for block by block (in most cases the next one), then by halves
-    int64_t lo = next, hi = a.n, step = a.run;
-    while (lo + step < a.n && a.keys[lo + step] == key) {
-        lo += step;
-        step *= 2;
-    }
-    if (lo + step < hi) hi = lo + step;
-    while (lo < hi) {
-        const int64_t mid = lo + (hi - lo) / 2;
-        if (a.keys[mid] == key) lo = mid + 1;
-        else hi = mid;
-    }
-    const int64_t last = (lo - 1) / a.run;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the blocks that begin with this row, 64 candidates at a time
+    int64_t last = block;
+    for (;;) {
+        const int64_t at = (last + 1 + lane) * a.run;
+        const uint64_t with = __ballot(at < a.n && a.keys[at < a.n ? at : 0] == key);
+        last += ~with ? __builtin_ctzll(~with) : 64;
+        if (~with) break;
+    }
     auto add = [&](int64_t col, int64_t first, int64_t hop) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         const float *parts = a.parts + col;
@@ -530,23 +566,22 @@ size_t embedding_grad_workspace(int64_t rows, int64_t cols, int64_t n_tokens) { 
 int launch_embedding_lookup(const LookupArgs &a, bool table_f32, bool out_f32, void *stream) {
     if (a.tokens.n == 0 || a.cols == 0) return 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    int log_lanes = 2;
-    while (log_lanes < 8 && ((int64_t)8 << log_lanes) < a.cols) ++log_lanes;
-    const int64_t chunks = (a.cols + kLookupThreads * 8 - 1) / (kLookupThreads * 8), per = kLookupThreads >> log_lanes;
-    const bool many = a.cols >= 8 && (a.tokens.n / per) * chunks >= 8192;       // enough for every CU also at four rows a lane
-    const int64_t groups = (a.tokens.n + per * (many ? 4 : 1) - 1) / (per * (many ? 4 : 1));
-    if (groups * chunks > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    const dim3 grid((unsigned)(groups * chunks)), block(kLookupThreads);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, log_lanes, (uint32_t)chunks); };
     auto of_types = [&](auto t, auto o) {
         using TT = decltype(t);
         using OT = decltype(o);
-        if (a.cols < 8) go(embedding_lookup_kernel<TT, OT, 1, true>);
-        else many ? go(embedding_lookup_kernel<TT, OT, 4, false>) : go(embedding_lookup_kernel<TT, OT, 1, false>);
+        constexpr int W = kLookupWidth<OT>;
+        const int64_t row_vectors = (a.cols + W - 1) / W, vectors = a.tokens.n * row_vectors;
+        const bool many = a.cols >= W && vectors >= (int64_t)kLookupThreads * 2 * 1024;   // enough for every CU also at two a lane
+        const int64_t per = kLookupThreads * (many ? 2 : 1), groups = (vectors + per - 1) / per;
+        if (groups > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+        const Rows rows = rows_of(a.tokens.n, row_vectors);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kLookupThreads), 0, st, a, rows); };
+        if (a.cols < W) go(embedding_lookup_kernel<TT, OT, 1, true>);
+        else many ? go(embedding_lookup_kernel<TT, OT, 2, false>) : go(embedding_lookup_kernel<TT, OT, 1, false>);
+        return (int)hipGetLastError();
     };
-    if (table_f32) out_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
-    else out_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
-    return (int)hipGetLastError();
+    if (table_f32) return out_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
+    return out_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
 }
 
 int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32, void *stream) {
@@ -567,13 +602,18 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     s.width = (s.bits + s.passes - 1) / s.passes;
     s.tiles = l.tiles;
     s.subtiles = l.subtiles;
-    int64_t fills = 0;
+    // Zeros for rows without tokens: as much as the sort takes the time of goes blindly with it (the last rows, of which tokens
+    // name the fewest), the rest behind the sums, past the rows that have some.  (All of it with the sort: 8191 tokens and a gradient of
+    // 524 MB 133 us, 127 this way.)
+    int64_t fills = 0, fill_later = 0;
     if (!a.accumulate) {
-        const int64_t size = grad_f32 ? 4 : 2;
+        const int64_t size = grad_f32 ? 4 : 2, row_bytes = a.cols * size;
+        const int64_t blind = n == 0 ? rows : kBlindBytes / row_bytes < rows ? kBlindBytes / row_bytes : rows;
         const bool whole = a.grad_stride == a.cols;
-        s.fill.at = static_cast<char *>(a.grad);
-        s.fill.rows = whole ? 1 : rows;
-        s.fill.row_bytes = (whole ? rows * a.cols : a.cols) * size;
+        fill_later = rows - blind;
+        s.fill.at = static_cast<char *>(a.grad) + fill_later * a.grad_stride * size;
+        s.fill.rows = whole ? 1 : blind;
+        s.fill.row_bytes = whole ? blind * row_bytes : row_bytes;
         s.fill.stride_bytes = a.grad_stride * size;
         const int64_t pieces = s.fill.rows * ((s.fill.row_bytes + 32767) / 32768);
         fills = pieces < 2048 ? pieces : 2048;
@@ -584,6 +624,7 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
         const dim3 grid((unsigned)(1 + fills)), block(kSortThreads);
         if (n <= kSortThreads) hipLaunchKernelGGL(sort_small_kernel<1>, grid, block, 0, st, s);
         else if (n <= 4 * kSortThreads) hipLaunchKernelGGL(sort_small_kernel<4>, grid, block, 0, st, s);
+        else if (n <= 8 * kSortThreads) hipLaunchKernelGGL(sort_small_kernel<8>, grid, block, 0, st, s);
         else hipLaunchKernelGGL(sort_small_kernel<16>, grid, block, 0, st, s);
     } else {
         hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)(l.tiles + fills)), dim3(kSortThreads), 0, st, s);
@@ -626,10 +667,12 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     };
     if (dy_f32) grad_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
     else grad_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
-    if (l.blocks > 1) {
-        auto join = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)((l.blocks - 1) * join_chunks)), dim3(256), 0, st, u, (uint32_t)join_chunks);
-        };
+    const int64_t joins = (l.blocks - 1) * join_chunks, all = joins + (fill_later + 4 * kFillRows - 1) / (4 * kFillRows);
+    if (all > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    u.fill_rows = fill_later;
+    u.join_groups = (uint32_t)joins;
+    if (all > 0) {
+        auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)all), dim3(256), 0, st, u, (uint32_t)join_chunks); };
         grad_f32 ? join(embedding_join_kernel<float>) : join(embedding_join_kernel<bf16_t>);
     }
     return (int)hipGetLastError();

@@ -7,10 +7,13 @@ namespace rose {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWorkgroups = 2048;                // at most: eight a CU
-// All tensors laid end to end are cut into pieces, which the workgroups take in turn.
-constexpr int64_t kSmallPiece = 8192, kLargePiece = 32768;
-int64_t piece_of(int64_t total) { return total <= kWorkgroups * kSmallPiece ? kSmallPiece : kLargePiece; }
+constexpr int kWorkgroups = 2048;                // that sum squares, at most: eight a CU
+constexpr int kAhead = 4;                        // vectors that a thread has under way
+// elements of 16 bytes, what a lane reads or writes at a time: neighbouring lanes touch neighbouring vectors in either type
+template <class T> constexpr int kPer = 16 / sizeof(T);
+// All tensors laid end to end are cut into pieces.  A small one is a vector for each thread kAhead times.
+template <class T> constexpr int64_t kSmallPiece = kAhead * kThreads * kPer<T>;
+constexpr int64_t kLargePiece = 32768;
 
 // The tensor that holds position `at`: the last one that begins at or before it, 64 candidates at a time.
 __device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, int64_t at) {
@@ -28,7 +31,7 @@ __device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, 
 // Calls f(tensor, first element, number) for every stretch of a tensor in this workgroup's pieces.
 template <class F>
 __device__ __forceinline__ void for_stretches(const GradArgs &a, F f) {
-    for (int64_t from = blockIdx.x * a.piece;; from += gridDim.x * a.piece) {
+    for (int64_t from = blockIdx.x * a.piece;;) {
         // (the tensor is looked for before the end is known: one trip to memory less in front of the first element)
         int32_t t = tensor_at(a.offsets, a.n_tensors, from);
         const int64_t total = a.offsets[a.n_tensors], to = from + a.piece < total ? from + a.piece : total;
@@ -39,14 +42,9 @@ __device__ __forceinline__ void for_stretches(const GradArgs &a, F f) {
             const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
             if (lo < hi) f(t, lo - base, hi - lo);
         }
+        from += gridDim.x * a.piece;
+        if (from >= total) return;
     }
-}
-
-__device__ __forceinline__ double squares(const float (&f)[8]) {
-    double s = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fma((double)f[e], (double)f[e], s);
-    return s;
 }
 
 // sum over the workgroup, the same in every thread
@@ -71,39 +69,27 @@ __device__ __forceinline__ int64_t head_of(const T *p, int64_t n) {
 
 template <class T>
 __device__ __forceinline__ double squares_of(const T *p, int64_t n) {
-    constexpr int kAhead = 4;
+    const int64_t head = head_of(p, n), vectors = (n - head) / kPer<T>, tail = head + vectors * kPer<T>;
+    // (what is in front of the first vector and behind the last: fewer elements than a vector has)
+    const double before = threadIdx.x < head ? (double)to_f32(p[threadIdx.x]) : 0.;
+    const double behind = threadIdx.x < n - tail ? (double)to_f32(p[tail + threadIdx.x]) : 0.;
     double s = 0;
-    const int64_t head = head_of(p, n), vectors = (n - head) / 8, tail = head + vectors * 8;
-    const T *body = p + head;
-    int64_t i = threadIdx.x;
-    for (; i + (kAhead - 1) * kThreads < vectors; i += kAhead * kThreads) {
-        Raw8<T> raw[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) load8(body + (i + u * kThreads) * 8, raw[u]);
+    for (int64_t i = threadIdx.x; i < vectors; i += kAhead * kThreads) {
+        Raw<T, kPer<T>> raw[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            float f[8];
-            widen8(raw[u], f);
-            s += squares(f);
+            zero(raw[u]);
+            if (i + u * kThreads < vectors) load<true>(p + head + (i + u * kThreads) * kPer<T>, raw[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float f[kPer<T>];
+            widen(raw[u], f);
+#pragma unroll
+            for (int e = 0; e < kPer<T>; ++e) s = fma((double)f[e], (double)f[e], s);
         }
     }
-    for (; i < vectors; i += kThreads) {
-        Raw8<T> raw;
-        float f[8];
-        load8(body + i * 8, raw);
-        widen8(raw, f);
-        s += squares(f);
-    }
-    // (what is in front of the first vector and behind the last)
-    if (threadIdx.x < head) {
-        const double f = to_f32(p[threadIdx.x]);
-        s = fma(f, f, s);
-    }
-    if (threadIdx.x < n - tail) {
-        const double f = to_f32(p[tail + threadIdx.x]);
-        s = fma(f, f, s);
-    }
-    return s;
+    return fma(before, before, fma(behind, behind, s));
 }
 
 template <class T>
@@ -131,53 +117,39 @@ __global__ __launch_bounds__(kThreads) void grad_sum_kernel(GradArgs a) {
     if (threadIdx.x == 0) *a.sum = s;
 }
 
-// The first kAhead vectors of a stretch that this thread scales, asked for before the factor is known.
-constexpr int kAhead = 4;
+// The vectors of a stretch that this thread scales, asked for before the factor is known.  (A stretch is no longer than a small piece.)
 template <class T>
 struct Begun {
-    Raw8<T> raw[kAhead];
+    Raw<T, kPer<T>> raw[kAhead];
+    T before, behind;
 };
 template <class T>
 __device__ __forceinline__ void begin(const T *p, const T *q, int64_t n, Begun<T> &b) {
-    const int64_t head = head_of(q, n), vectors = (n - head) / 8;
+    const int64_t head = head_of(q, n), vectors = (n - head) / kPer<T>, tail = head + vectors * kPer<T>;
+    if (threadIdx.x < head) b.before = p[threadIdx.x];
+    if (threadIdx.x < n - tail) b.behind = p[tail + threadIdx.x];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
         const int64_t i = threadIdx.x + u * kThreads;
-        if (i < vectors) load8(p + head + i * 8, b.raw[u]);
+        if (i < vectors) load<true>(p + head + i * kPer<T>, b.raw[u]);
     }
 }
 template <class T>
-__device__ __forceinline__ void scale_into(const T *p, T *q, int64_t n, float factor, const Begun<T> &begun) {
-    const int64_t head = head_of(q, n), vectors = (n - head) / 8, tail = head + vectors * 8;
-    const T *from = p;
-    T *to = q;
-    p += head;
-    q += head;
-    auto put = [&](int64_t i, const Raw8<T> &raw) {
-        float f[8];
-        widen8(raw, f);
+__device__ __forceinline__ void scale_into(T *q, int64_t n, float factor, const Begun<T> &b) {
+    const int64_t head = head_of(q, n), vectors = (n - head) / kPer<T>, tail = head + vectors * kPer<T>;
+    if (threadIdx.x < head) q[threadIdx.x] = from_f32<T>(to_f32(b.before) * factor);
+    if (threadIdx.x < n - tail) q[tail + threadIdx.x] = from_f32<T>(to_f32(b.behind) * factor);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= factor;
-        store8(q + i * 8, f);
-    };
+    for (int u = 0; u < kAhead; ++u) {
+        const int64_t i = threadIdx.x + u * kThreads;
+        if (i < vectors) {
+            float f[kPer<T>];
+            widen(b.raw[u], f);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-        if (threadIdx.x + u * kThreads < vectors) put(threadIdx.x + u * kThreads, begun.raw[u]);
-    int64_t i = threadIdx.x + kAhead * kThreads;
-    for (; i + (kAhead - 1) * kThreads < vectors; i += kAhead * kThreads) {
-        Raw8<T> raw[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) load8(p + (i + u * kThreads) * 8, raw[u]);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) put(i + u * kThreads, raw[u]);
+            for (int e = 0; e < kPer<T>; ++e) f[e] *= factor;
+            store<true>(q + head + i * kPer<T>, f);
+        }
     }
-    for (; i < vectors; i += kThreads) {
-        Raw8<T> raw;
-        load8(p + i * 8, raw);
-        put(i, raw);
-    }
-    if (threadIdx.x < head) to[threadIdx.x] = from_f32<T>(to_f32(from[threadIdx.x]) * factor);
-    if (threadIdx.x < n - tail) to[tail + threadIdx.x] = from_f32<T>(to_f32(from[tail + threadIdx.x]) * factor);
 }
 
 template <class T, bool FROM_PARTIALS>
@@ -199,54 +171,70 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
         Begun<T> begun;
         if (any) begin(p + first, q + first, n, begun);
         if (!known) find_factor();
-        if (any && !(p == q && factor == 1.f)) scale_into(p + first, q + first, n, factor, begun);
+        if (any && !(p == q && factor == 1.f)) scale_into(q + first, n, factor, begun);
     });
     if (!known) find_factor();
 }
 
-int workgroups(int64_t total) {
-    const int64_t pieces = (total + kSmallPiece - 1) / kSmallPiece;
-    return (int)(pieces < 1 ? 1 : pieces > kWorkgroups ? kWorkgroups : pieces);
+template <class T>
+int64_t small_pieces(int64_t total) {
+    const int64_t n = (total + kSmallPiece<T> - 1) / kSmallPiece<T>;
+    return n < 1 ? 1 : n;
 }
 
-}  // namespace
-
-static_assert(kGradPartials >= kWorkgroups, "the workspace holds a partial sum of each workgroup");
-
-static int squares(GradArgs &a, int64_t total, bool f32, hipStream_t st) {
-    a.piece = piece_of(total);
-    a.n_partials = workgroups(total);
-    if (f32) hipLaunchKernelGGL(grad_squares_kernel<float>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL(grad_squares_kernel<bf16_t>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
+template <class T>
+int squares(GradArgs &a, int64_t total, hipStream_t st) {
+    const int64_t n = small_pieces<T>(total);
+    a.piece = n > kWorkgroups ? kLargePiece : kSmallPiece<T>;
+    a.n_partials = (int)(n > kWorkgroups ? kWorkgroups : n);
+    hipLaunchKernelGGL(grad_squares_kernel<T>, dim3(a.n_partials), dim3(kThreads), 0, st, a);
     return (int)hipGetLastError();
 }
 
-int launch_grad_sum_squares(const GradArgs &args, int64_t total, bool f32, void *stream) {
-    GradArgs a = args;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    if (int e = squares(a, total, f32, st)) return e;
+template <class T, bool FROM_PARTIALS>
+int clip(GradArgs &a, int64_t total, hipStream_t st) {
+    const int64_t n = small_pieces<T>(total), most = 1 << 30;
+    a.piece = kSmallPiece<T>;
+    hipLaunchKernelGGL((grad_clip_kernel<T, FROM_PARTIALS>), dim3((unsigned)(n < most ? n : most)), dim3(kThreads), 0, st, a);
+    return (int)hipGetLastError();
+}
+
+int sum_squares(GradArgs &a, int64_t total, bool f32, hipStream_t st) {
+    if (int e = f32 ? squares<float>(a, total, st) : squares<bf16_t>(a, total, st)) return e;
     hipLaunchKernelGGL(grad_sum_kernel, dim3(1), dim3(kThreads), 0, st, a);
     return (int)hipGetLastError();
 }
 
+template <class T>
+int clip_norm(GradArgs &a, int64_t total, hipStream_t st) {
+    if (small_pieces<T>(total) <= kWorkgroups) {
+        if (int e = squares<T>(a, total, st)) return e;
+        return clip<T, true>(a, total, st);
+    }
+    a.sum = a.partials + kWorkgroups;
+    if (int e = sum_squares(a, total, sizeof(T) == 4, st)) return e;
+    return clip<T, false>(a, total, st);
+}
+
+}  // namespace
+
+static_assert(kGradPartials > kWorkgroups, "the workspace holds a partial sum of each workgroup, and their sum");
+
+int launch_grad_sum_squares(const GradArgs &args, int64_t total, bool f32, void *stream) {
+    GradArgs a = args;
+    return sum_squares(a, total, f32, static_cast<hipStream_t>(stream));
+}
+
 int launch_grad_clip(const GradArgs &args, int64_t total, bool f32, void *stream) {
     GradArgs a = args;
-    a.piece = piece_of(total);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid(workgroups(total)), block(kThreads);
-    if (f32) hipLaunchKernelGGL((grad_clip_kernel<float, false>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((grad_clip_kernel<bf16_t, false>), grid, block, 0, st, a);
-    return (int)hipGetLastError();
+    return f32 ? clip<float, false>(a, total, st) : clip<bf16_t, false>(a, total, st);
 }
 
 int launch_grad_clip_norm(const GradArgs &args, int64_t total, bool f32, void *stream) {
     GradArgs a = args;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (int e = squares(a, total, f32, st)) return e;
-    const dim3 grid(workgroups(total)), block(kThreads);
-    if (f32) hipLaunchKernelGGL((grad_clip_kernel<float, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((grad_clip_kernel<bf16_t, true>), grid, block, 0, st, a);
-    return (int)hipGetLastError();
+    return f32 ? clip_norm<float>(a, total, st) : clip_norm<bf16_t>(a, total, st);
 }
 
 }  // namespace rose

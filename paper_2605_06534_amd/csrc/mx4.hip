@@ -22,100 +22,83 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
 __device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_float(scale ? scale << 23 : 0x00400000u); }
 
 // -------------------------------------------------------------------------------------------------
-// quantisation: four lanes a block, eight elements each, kUnits times eight a lane
+// quantisation: four lanes a block of bf16, eight of fp32, 16 bytes each, kUnits times so many a lane
 // -------------------------------------------------------------------------------------------------
-constexpr int kUnits = 4;
+constexpr int kUnits = 2;
 
 struct QuantArgs {
     const void *x;                              // the matrix, of which ...
     void *out;                                  // ... or into which
     const uint8_t *codes_in, *scales_in;
     uint8_t *codes, *scales;
-    int64_t rows, cols, stride, units;          // units: eights of all rows, filled up to whole blocks
-    uint32_t row_units, by_row_units;           // of a row; 2^32 over that, rounded up
+    int64_t cols, stride;
+    Rows rows;                                  // vectors of 16 bytes of x or out in all rows, filled up to whole blocks
 };
-
-// Row and column of this lane's u-th eight.  A workgroup's kThreads * kUnits of them begin in one row; where rows are shorter the
-// quotient of two numbers below 2048 comes from a product with the reciprocal (exact: off by less than 2048 / 2^32).
-struct Place {
-    int64_t row;
-    uint32_t in_row;
-    bool inside;
-};
-__device__ __forceinline__ Place place_of(const QuantArgs &a, int u) {
-    const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnits), row0 = first / a.row_units;
-    const int64_t unit = first + u * kThreads + threadIdx.x;
-    const uint32_t from_row0 = (uint32_t)(unit - row0 * a.row_units);
-    const uint32_t rows = a.row_units >= kThreads * kUnits ? (from_row0 >= a.row_units ? 1u : 0u) : __umulhi(from_row0, a.by_row_units);
-    return Place{row0 + rows, from_row0 - rows * a.row_units, unit < a.units};
-}
-
+template <class T> constexpr int kWidth = 16 / sizeof(T);      // elements of a lane, 16 bytes: neighbouring lanes read neighbouring vectors
 // the elements from the k-th on, zeros behind them
-__device__ __forceinline__ void drop(Raw8<bf16_t> &r, int k) {
-    const u32x4 zeros = {0, 0, 0, 0};
-    if (k >= 8) r.v = zeros;
-    if (k & 4) r.v = u32x4{r.v[2], r.v[3], 0, 0};
-    if (k & 2) r.v = u32x4{r.v[1], r.v[2], r.v[3], 0};
-    if (k & 1) r.v = u32x4{r.v[0] >> 16 | r.v[1] << 16, r.v[1] >> 16 | r.v[2] << 16, r.v[2] >> 16 | r.v[3] << 16, r.v[3] >> 16};
-}
-__device__ __forceinline__ void drop(Raw8<float> &r, int k) {
-    const f32x4 zeros = {0.f, 0.f, 0.f, 0.f};
-    if (k >= 8) r.lo = r.hi = zeros;
-    if (k & 4) {
-        r.lo = r.hi;
-        r.hi = zeros;
-    }
+__device__ __forceinline__ void drop_words(uint32_t (&d)[4], int k) {
     if (k & 2) {
-        r.lo = f32x4{r.lo[2], r.lo[3], r.hi[0], r.hi[1]};
-        r.hi = f32x4{r.hi[2], r.hi[3], 0.f, 0.f};
+        d[0] = d[2];
+        d[1] = d[3];
+        d[2] = d[3] = 0;
     }
     if (k & 1) {
-        r.lo = f32x4{r.lo[1], r.lo[2], r.lo[3], r.hi[0]};
-        r.hi = f32x4{r.hi[1], r.hi[2], r.hi[3], 0.f};
+        d[0] = d[1];
+        d[1] = d[2];
+        d[2] = d[3];
+        d[3] = 0;
     }
+    if (k >= 4) d[0] = d[1] = d[2] = d[3] = 0;
 }
+__device__ __forceinline__ void drop(Raw<bf16_t, 8> &r, int k) {
+    drop_words(r.d, k >> 1);
+    if (k & 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.d[i] = r.d[i] >> 16 | (i < 3 ? r.d[i < 3 ? i + 1 : 3] << 16 : 0);
+}
+__device__ __forceinline__ void drop(Raw<float, 4> &r, int k) { drop_words(r.d, k); }
 
-// Largest magnitude of eight elements, as an fp32 pattern
-__device__ __forceinline__ uint32_t largest(const Raw8<bf16_t> &r) {
+// Largest magnitude of a lane's elements, as an fp32 pattern
+__device__ __forceinline__ uint32_t largest(const Raw<bf16_t, 8> &r) {
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     u16x2 top = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)(r.v[i] & 0x7FFF7FFFu)));
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)(r.d[i] & 0x7FFF7FFFu)));
     return (uint32_t)(top[0] > top[1] ? top[0] : top[1]) << 16;
 }
-__device__ __forceinline__ uint32_t largest(const Raw8<float> &r) {
+__device__ __forceinline__ uint32_t largest(const Raw<float, 4> &r) {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = __float_as_uint(r.lo[i]) & 0x7FFFFFFFu, hi = __float_as_uint(r.hi[i]) & 0x7FFFFFFFu;
-        top = lo > top ? lo : top;
-        top = hi > top ? hi : top;
+        const uint32_t v = r.d[i] & 0x7FFFFFFFu;
+        top = v > top ? v : top;
     }
     return top;
 }
 // Their codes: the conversions divide by the scale and round to the nearest, ties to even, at most 6.
-__device__ __forceinline__ uint32_t codes_of(const Raw8<bf16_t> &r, float by) {
-    const uint32_t pair[4] = {r.v[0], r.v[1], r.v[2], r.v[3]};
+__device__ __forceinline__ uint32_t codes_of(const Raw<bf16_t, 8> &r, float by) {
     uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[0]), by, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[1]), by, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[2]), by, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, pair[3]), by, 3);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.d[0]), by, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.d[1]), by, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.d[2]), by, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, r.d[3]), by, 3);
 }
-__device__ __forceinline__ uint32_t codes_of(const Raw8<float> &r, float by) {
+__device__ __forceinline__ uint32_t codes_of(const Raw<float, 4> &r, float by) {
     uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.lo[0], r.lo[1], by, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.lo[2], r.lo[3], by, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.hi[0], r.hi[1], by, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, r.hi[2], r.hi[3], by, 3);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(r.d[0]), __uint_as_float(r.d[1]), by, 0);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, __uint_as_float(r.d[2]), __uint_as_float(r.d[3]), by, 1);
 }
-// Codes of a lane's eight values and the scale of the block that it shares with three neighbours (all four call it).
-template <class T>
-__device__ __forceinline__ uint32_t quantised(const Raw8<T> &raw, uint32_t &scale) {
+// Codes of a lane's W values and the scale of the block that it shares with its 32 / W - 1 neighbours (all of them call it).
+template <class T, int W>
+__device__ __forceinline__ uint32_t quantised(const Raw<T, W> &raw, uint32_t &scale) {
     uint32_t top = largest(raw), other = __builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true);      // lane ^ 1
     top = other > top ? other : top;
     other = __builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true);                                   // lane ^ 2
     top = other > top ? other : top;
+    if constexpr (W == 4) {
+        other = __builtin_amdgcn_mov_dpp((int)top, 0x141, 0xF, 0xF, true);                              // lane ^ 7
+        top = other > top ? other : top;
+    }
     scale = scale_of(top);
     const uint32_t codes = codes_of(raw, scale_value(scale));
     return scale == kNanScale ? 0 : codes;
@@ -123,60 +106,76 @@ __device__ __forceinline__ uint32_t quantised(const Raw8<T> &raw, uint32_t &scal
 
 template <class T, bool NARROW>
 __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(QuantArgs a) {
-    Raw8<T> raw[kUnits];
-    int behind[kUnits];                         // rows that end inside an eight: the last whole one, moved
+    constexpr int W = kWidth<T>, kLanes = 32 / W;
+    const Group<kThreads * kUnits> group(a.rows);
+    Raw<T, W> raw[kUnits];
+    int behind[kUnits];                         // rows that end inside a vector: the last whole one, moved by so many
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const Place p = place_of(a, u);
-        const int64_t col = (int64_t)p.in_row * 8, at = col + 8 <= a.cols ? col : a.cols - 8;
-        const T *row = static_cast<const T *>(a.x) + (p.inside ? p.row : 0) * a.stride;
+        int64_t row;
+        uint32_t vector;
+        group.place(a.rows, u * kThreads + threadIdx.x, row, vector);
+        const int64_t col = (int64_t)vector * W, at = col + W <= a.cols ? col : a.cols - W;
+        const T *from = static_cast<const T *>(a.x) + (group.first + u * kThreads + threadIdx.x < a.rows.vectors ? row : 0) * a.stride;
         behind[u] = 0;
-        if (NARROW) load8(row, p.in_row == 0 ? (int)a.cols : 0, raw[u]);
+        if constexpr (NARROW) load(from, vector == 0 ? (int)a.cols : 0, raw[u]);
         else {
-            load8(row + at, raw[u]);
-            behind[u] = (int)(col - at < 8 ? col - at : 8);
+            load<true>(from + at, raw[u]);
+            behind[u] = (int)(col - at < W ? col - at : W);
         }
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const int64_t unit = ((int64_t)blockIdx.x * kUnits + u) * kThreads + threadIdx.x;
+        const int64_t unit = group.first + u * kThreads + threadIdx.x;
         if (behind[u]) drop(raw[u], behind[u]);
         uint32_t scale;
         const uint32_t codes = quantised(raw[u], scale);
-        if (unit >= a.units) return;            // (whole blocks: the four lanes of one go together)
-        reinterpret_cast<uint32_t *>(a.codes)[unit] = codes;
-        if ((unit & 3) == 0) a.scales[unit >> 2] = (uint8_t)scale;
+        if (unit >= a.rows.vectors) return;     // (whole blocks: the lanes of one go together)
+        if constexpr (W == 8) __builtin_nontemporal_store(codes, reinterpret_cast<uint32_t *>(a.codes) + unit);
+        else __builtin_nontemporal_store((uint16_t)codes, reinterpret_cast<uint16_t *>(a.codes) + unit);
+        if (unit % kLanes == 0) a.scales[unit / kLanes] = (uint8_t)scale;
     }
 }
 
 // two values of a byte of codes
-__device__ __forceinline__ void expand(uint32_t codes, float by, bool nan, float (&f)[8]) {
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 1);
-    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 3);
-    const float v[8] = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+template <int W>
+__device__ __forceinline__ void expand(uint32_t codes, float by, bool nan, float (&f)[W]) {
+    f32x2 pair[4];
+    pair[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 0);
+    pair[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 1);
+    if constexpr (W == 8) {
+        pair[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 2);
+        pair[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, by, 3);
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = nan ? __uint_as_float(0x7FC00000u) : v[e];
+    for (int e = 0; e < W; ++e) f[e] = nan ? __uint_as_float(0x7FC00000u) : pair[e / 2][e & 1];
 }
 
 template <class T, bool NARROW>
 __global__ __launch_bounds__(kThreads) void mx4_dequantize_kernel(QuantArgs a) {
+    constexpr int W = kWidth<T>, kLanes = 32 / W;
+    const Group<kThreads * kUnits> group(a.rows);
     uint32_t codes[kUnits], scale[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const int64_t unit = ((int64_t)blockIdx.x * kUnits + u) * kThreads + threadIdx.x, at = unit < a.units ? unit : 0;
-        codes[u] = reinterpret_cast<const uint32_t *>(a.codes_in)[at];
-        scale[u] = a.scales_in[at >> 2];
+        const int64_t unit = group.first + u * kThreads + threadIdx.x, at = unit < a.rows.vectors ? unit : 0;
+        if constexpr (W == 8) codes[u] = reinterpret_cast<const uint32_t *>(a.codes_in)[at];
+        else codes[u] = reinterpret_cast<const uint16_t *>(a.codes_in)[at];
+        scale[u] = a.scales_in[at / kLanes];
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-        const Place p = place_of(a, u);
-        const int64_t col = (int64_t)p.in_row * 8;
-        if (!p.inside || col >= a.cols) continue;
-        float f[8];
+        int64_t row;
+        uint32_t vector;
+        group.place(a.rows, u * kThreads + threadIdx.x, row, vector);
+        const int64_t col = (int64_t)vector * W;
+        if (group.first + u * kThreads + threadIdx.x >= a.rows.vectors) return;
+        if (col >= a.cols) continue;
+        float f[W];
         expand(codes[u], scale_value(scale[u]), scale[u] == kNanScale, f);
-        T *q = static_cast<T *>(a.out) + p.row * a.stride + col;
-        if (!NARROW && col + 8 <= a.cols) store8(q, f);
-        else store8(q, (int)(a.cols - col), f);
+        T *q = static_cast<T *>(a.out) + row * a.stride + col;
+        if (!NARROW && col + W <= a.cols) store<true>(q, f);
+        else store(q, (int)(a.cols - col), f);
     }
 }
 
@@ -419,8 +418,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
                 f[e] = sum[i][j][e];
                 f[e + 4] = sum[i + 1][j][e];
             }
-            if (col + 8 <= a.n) store8(q, f);
-            else if (col < a.n) store8(q, (int)(a.n - col), f);
+            if (col + 8 <= a.n) store(q, f);
+            else if (col < a.n) store(q, (int)(a.n - col), f);
         }
     }
 }
@@ -507,10 +506,10 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4ProductArgs a, int nb, 
                     for (int h = 0; h < kChunk / 2; ++h) {
                         const int64_t col = (int64_t)chunk * 256 + h * 512 + lane * 8;
                         const bf16_t *p = static_cast<const bf16_t *>(a.x) + (int64_t)(r0 + r) * a.x_stride + col;
-                        zero8(raw[r][h]);
+                        zero(raw[r][h]);
                         if (r0 + r < m) {
-                            if (col + 8 <= a.k) load8(p, raw[r][h]);
-                            else if (col < a.k) load8(p, (int)(a.k - col), raw[r][h]);
+                            if (col + 8 <= a.k) load(p, raw[r][h]);
+                            else if (col < a.k) load(p, (int)(a.k - col), raw[r][h]);
                         }
                     }
 #pragma unroll
@@ -604,31 +603,37 @@ int64_t blocks_of(int64_t cols) { return (cols + ROSE_MX4_BLOCK - 1) / ROSE_MX4_
 }  // namespace
 
 template <class Kernel>
-static int launch_quant(QuantArgs a, Kernel kernel, hipStream_t st) {
-    const int64_t row_units = blocks_of(a.cols) * 4, grid = (a.rows * row_units + kThreads * kUnits - 1) / (kThreads * kUnits);
-    if (grid == 0) return 0;
-    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    a.units = a.rows * row_units;
-    a.row_units = (uint32_t)row_units;
-    a.by_row_units = (uint32_t)(((1ull << 32) + row_units - 1) / row_units);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+static int launch_quant(QuantArgs a, int64_t rows, int64_t width, Kernel kernel, hipStream_t st) {
+    const int64_t row_vectors = blocks_of(a.cols) * (ROSE_MX4_BLOCK / width), per = kThreads * kUnits, groups = (rows * row_vectors + per - 1) / per;
+    if (groups == 0) return 0;
+    if (groups > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    a.rows = rows_of(rows, row_vectors);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, st, a);
     return (int)hipGetLastError();
 }
 
 int launch_mx4_quantize(const void *x, bool f32, int64_t rows, int64_t cols, int64_t stride, uint8_t *codes, uint8_t *scales,
                         void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const QuantArgs a = {x, nullptr, nullptr, nullptr, codes, scales, rows, cols, stride, 0, 0, 0};
-    if (cols < 8) return f32 ? launch_quant(a, mx4_quantize_kernel<float, true>, st) : launch_quant(a, mx4_quantize_kernel<bf16_t, true>, st);
-    return f32 ? launch_quant(a, mx4_quantize_kernel<float, false>, st) : launch_quant(a, mx4_quantize_kernel<bf16_t, false>, st);
+    const QuantArgs a = {x, nullptr, nullptr, nullptr, codes, scales, cols, stride, {}};
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        constexpr int64_t W = kWidth<T>;
+        return cols < W ? launch_quant(a, rows, W, mx4_quantize_kernel<T, true>, st) : launch_quant(a, rows, W, mx4_quantize_kernel<T, false>, st);
+    };
+    return f32 ? go(float{}) : go(bf16_t{});
 }
 
 int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out, bool f32,
                           int64_t stride, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const QuantArgs a = {nullptr, out, codes, scales, nullptr, nullptr, rows, cols, stride, 0, 0, 0};
-    if (cols < 8) return f32 ? launch_quant(a, mx4_dequantize_kernel<float, true>, st) : launch_quant(a, mx4_dequantize_kernel<bf16_t, true>, st);
-    return f32 ? launch_quant(a, mx4_dequantize_kernel<float, false>, st) : launch_quant(a, mx4_dequantize_kernel<bf16_t, false>, st);
+    const QuantArgs a = {nullptr, out, codes, scales, nullptr, nullptr, cols, stride, {}};
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        constexpr int64_t W = kWidth<T>;
+        return cols < W ? launch_quant(a, rows, W, mx4_dequantize_kernel<T, true>, st) : launch_quant(a, rows, W, mx4_dequantize_kernel<T, false>, st);
+    };
+    return f32 ? go(float{}) : go(bf16_t{});
 }
 
 bool mx4_product_takes_bf16(int64_t m) { return m <= kBf16Rows; }
