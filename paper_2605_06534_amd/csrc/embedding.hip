@@ -351,10 +351,12 @@ __device__ __forceinline__ void fill_unnamed(const SumArgs &a, uint32_t group) {
     const int64_t first = (int64_t)group * kFillRows, row = first + (lane >> 3);
     int64_t lo = 0, hi = a.n;                            // the first token of this row or a later one is at lo .. hi
     while (__ballot(lo < hi)) {
+        const bool open = lo < hi;                       // (a row that is found waits for the others)
         const int64_t step = (hi - lo + 7) / 8, mine = lo + (sub + 1) * step - 1;
-        const bool before = mine < hi && a.keys[mine] < row;
+        const bool before = open && mine < hi && a.keys[mine] < row;
         const int64_t below = __popcll((__ballot(before) >> (lane & 56)) & 0xFF);
         const int64_t end = lo + (below + 1) * step - 1;
+        if (!open) continue;
         lo += below * step;
         hi = end < hi ? end : hi;
         lo = lo < hi ? lo : hi;
