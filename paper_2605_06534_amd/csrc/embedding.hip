@@ -374,14 +374,16 @@ __device__ __forceinline__ void fill_unnamed(const SumArgs &a, uint32_t group) {
     }
 }
 
-// A block of sorted tokens and eight columns a lane, one wave a workgroup.  A row whose tokens all lie in the block is
+// A block of sorted tokens and 16 bytes of the gradient a lane, one wave a workgroup.  A row whose tokens all lie in the block is
 // finished here; what crosses the block's ends is left for the join.  Rows come kAhead at a time, the next ones asked for before
 // the last are added, and with them (ADD) what is in the gradient of the rows that end among them: a load where a run ends would
-// wait for all that were asked for before it, stores included.  (ADD: two at a time, four take registers that waves could use:
-// 65536 tokens of 5120 columns 272 us, 295.)
+// wait for all that were asked for before it, stores included.  (ADD: half as many, eight take registers that waves could use.  Four columns of an fp32 gradient a
+// lane: neighbouring lanes read and write neighbouring vectors.  65536 tokens of 5120 columns, dy fp32 346 us; eight columns a lane 386.)
+template <class GT> constexpr int kSumWidth = 16 / sizeof(GT);
 template <class DT, class GT, bool NARROW, bool ADD>
 __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
-    constexpr int kAhead = ADD ? 2 : 8;
+    constexpr int W = kSumWidth<GT>;
+    constexpr int kAhead = ADD ? 4 : 8;
     constexpr int kWindow = 32;
     // Workgroups i, i + 8, ... run on one XCD; all columns of a block go to one.  (With each column of waves on an XCD of its own,
     // as where there are eight of them, an XCD reads the same kilobyte of every row: a quarter of its L2's channels.)
@@ -393,7 +395,7 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
     const uint32_t first_key = a.keys[from], first_place = a.places[from], last_key = from > 0 ? a.keys[from - 1] : 0xFFFFFFFFu;
     if (first_key >= a.rows) return;
     const int64_t lane_of_row = (int64_t)chunk * a.lanes + lane;
-    const Columns<NARROW> col(lane < a.lanes ? lane_of_row * 8 : a.cols, a.cols);
+    const Columns<NARROW, W> col(lane < a.lanes ? lane_of_row * W : a.cols, a.cols);
     float *parts = a.parts + block * 2 * a.parts_stride;
     // Rows and tokens of 64 positions from a window's first on, a lane each: read from there without another trip to memory.
     // Positions behind the block name its first token, so that loads need no condition.
@@ -403,12 +405,12 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
         next_places = j + lane < to ? a.places[j + lane] : first_place;
     };
     auto key_at = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane(keys, i); };
-    Raw8<DT> raw[2][kAhead];
-    Raw8<GT> old[2][ADD ? kAhead : 1];
+    Raw<DT, W> raw[2][kAhead];
+    Raw<GT, W> old[2][ADD ? kAhead : 1];
     auto get = [&](int64_t window, int i0, int which) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            col.template load<sizeof(DT) == 2>(static_cast<const DT *>(a.dy) + (int64_t)(uint32_t)__builtin_amdgcn_readlane(places, i0 + u) * a.dy_stride, raw[which][u]);
+            col.template load<true>(static_cast<const DT *>(a.dy) + (int64_t)(uint32_t)__builtin_amdgcn_readlane(places, i0 + u) * a.dy_stride, raw[which][u]);
             if constexpr (ADD) {
                 const uint32_t key = key_at(i0 + u);
                 if (key < a.rows && key_at(i0 + u + 1) != key && window + i0 + u < to)
@@ -416,7 +418,7 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
             }
         }
     };
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float sum[W] = {};
     bool open = last_key == first_key;                  // the run began before the block
     auto add = [&](int64_t window, int i0, int which) {
 #pragma unroll
@@ -424,25 +426,25 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
             const int64_t j = window + i0 + u;
             const uint32_t key = key_at(i0 + u);
             if (j >= to || key >= a.rows) return false;
-            float f[8];
+            float f[W];
             widen(raw[which][u], f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += f[e];
+            for (int e = 0; e < W; ++e) sum[e] += f[e];
             const bool ends = key_at(i0 + u + 1) != key;
             if (ends && !open) {
                 if constexpr (ADD) {
                     widen(old[which][u], f);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] = f[e] + sum[e] * a.scale;
+                    for (int e = 0; e < W; ++e) sum[e] = f[e] + sum[e] * a.scale;
                 } else
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] *= a.scale;
+                    for (int e = 0; e < W; ++e) sum[e] *= a.scale;
                 col.store(static_cast<GT *>(a.grad) + (int64_t)key * a.grad_stride, sum);
             } else if (ends || j + 1 == to) col.store(parts + (open ? 0 : a.parts_stride), sum);
             if (ends) {
                 open = false;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+                for (int e = 0; e < W; ++e) sum[e] = 0.f;
             }
         }
         return true;
@@ -651,7 +653,7 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     u.accumulate = a.accumulate;
     u.run = l.run;
     // waves of as many lanes as another, and none of a single one, which would share columns with another wave (see Columns)
-    const int64_t vectors = (a.cols + 7) / 8;
+    const int64_t width = grad_f32 ? kSumWidth<float> : kSumWidth<bf16_t>, vectors = (a.cols + width - 1) / width;
     int64_t chunks = (vectors + 63) / 64, lanes = (vectors + chunks - 1) / chunks;
     while (vectors > 1 && vectors % lanes == 1) --lanes;
     chunks = (vectors + lanes - 1) / lanes;
@@ -664,7 +666,7 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     auto of_types = [&](auto d, auto g) {
         using DT = decltype(d);
         using GT = decltype(g);
-        if (a.cols < 8) a.accumulate ? sum(embedding_sum_kernel<DT, GT, true, true>) : sum(embedding_sum_kernel<DT, GT, true, false>);
+        if (a.cols < width) a.accumulate ? sum(embedding_sum_kernel<DT, GT, true, true>) : sum(embedding_sum_kernel<DT, GT, true, false>);
         else a.accumulate ? sum(embedding_sum_kernel<DT, GT, false, true>) : sum(embedding_sum_kernel<DT, GT, false, false>);
     };
     if (dy_f32) grad_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});

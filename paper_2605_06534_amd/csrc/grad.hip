@@ -28,19 +28,21 @@ __device__ __forceinline__ int32_t tensor_at(const int64_t *offsets, int32_t n, 
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Calls f(tensor, first element, number) for every stretch of a tensor in this workgroup's pieces.
-template <class F>
+// Calls f(from, to, number) for every stretch of a tensor in this workgroup's pieces.
+template <class T, bool OUT, class F>
 __device__ __forceinline__ void for_stretches(const GradArgs &a, F f) {
     for (int64_t from = blockIdx.x * a.piece;;) {
-        // (the tensor is looked for before the end is known: one trip to memory less in front of the first element)
+        // (the tensor is looked for before the end is known, and all that is known of it is asked for together: each
+        // trip to memory in front of the first element counts)
         int32_t t = tensor_at(a.offsets, a.n_tensors, from);
         const int64_t total = a.offsets[a.n_tensors], to = from + a.piece < total ? from + a.piece : total;
-        if (from >= total) return;
         for (; t < a.n_tensors; ++t) {
             const int64_t base = a.offsets[t], end = a.offsets[t + 1];
+            const T *p = static_cast<const T *>(a.grad_ptrs[t]);
+            T *q = OUT ? static_cast<T *>(a.out_ptrs[t]) : nullptr;
             if (base >= to) break;
             const int64_t lo = from > base ? from : base, hi = to < end ? to : end;
-            if (lo < hi) f(t, lo - base, hi - lo);
+            if (lo < hi && p && (!OUT || q)) f(p + (lo - base), q + (lo - base), hi - lo);
         }
         from += gridDim.x * a.piece;
         if (from >= total) return;
@@ -96,24 +98,34 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(GradArgs a) {
     __shared__ double waves[kThreads / 64];
     double s = 0;
-    for_stretches(a, [&](int32_t t, int64_t first, int64_t n) {
-        const T *p = static_cast<const T *>(a.grad_ptrs[t]);
-        if (p) s += squares_of(p + first, n);
-    });
+    for_stretches<T, false>(a, [&](const T *p, T *, int64_t n) { s += squares_of(p, n); });
     s = sum_over(s, waves);
     if (threadIdx.x == 0) a.partials[blockIdx.x] = s;
 }
 
 // all partial sums, in one order whoever adds them
-__device__ __forceinline__ double sum_partials(const GradArgs &a, double (&waves)[kThreads / 64]) {
-    double s = 0;
-    for (int i = threadIdx.x; i < a.n_partials; i += kThreads) s += a.partials[i];
-    return sum_over(s, waves);
-}
+struct Partials {
+    double v[kWorkgroups / kThreads];
+    __device__ __forceinline__ void load(const GradArgs &a) {
+#pragma unroll
+        for (int k = 0; k < kWorkgroups / kThreads; ++k) {
+            const int i = k * kThreads + threadIdx.x;
+            v[k] = i < a.n_partials ? a.partials[i] : 0.;
+        }
+    }
+    __device__ __forceinline__ double sum(double (&waves)[kThreads / 64]) const {
+        double s = 0;
+#pragma unroll
+        for (int k = 0; k < kWorkgroups / kThreads; ++k) s += v[k];
+        return sum_over(s, waves);
+    }
+};
 
 __global__ __launch_bounds__(kThreads) void grad_sum_kernel(GradArgs a) {
     __shared__ double waves[kThreads / 64];
-    const double s = sum_partials(a, waves);
+    Partials partials;
+    partials.load(a);
+    const double s = partials.sum(waves);
     if (threadIdx.x == 0) *a.sum = s;
 }
 
@@ -155,23 +167,22 @@ __device__ __forceinline__ void scale_into(T *q, int64_t n, float factor, const 
 template <class T, bool FROM_PARTIALS>
 __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
     __shared__ double waves[kThreads / 64];
+    Partials partials;
+    if (FROM_PARTIALS) partials.load(a);
     float factor = 0.f;
     bool known = false;
     auto find_factor = [&] {
-        const float norm = (float)sqrt(FROM_PARTIALS ? sum_partials(a, waves) : *a.sum);
+        const float norm = (float)sqrt(FROM_PARTIALS ? partials.sum(waves) : *a.sum);
         if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
         const float ratio = a.max_norm / (norm + 1e-6f);
         factor = ratio >= 1.f ? 1.f : ratio;                // (a NaN stays one)
         known = true;
     };
-    for_stretches(a, [&](int32_t t, int64_t first, int64_t n) {
-        const T *p = static_cast<const T *>(a.grad_ptrs[t]);
-        T *q = static_cast<T *>(a.out_ptrs[t]);
-        const bool any = p && q;
+    for_stretches<T, true>(a, [&](const T *p, T *q, int64_t n) {
         Begun<T> begun;
-        if (any) begin(p + first, q + first, n, begun);
+        begin(p, q, n, begun);
         if (!known) find_factor();
-        if (any && !(p == q && factor == 1.f)) scale_into(q + first, n, factor, begun);
+        if (!(p == q && factor == 1.f)) scale_into(q, n, factor, begun);
     });
     if (!known) find_factor();
 }

@@ -292,13 +292,38 @@ __device__ __forceinline__ void tile_of(int n_tiles, int m_tiles, int &nt, int &
     nt = in_group / rows;
 }
 
+__device__ __forceinline__ u32x4 packed(f32x4 a, f32x4 b) {
+    return u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
+}
+// 16 bytes of a row of outputs of which `left` are in the matrix
+template <bool ONCE>
+__device__ __forceinline__ void store_some(float *p, int64_t left, const u32x4 &v) {
+    if (left >= 4) {
+        if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any *>(p));
+        else *reinterpret_cast<u32x4_any *>(p) = v;
+    } else
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < left) p[e] = __uint_as_float(v[e]);
+}
+template <bool ONCE>
+__device__ __forceinline__ void store_some(bf16_t *p, int64_t left, const u32x4 &v) {
+    if (left >= 8) {
+        if constexpr (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any *>(p));
+        else *reinterpret_cast<u32x4_any *>(p) = v;
+    } else
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) p[e].bits = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+}
+
 template <class OT, int BN, int BM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArgs a, int nb, int n_tiles, int m_tiles) {
     constexpr int kThr = 64 * WN * WM, FN = BN / WN / 16, FM = BM / WM / 16, kRows = BN + BM;
     constexpr int kPer = kThr / 8;                      // rows that one load of all threads takes
     constexpr int kLoadsW = BN / kPer, kLoads = kRows / kPer;
     constexpr uint32_t kSlot = kRows * 128, kScaleSlot = kRows * 16;
-    static_assert(BN % kPer == 0 && BM % kPer == 0 && kPer % 16 == 0 && FN % 2 == 0 && kRows == kThr, "a row of scales a thread");
+    static_assert(BN % kPer == 0 && BM % kPer == 0 && kPer % 16 == 0 && FN % 4 == 0 && kRows == kThr, "a row of scales a thread");
     __shared__ __attribute__((aligned(1024))) uint8_t codes[2][kSlot];
     __shared__ __attribute__((aligned(16))) u32x4 scales[2][kRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), of16 = lane & 15, quarter = lane >> 4;
@@ -404,22 +429,36 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
     } while (d < slots);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // (loads may still be on their way to LDS)
 
+    // A lane has eight neighbouring outputs of fragments 2p and 2p + 1.  Lanes l and l + 8 of sixteen change halves of what they
+    // have, so that eight lanes write a whole line of 128 bytes: first of row l, then of row l + 8.
+    const bool upper = of16 & 8;
+    auto write = [&](int64_t row, int64_t col, const u32x4 &lower_half, const u32x4 &upper_half, int between) {
+        u32x4 mine[2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = lower_half[e], hi = upper_half[e];
+            const uint32_t other = __builtin_amdgcn_mov_dpp((int)(upper ? lo : hi), 0x128, 0xF, 0xF, true);      // lane ^ 8
+            mine[0][e] = upper ? other : lo;
+            mine[1][e] = upper ? hi : other;
+        }
+        const int64_t at = col + (upper ? between : 0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t r = row + (of16 & 7) + h * 8;
+            if (r < a.m) store_some<true>(static_cast<OT *>(a.out) + r * a.out_stride + at, a.n - at, mine[h]);
+        }
+    };
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
-        const int64_t row = m0 + wm * (FM * 16) + j * 16 + of16;
-        if (row >= a.m) continue;
+        const int64_t row = m0 + wm * (FM * 16) + j * 16;
 #pragma unroll
-        for (int i = 0; i < FN; i += 2) {
+        for (int i = 0; i < FN; i += 4) {
             const int64_t col = n0 + wn * (FN * 16) + i * 16 + quarter * 8;
-            OT *q = static_cast<OT *>(a.out) + row * a.out_stride + col;
-            float f[8];
+            if constexpr (sizeof(OT) == 4) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f[e] = sum[i][j][e];
-                f[e + 4] = sum[i + 1][j][e];
-            }
-            if (col + 8 <= a.n) store(q, f);
-            else if (col < a.n) store(q, (int)(a.n - col), f);
+                for (int p = 0; p < 4; p += 2)
+                    write(row, col + p * 16, __builtin_bit_cast(u32x4, sum[i + p][j]), __builtin_bit_cast(u32x4, sum[i + p + 1][j]), 4);
+            } else write(row, col, packed(sum[i][j], sum[i + 1][j]), packed(sum[i + 2][j], sum[i + 3][j]), 32);
         }
     }
 }
