@@ -377,13 +377,14 @@ __device__ __forceinline__ void fill_unnamed(const SumArgs &a, uint32_t group) {
 // A block of sorted tokens and 16 bytes of the gradient a lane, one wave a workgroup.  A row whose tokens all lie in the block is
 // finished here; what crosses the block's ends is left for the join.  Rows come kAhead at a time, the next ones asked for before
 // the last are added, and with them (ADD) what is in the gradient of the rows that end among them: a load where a run ends would
-// wait for all that were asked for before it, stores included.  (ADD: half as many, eight take registers that waves could use.  Four columns of an fp32 gradient a
-// lane: neighbouring lanes read and write neighbouring vectors.  65536 tokens of 5120 columns, dy fp32 346 us; eight columns a lane 386.)
+// wait for all that were asked for before it, stores included.  (ADD: two rows of fp32 or four of bf16, twice as many take
+// registers that waves could use: 65536 tokens of 5120 columns of bf16 into fp32 252 us, 261 with four.)  Neighbouring lanes
+// read and write neighbouring vectors of the gradient (eight fp32 columns a lane: 386 us from fp32, 349 with four).
 template <class GT> constexpr int kSumWidth = 16 / sizeof(GT);
 template <class DT, class GT, bool NARROW, bool ADD>
 __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
     constexpr int W = kSumWidth<GT>;
-    constexpr int kAhead = ADD ? 4 : 8;
+    constexpr int kAhead = ADD ? W / 2 : 8;
     constexpr int kWindow = 32;
     // Workgroups i, i + 8, ... run on one XCD; all columns of a block go to one.  (With each column of waves on an XCD of its own,
     // as where there are eight of them, an XCD reads the same kilobyte of every row: a quarter of its L2's channels.)
@@ -552,10 +553,11 @@ GradLayout grad_layout(int64_t rows, int64_t cols, int64_t n) {
         l.tiles = (int32_t)((n + (int64_t)l.subtiles * kTile - 1) / ((int64_t)l.subtiles * kTile));
         l.counts = take((size_t)4 * l.tiles * kBins * 4);
     }
-    // blocks as short as fill the chip, but no shorter: each leaves parts of two runs to be joined
+    // blocks as short as fill the chip, but no shorter: each leaves parts of two runs to be joined (65536 tokens of 5120
+    // columns: blocks of 256 tokens 296 us, of 128 264, of 64 261, of 32 275)
     const int64_t waves = (cols + 511) / 512;
     l.run = kShortestRun;
-    while (l.run * 8192 < n * waves && l.run < 4096) l.run *= 2;
+    while (l.run * 16384 < n * waves && l.run < 4096) l.run *= 2;
     l.blocks = (n + l.run - 1) / l.run;
     l.parts_stride = (cols + 7) / 8 * 8;
     l.parts = take(l.blocks > 1 ? (size_t)l.blocks * 2 * (size_t)l.parts_stride * 4 : 0);
