@@ -469,11 +469,11 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
 
 // A run that crosses the end of the block it begins in: the sums of its parts.  Four columns a lane; where there are few
 // parts each of the four waves adds those of its own 256 columns, where there are many the waves take every fourth part and
-// their sums are added in order, 256 columns after the other.
+// their sums are added in order.
 // The workgroups behind these write zeros to rows that no token names.
 template <class GT>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, uint32_t chunks) {
-    __shared__ f32x4 sums[4][64];
+    __shared__ f32x4 sums[4][4][64];                    // [columns][wave][lane]
     if (blockIdx.x >= a.join_groups) {
         fill_unnamed<GT>(a, (blockIdx.x - a.join_groups) * 4 + (threadIdx.x >> 6));
         return;
@@ -491,12 +491,22 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, uint32_t
         last += ~with ? __builtin_ctzll(~with) : 64;
         if (~with) break;
     }
+    // (eight parts on the way whatever is left, not one after the other where fewer are)
     auto add = [&](int64_t col, int64_t first, int64_t hop) {
+        constexpr int kParts = 8;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         const float *parts = a.parts + col;
-#pragma unroll 4
-        for (int64_t b = block + first; b <= last; b += hop)
-            sum += *reinterpret_cast<const f32x4 *>(parts + (2 * b + (b == block ? 1 : 0)) * a.parts_stride);
+        for (int64_t b = block + first; b <= last; b += kParts * hop) {
+            f32x4 v[kParts];
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) {
+                const int64_t p = b + k * hop <= last ? b + k * hop : b;
+                v[k] = *reinterpret_cast<const f32x4 *>(parts + (2 * p + (p == block ? 1 : 0)) * a.parts_stride);
+            }
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+                if (b + k * hop <= last) sum += v[k];
+        }
         return sum;
     };
     auto write = [&](int64_t col, f32x4 sum) {
@@ -511,13 +521,13 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, uint32_t
         if (col < a.cols) write(col, add(col, 0, 1));
         return;
     }
-    for (int64_t c = first_col; c < first_col + 1024 && c < a.cols; c += 256) {
-        const int64_t col = c + lane * 4;
-        if (col < a.cols) sums[wave][lane] = add(col, wave, 4);
-        __syncthreads();
-        if (wave == 0 && col < a.cols) write(col, ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane]);
-        __syncthreads();
+    for (int c = 0; c < 4; ++c) {
+        const int64_t col = first_col + c * 256 + lane * 4;
+        if (col < a.cols) sums[c][wave][lane] = add(col, wave, 4);
     }
+    __syncthreads();
+    const int64_t col = first_col + wave * 256 + lane * 4;
+    if (col < a.cols) write(col, ((sums[wave][0][lane] + sums[wave][1][lane]) + sums[wave][2][lane]) + sums[wave][3][lane]);
 }
 
 // where things lie in the workspace
