@@ -681,13 +681,20 @@ template <int MT, int NT, bool BF16>
 static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     const int64_t groups = (a.n + NT * 16 - 1) / (NT * 16), steps = (blocks_of(a.k) + 7) / 8;
     const size_t wave_lds = (few_lds<MT, NT, BF16>(a.m) + 127) / 128 * 128;
-    // as many waves as make about eight for every CU together, with as many steps each as another, and their rings in 72 KB
-    int64_t waves = (2048 + groups - 1) / groups;
-    const int64_t fit = (int64_t)((72 << 10) / wave_lds);
-    waves = waves > 8 ? 8 : waves;
-    waves = waves > fit ? fit : waves;
-    const int64_t each = steps > waves ? (steps + waves - 1) / waves : 1;
-    waves = steps > 0 ? (steps + each - 1) / each : 1;
+    // As many waves as make about eight for every CU together, with as many steps each as another, and their rings in 79 KB of
+    // LDS, half a CU's.  Nearly all of it where the workgroups are at most one a CU and a wave would have more than a chunk
+    // and a half of steps: 64 x 8192 x 5120 13.9 us, 11.0 so; with fewer steps the next launch waits for the LDS and it costs
+    // more than it gives (17 x 4096 x 4096 4.0 us, 5.7 so).
+    int64_t waves = 1, each = 1;
+    auto divide = [&](int64_t lds) {
+        const int64_t fit = lds / (int64_t)wave_lds, most = (2048 + groups - 1) / groups;
+        waves = most < fit ? most : fit;
+        waves = waves > 8 ? 8 : waves;
+        each = steps > waves ? (steps + waves - 1) / waves : 1;
+        waves = steps > 0 ? (steps + each - 1) / each : 1;
+    };
+    divide(79 << 10);
+    if (groups <= 256 && each > kChunk * 3 / 2) divide(148 << 10);
     const dim3 grid((unsigned)groups), block((unsigned)(64 * waves));
     if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
     else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
@@ -707,9 +714,9 @@ static int launch_tiles(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.m == 0 || a.n == 0) return 0;
-    // (every workgroup reads all activations: with many of them and of their rows 32 rows of the weights share a reading;
-    // 64 x 19008 x 5120: 17.8 us against 32.5, 47 x 4099 x 4096: 10.2 against 6.8)
-    const bool wide = a.n >= 8192;
+    // (every workgroup reads all activations: where groups of 16 rows of the weights are one and a half for every CU, 32 rows
+    // share a reading; 64 x 19008 x 5120: 17.8 us against 32.5, 32 x 6912 x 5120 5.7 against 7.6, 47 x 4099 x 4096 7.0 against 6.5)
+    const bool wide = a.n >= 6144;
     if (a.m <= 16) return a.x ? launch_few<1, 1, true>(a, out_f32, st) : launch_few<1, 1, false>(a, out_f32, st);
     if (a.m <= 32) return wide ? launch_few<2, 2, false>(a, out_f32, st) : launch_few<2, 1, false>(a, out_f32, st);
     if (a.m <= 64) return wide ? launch_few<4, 2, false>(a, out_f32, st) : launch_few<4, 1, false>(a, out_f32, st);
