@@ -465,7 +465,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 
 // ---- products of few rows: the weights go by once ----
 //
-// A workgroup takes NT * 16 rows of the weights and all of the activations (MT * 16 rows at most); its waves divide the
+// A workgroup takes NT * 16 rows of the weights and MT * 16 of the activations, all of them as a rule; its waves divide the
 // columns among them and their sums are added up through LDS in their order.  The weights are read once, so all there is to do is
 // to keep enough of them on the way: each wave has a ring of its own in LDS that loads fill (as above) and that it alone
 // reads, without barriers.  (Loads straight to registers, each lane its row's: 64 lines an instruction where eight lanes of
@@ -492,13 +492,13 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4ProductArgs a, int nb, 
     constexpr uint32_t kStep = kTiles * 2048;
     const int lane = threadIdx.x & 63, of16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int64_t n0 = (int64_t)blockIdx.x * (NT * 16), row_bytes = (int64_t)nb * 16;
-    const int steps = (nb + 7) / 8, m = (int)a.m;
+    const int64_t n0 = (int64_t)blockIdx.x * (NT * 16), m0 = (int64_t)blockIdx.y * (MT * 16), row_bytes = (int64_t)nb * 16;
+    const int steps = (nb + 7) / 8, m = (int)a.m;       // (BF16: all of them)
     const uint32_t ring = lds_address(lds) + wave * wave_lds, w_scales = ring + kRing * kStep, x_scales = w_scales + NT * 16 * kScaleRow;
     const uint32_t x_codes = x_scales + m * kScaleRow;         // BF16 only
     // rows behind the last give zeros
     const u32x4 w_res = resource_of(a.w_codes + n0 * row_bytes, (a.n - n0) * row_bytes);
-    const u32x4 x_res = BF16 ? w_res : resource_of(a.a_codes, a.m * row_bytes);
+    const u32x4 x_res = BF16 ? w_res : resource_of(a.a_codes + m0 * row_bytes, (a.m - m0) * row_bytes);
     const int part = (lane & 7) ^ (lane >> 3);
     const uint32_t off = (uint32_t)(lane >> 3) * (uint32_t)row_bytes + part * 16;
     auto ask = [&](int step, int slot) {
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4ProductArgs a, int nb, 
         if constexpr (!BF16) {
 #pragma unroll
             for (int t = 0; t < MT * 16; t += 32) {
-                const int64_t row = t + s_row < a.m ? t + s_row : a.m - 1;
+                const int64_t row = m0 + t + s_row < a.m ? m0 + t + s_row : a.m - 1;
                 if (t + s_row < MT * 16) put_lds(x_scales + (t + s_row) * kScaleRow + (lane & 1) * 16, turned(scales_at(a.a_scales + row * nb, s_from, nb)));
             }
         } else {
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4ProductArgs a, int nb, 
             s = from_lds<f32x4>(at);
             for (int v = 1; v < waves; ++v) s += from_lds<f32x4>(at + v * wave_lds);
         }
-        const int64_t row = (t % MT) * 16 + of16, col = n0 + (t / MT) * 16 + quarter * 4;
+        const int64_t row = m0 + (t % MT) * 16 + of16, col = n0 + (t / MT) * 16 + quarter * 4;
         if (row >= a.m) continue;
         OT *q = static_cast<OT *>(a.out) + row * a.out_stride + col;
         if (col + 4 > a.n) {
@@ -679,7 +679,8 @@ bool mx4_product_takes_bf16(int64_t m) { return m <= kBf16Rows; }
 
 template <int MT, int NT, bool BF16>
 static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
-    const int64_t groups = (a.n + NT * 16 - 1) / (NT * 16), steps = (blocks_of(a.k) + 7) / 8;
+    const int64_t n_groups = (a.n + NT * 16 - 1) / (NT * 16), m_groups = (a.m + MT * 16 - 1) / (MT * 16), groups = n_groups * m_groups;
+    const int64_t steps = (blocks_of(a.k) + 7) / 8;
     const size_t wave_lds = (few_lds<MT, NT, BF16>(a.m) + 127) / 128 * 128;
     // As many waves as make about eight for every CU together, with as many steps each as another, and their rings in 79 KB of
     // LDS, half a CU's.  Nearly all of it where the workgroups are at most one a CU and a wave would have more than a chunk
@@ -695,7 +696,7 @@ static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     };
     divide(79 << 10);
     if (groups <= 256 && each > kChunk * 3 / 2) divide(148 << 10);
-    const dim3 grid((unsigned)groups), block((unsigned)(64 * waves));
+    const dim3 grid((unsigned)n_groups, (unsigned)m_groups), block((unsigned)(64 * waves));
     if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
     else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
     return (int)hipGetLastError();
@@ -720,10 +721,16 @@ int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     if (a.m <= 16) return a.x ? launch_few<1, 1, true>(a, out_f32, st) : launch_few<1, 1, false>(a, out_f32, st);
     if (a.m <= 32) return wide ? launch_few<2, 2, false>(a, out_f32, st) : launch_few<2, 1, false>(a, out_f32, st);
     if (a.m <= 64) return wide ? launch_few<4, 2, false>(a, out_f32, st) : launch_few<4, 1, false>(a, out_f32, st);
+    // More rows the same way where that is at most a workgroup a CU, and the sums are long: waves divide them, which tiles do
+    // not (128 x 4096 x 14336 18.4 us, 31.8 in tiles of 64; 512 x 1024 x 5120 9.5 and 12.4; but 128 x 1024 x 1024 4.5 and 4.0).
+    const int64_t across = (a.n + 31) / 32 * ((a.m + 63) / 64);
+    if (across <= 256 && a.k > 2048) return launch_few<4, 2, false>(a, out_f32, st);
     // 256 x 256 tiles move half of what 128 x 128 ones do but fill a CU each; the smaller ones, two a CU, where there are few
-    // (256 x 19008 x 5120: 38.5 us with the large ones, 28.8 with the small; 4096 x 4096 x 4096: 39.8 and 48.7).
-    const int64_t large = ((a.n + 255) / 256) * ((a.m + 255) / 256);
-    return large >= 192 ? launch_tiles<256, 256, 4, 2>(a, out_f32, st) : launch_tiles<128, 128, 2, 2>(a, out_f32, st);
+    // (256 x 19008 x 5120: 38.5 us with the large ones, 26.6 with the small; 4096 x 4096 x 4096: 38.5 and 48.7), and tiles of 64
+    // where also those leave CUs idle (256 x 6912 x 5120 20.0 us, 15.4 with 64; 512 x 6912 x 5120 20.8 and 21.0).
+    auto tiles = [&](int64_t b) { return ((a.n + b - 1) / b) * ((a.m + b - 1) / b); };
+    if (tiles(256) >= 192) return launch_tiles<256, 256, 4, 2>(a, out_f32, st);
+    return tiles(128) >= 192 ? launch_tiles<128, 128, 2, 2>(a, out_f32, st) : launch_tiles<64, 64, 1, 2>(a, out_f32, st);
 }
 
 }  // namespace rose

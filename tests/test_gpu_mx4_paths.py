@@ -1,0 +1,47 @@
+"""Products of 4-bit matrices at the sizes between few rows and many: tiles of 64, and groups of rows whose sums are
+divided among waves.  Against the products of the values in 64 bits; bounds as k additions that lose a unit in the last
+place each, and the rounding to the result's type."""
+import pytest
+import torch
+
+import paper_2605_06534_amd as R
+
+pytestmark = pytest.mark.gpu
+
+
+def rounded_matrix(rows, cols, seed, std=1.0):
+    x = torch.randn(rows, cols, generator=torch.Generator("cuda").manual_seed(seed), device="cuda") * std
+    q, values = R.Mx4(rows, cols), torch.empty(rows, cols, device="cuda")
+    R.mx4_quantize(x, q)
+    R.mx4_dequantize(q, values)
+    return x, q, values.double()
+
+
+@pytest.mark.parametrize("k", [31, 544, 2080, 5121])
+@pytest.mark.parametrize("m,n", [(65, 70), (100, 1003), (129, 4100), (640, 130), (333, 2500), (1500, 1500), (3000, 20)])
+def test_products_between_few_rows_and_many(m, n, k):
+    print("case: product", m, n, k, flush=True)
+    x, qa, a = rounded_matrix(m, k, 71)
+    _, qw, w = rounded_matrix(n, k, 72, 0.05)
+    want, size = a @ w.t().contiguous(), a.abs() @ w.abs().t().contiguous()
+    for dtype, pad in ((torch.float32, 0), (torch.bfloat16, 3)):
+        half = torch.finfo(dtype).eps / 2
+        bound = k * 2.0 ** -23 * size * (1 + half) + want.abs() * half + 2.0 ** -134
+        out = torch.full((m, n + pad), 7.0, dtype=dtype, device="cuda")
+        R.mx4_matmul(qa, qw, out[:, :n])
+        assert ((out[:, :n].double() - want).abs() <= bound).all() and (out[:, n:] == 7).all()
+        again = torch.empty(m, n, dtype=dtype, device="cuda")
+        R.mx4_linear(x, qw, again, R.mx4_linear_workspace(m, n, k))
+        assert torch.equal(again, out[:, :n])                     # the same bits, also from values that are rounded on the way
+
+
+def test_a_row_that_is_no_number_stays_alone():
+    print("case: product with NaN in groups of rows", flush=True)
+    m, n, k = 200, 300, 4096
+    x, _, _ = rounded_matrix(m, k, 73)
+    _, qw, _ = rounded_matrix(n, k, 74)
+    x[77, 4000] = float("nan")
+    out = torch.empty(m, n, device="cuda")
+    R.mx4_linear(x, qw, out, R.mx4_linear_workspace(m, n, k))
+    bad = torch.isnan(out)
+    assert bad[77].all() and bad.sum().item() == n
