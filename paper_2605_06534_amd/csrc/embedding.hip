@@ -336,7 +336,7 @@ struct SumArgs {
     float *parts;                               // [block][2][parts_stride]: sums of runs that begin before the block, behind it
     int64_t parts_stride, run;                  // run: tokens of a block
     int64_t fill_rows;                          // the rows below this one that no token names become zero here
-    uint32_t join_groups;                       // workgroups that join
+    uint32_t sum_groups;                        // workgroups that sum; those behind them write zeros
     uint32_t chunks;                            // a row's columns go to this many waves ...
     int32_t lanes;                              // ... of so many lanes
     float scale;
@@ -386,6 +386,10 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
     constexpr int W = kSumWidth<GT>;
     constexpr int kAhead = ADD ? W / 2 : 8;
     constexpr int kWindow = 32;
+    if (!ADD && blockIdx.x >= a.sum_groups) {
+        fill_unnamed<GT>(a, blockIdx.x - a.sum_groups);
+        return;
+    }
     // Workgroups i, i + 8, ... run on one XCD; all columns of a block go to one.  (With each column of waves on an XCD of its own,
     // as where there are eight of them, an XCD reads the same kilobyte of every row: a quarter of its L2's channels.)
     const uint32_t turn = blockIdx.x >> 3, chunk = turn % a.chunks;
@@ -470,14 +474,9 @@ __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {
 // A run that crosses the end of the block it begins in: the sums of its parts.  Four columns a lane; where there are few
 // parts each of the four waves adds those of its own 256 columns, where there are many the waves take every fourth part and
 // their sums are added in order.
-// The workgroups behind these write zeros to rows that no token names.
 template <class GT>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a, uint32_t chunks) {
     __shared__ f32x4 sums[4][4][64];                    // [columns][wave][lane]
-    if (blockIdx.x >= a.join_groups) {
-        fill_unnamed<GT>(a, (blockIdx.x - a.join_groups) * 4 + (threadIdx.x >> 6));
-        return;
-    }
     const uint32_t block = blockIdx.x / chunks, chunk = blockIdx.x - block * chunks;
     const int64_t from = (int64_t)block * a.run, next = from + a.run;
     const uint32_t key = a.keys[next], in_front = a.keys[next - 1], before = from > 0 ? a.keys[from - 1] : 0xFFFFFFFFu;
@@ -619,8 +618,8 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     s.tiles = l.tiles;
     s.subtiles = l.subtiles;
     // Zeros for rows without tokens: as much as the sort takes the time of goes blindly with it (the last rows, of which tokens
-    // name the fewest), the rest behind the sums, past the rows that have some.  (All of it with the sort: 8191 tokens and a gradient of
-    // 524 MB 133 us, 127 this way.)
+    // name the fewest), the rest in the launch of the sums, past the rows that have some.  (All of it with the sort: 8191 tokens
+    // and a gradient of 524 MB 133 us, 114 this way.)
     int64_t fills = 0, fill_later = 0;
     if (!a.accumulate) {
         const int64_t size = grad_f32 ? 4 : 2, row_bytes = a.cols * size;
@@ -672,8 +671,10 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     const int64_t join_chunks = (a.cols + 1023) / 1024;
     u.lanes = (int32_t)lanes;
     u.chunks = (uint32_t)chunks;
-    const int64_t grid = (l.blocks + 7) / 8 * 8 * chunks;
+    const int64_t sums = (l.blocks + 7) / 8 * 8 * chunks, grid = sums + (fill_later + kFillRows - 1) / kFillRows;
     if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    u.fill_rows = fill_later;
+    u.sum_groups = (uint32_t)sums;
     auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64), 0, st, u); };
     auto of_types = [&](auto d, auto g) {
         using DT = decltype(d);
@@ -683,12 +684,10 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     };
     if (dy_f32) grad_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
     else grad_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
-    const int64_t joins = (l.blocks - 1) * join_chunks, all = joins + (fill_later + 4 * kFillRows - 1) / (4 * kFillRows);
-    if (all > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    u.fill_rows = fill_later;
-    u.join_groups = (uint32_t)joins;
-    if (all > 0) {
-        auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)all), dim3(256), 0, st, u, (uint32_t)join_chunks); };
+    const int64_t joins = (l.blocks - 1) * join_chunks;
+    if (joins > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    if (joins > 0) {
+        auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)joins), dim3(256), 0, st, u, (uint32_t)join_chunks); };
         grad_f32 ? join(embedding_join_kernel<float>) : join(embedding_join_kernel<bf16_t>);
     }
     return (int)hipGetLastError();
