@@ -124,7 +124,7 @@ def _check(status, what):
 def _stream(stream):
     if stream is None:
         # (the current stream's handle itself: torch.cuda.current_stream() makes an object for it first, 3 us a call)
-        return _vp(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return _vp(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -387,6 +387,7 @@ def object_check(plan, obj, stream=None, with_payload=False):
 # operators at the two ends of a synchronisation
 # ---------------------------------------------------------------------------------------------------
 _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
 def _dtype(dtype, what):
@@ -398,17 +399,22 @@ def _dtype(dtype, what):
 
 def _matrix(t, what):
     """-> (pointer, type, rows, columns, stride) of a matrix on the GPU whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda or (t.size(1) > 1 and t.stride(1) != 1):
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise RoseError(ERR_SHAPE, "%s: a matrix on the GPU with contiguous rows is wanted" % what)
-    rows, cols = t.shape
-    return t.data_ptr(), _dtype(t.dtype, what), rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    rows, cols = shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        raise RoseError(ERR_SHAPE, "%s: a matrix on the GPU with contiguous rows is wanted" % what)
+    return t.data_ptr(), _dtype(t.dtype, what), rows, cols, stride if rows > 1 or stride > cols else cols
 
 
 def _tokens(t, what):
     """-> (pointer, bytes of an id, how many)"""
-    if t.dim() != 1 or not t.is_cuda or not t.is_contiguous() or t.dtype not in (torch.int32, torch.int64):
+    size = _ID_BYTES.get(t.dtype)
+    if size is None or t.dim() != 1 or not t.is_cuda or not t.is_contiguous():
         raise RoseError(ERR_SHAPE, "%s: a contiguous list of int32 or int64 ids on the GPU is wanted" % what)
-    return t.data_ptr(), t.element_size(), t.numel()
+    return t.data_ptr(), size, len(t)
 
 
 def _same(ok, what):
