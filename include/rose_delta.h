@@ -485,7 +485,8 @@ rose_status rose_bw_probe_lines(void *dst, size_t bytes, uint32_t touched_per_2_
  * see are returned before anything is queued.  Sizes of zero are allowed where nothing is then read.
  * Matrices are row-major with rows `stride` elements apart (stride >= columns; what lies between is
  * neither read nor written); pointers need the alignment of their element type only, unless stated.
- * Every result is a function of the inputs alone: two calls give the same bits.
+ * Every result is a function of the inputs alone: two calls give the same bits.  (Of the norm of gradients the 64-bit
+ * sum's last bits also depend on how the tensors lie to lines of 128 bytes.)
  * ---------------------------------------------------------------------------------------------
  */
 typedef enum {
@@ -537,7 +538,8 @@ rose_status rose_embedding_grad(const void *dy, int32_t dy_dtype, int64_t dy_str
  *                         grad_ptrs, and where they do and nothing is to be scaled nothing is moved.  A norm that is
  *                         infinite or NaN goes through the same formula (finite gradients become 0 or NaN): a program
  *                         that skips such steps reads *norm.  *norm (device, 4-byte aligned, may be NULL) gets the norm.
- * rose_grad_clip_norm     both, for one rank that holds everything: one launch less, the same bits.
+ * rose_grad_clip_norm     both in one call, for one rank that holds everything: the same bits, and a launch less where
+ *                         the gradients are small.
  * ROSE_ERR_ARG for null pointers, negative sizes, an unknown type, a max_norm that is negative or NaN, a workspace
  * that is too small; ROSE_ERR_ALIGN for unaligned tables, sums or workspaces.
  */

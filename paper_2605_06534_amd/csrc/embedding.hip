@@ -27,7 +27,9 @@ __device__ __forceinline__ uint32_t row_of(const Tokens &t, int64_t i) {
 // -------------------------------------------------------------------------------------------------
 // lookup
 // -------------------------------------------------------------------------------------------------
-// R vectors of 16 bytes of the output a lane.  It asks for its tokens, then for their rows, before it uses the first.
+// R vectors of 16 bytes of the output a lane.  It asks for its tokens, then for their rows, before it uses the first.  HBM traffic
+// bounds it: 16384 tokens of 5120 columns, 950 of them in the shard, into bf16 25 us, 7.4 TB/s; into fp32 55 us.  (Outputs that
+// the caches keep: 42 us; four vectors a lane 29; one 25, and 210 instead of 187 for 65536 tokens that are all in the shard.)
 template <class OT> constexpr int kLookupWidth = 16 / sizeof(OT);
 template <class TT, class OT, int R, bool NARROW>
 __global__ __launch_bounds__(kLookupThreads) void embedding_lookup_kernel(LookupArgs a, Rows rows) {
@@ -380,6 +382,8 @@ __device__ __forceinline__ void fill_unnamed(const SumArgs &a, uint32_t group) {
 // wait for all that were asked for before it, stores included.  (ADD: two rows of fp32 or four of bf16, twice as many take
 // registers that waves could use: 65536 tokens of 5120 columns of bf16 into fp32 252 us, 261 with four.)  Neighbouring lanes
 // read and write neighbouring vectors of the gradient (eight fp32 columns a lane: 386 us from fp32, 349 with four).
+// What bounds it: rows of dy and of the gradient in no order, 960 MB in 194 us there; not added to, 8191 tokens of 4096 columns, with
+// the zeros of 396 MB 85 us.
 template <class GT> constexpr int kSumWidth = 16 / sizeof(GT);
 template <class DT, class GT, bool NARROW, bool ADD>
 __global__ __launch_bounds__(64) void embedding_sum_kernel(SumArgs a) {

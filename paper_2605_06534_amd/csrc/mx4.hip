@@ -22,7 +22,8 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
 __device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_float(scale ? scale << 23 : 0x00400000u); }
 
 // -------------------------------------------------------------------------------------------------
-// quantisation: four lanes a block of bf16, eight of fp32, 16 bytes each, kUnits times so many a lane
+// quantisation: four lanes a block of bf16, eight of fp32, 16 bytes each, kUnits times so many a lane.  HBM traffic bounds it
+// and its inverse: 151936 x 4096 bf16 247 us and 243, 6.4 TB/s (fp32 6.3 and 5.9); 6912 x 5120 17 us and 14
 // -------------------------------------------------------------------------------------------------
 constexpr int kUnits = 2;
 
@@ -203,9 +204,11 @@ __device__ __forceinline__ f32x4 product(u32x4 w, uint32_t w_scale, u32x4 a, uin
 // lanes read together lie in eight different groups of LDS banks.
 // Scales go through registers: sixteen of a row (two slots) a thread, turned around so that a lane finds the four that it
 // needs for its quarter of four instructions in one word, of which the instruction picks a byte.
-// 16384 x 6912 x 5120: 380 us, 3050 TFLOP/s (the simplest kernel: 7480 us); 4096 x 4096 x 4096: 40 us, 3460.  What bounds
-// it: without the loads from memory the same loop takes 310 us, without the multiplications 260, and 50 of either are
-// the stores, which nothing overlaps where one workgroup fills a CU.
+// 16384 x 6912 x 5120: 305 us, 3800 TFLOP/s (the simplest kernel: 7480 us; outputs written in half lines that caches keep 342);
+// 4096 x 4096 x 4096: 38 us, 3600.  What bounds it: either the loads from memory or the multiplications alone take three
+// quarters of that, and 7 us of each round of 256 tiles are outputs that leave and first slots that come, which nothing overlaps
+// where one workgroup fills a CU.  (Workgroups that take tile after tile and ask for the next one's first slots before they
+// write need more registers than there are: 380 us.)
 constexpr uint32_t kOutside = 0xFFFFF000u;      // an offset behind every resource: such loads give zeros
 
 __device__ __forceinline__ u32x4 resource_of(const uint8_t *p, int64_t bytes) {
@@ -471,6 +474,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 // reads, without barriers.  (Loads straight to registers, each lane its row's: 64 lines an instruction where eight lanes of
 // a row next to each other make 8; 6912 x 5120 took 10.1 us that way.)
 // With BF16 the wave quantises the activations that it needs by itself, a chunk of columns ahead of the multiplications.
+// 1 x 6912 x 5120: 6.0 us, of which 2.6 are the least launch; 1 x 151936 x 4096 61 us, 5.4 TB/s.
 typedef uint64_t __attribute__((aligned(2))) u64_any2;
 
 constexpr int kRing = 3;                        // steps of 256 columns on the way
