@@ -641,6 +641,13 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(Mx4ProductArgs a, int nb, 
     }
 }
 
+// sums of nothing (the kernels above take a row of one block at least)
+template <class OT>
+__global__ __launch_bounds__(kThreads) void mx4_zeros_kernel(Mx4ProductArgs a) {
+    for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x)
+        for (int64_t col = threadIdx.x; col < a.n; col += kThreads) static_cast<OT *>(a.out)[row * a.out_stride + col] = from_f32<OT>(0.f);
+}
+
 int64_t blocks_of(int64_t cols) { return (cols + ROSE_MX4_BLOCK - 1) / ROSE_MX4_BLOCK; }
 
 }  // namespace
@@ -696,7 +703,7 @@ static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
         waves = most < fit ? most : fit;
         waves = waves > 8 ? 8 : waves;
         each = steps > waves ? (steps + waves - 1) / waves : 1;
-        waves = steps > 0 ? (steps + each - 1) / each : 1;
+        waves = (steps + each - 1) / each;
     };
     divide(79 << 10);
     if (groups <= 256 && each > kChunk * 3 / 2) divide(148 << 10);
@@ -719,6 +726,12 @@ static int launch_tiles(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.m == 0 || a.n == 0) return 0;
+    if (a.k == 0) {
+        const dim3 grid((unsigned)(a.m < 65536 ? a.m : 65536));
+        if (out_f32) hipLaunchKernelGGL(mx4_zeros_kernel<float>, grid, dim3(kThreads), 0, st, a);
+        else hipLaunchKernelGGL(mx4_zeros_kernel<bf16_t>, grid, dim3(kThreads), 0, st, a);
+        return (int)hipGetLastError();
+    }
     // (every workgroup reads all activations: where groups of 16 rows of the weights are one and a half for every CU, 32 rows
     // share a reading; 64 x 19008 x 5120: 17.8 us against 32.5, 32 x 6912 x 5120 5.7 against 7.6, 47 x 4099 x 4096 7.0 against 6.5)
     const bool wide = a.n >= 6144;

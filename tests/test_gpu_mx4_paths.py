@@ -45,3 +45,16 @@ def test_a_row_that_is_no_number_stays_alone():
     R.mx4_linear(x, qw, out, R.mx4_linear_workspace(m, n, k))
     bad = torch.isnan(out)
     assert bad[77].all() and bad.sum().item() == n
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("m,n", [(1, 1), (5, 300), (65, 70), (400, 400), (70000, 3), (4000, 4000)])
+def test_sums_of_nothing(m, n, dtype):
+    """No columns: zeros, whichever way a product of that many rows would go."""
+    print("case: product without columns", m, n, dtype, flush=True)
+    out = torch.full((m, n + 1), 9.0, dtype=dtype, device="cuda")
+    R.mx4_matmul(R.Mx4(m, 0), R.Mx4(n, 0), out[:, :n])
+    assert (out[:, :n] == 0).all() and (out[:, n:] == 9).all()
+    out.fill_(9.0)
+    R.mx4_linear(torch.empty(m, 0, dtype=torch.bfloat16, device="cuda"), R.Mx4(n, 0), out[:, :n], R.mx4_linear_workspace(m, n, 0))
+    assert (out[:, :n] == 0).all() and (out[:, n:] == 9).all()
