@@ -58,3 +58,37 @@ def test_sums_of_nothing(m, n, dtype):
     out.fill_(9.0)
     R.mx4_linear(torch.empty(m, 0, dtype=torch.bfloat16, device="cuda"), R.Mx4(n, 0), out[:, :n], R.mx4_linear_workspace(m, n, 0))
     assert (out[:, :n] == 0).all() and (out[:, n:] == 9).all()
+
+
+@pytest.mark.parametrize("shifted", [False, True], ids=["aligned", "scales_anywhere"])
+@pytest.mark.parametrize("k", [1024, 2048, 5120])
+@pytest.mark.parametrize("m,n", [(66, 9000), (200, 1500), (1000, 1003), (1600, 2100), (129, 26000)])
+def test_whole_groups_of_scales(m, n, k, shifted):
+    """Columns in whole groups of 32 blocks, whose scales may go another way; also where their rows begin at odd addresses."""
+    print("case: product of whole groups", m, n, k, shifted, flush=True)
+
+    def matrix(rows, seed, std):
+        x = torch.randn(rows, k, generator=torch.Generator("cuda").manual_seed(seed), device="cuda") * std
+        x *= torch.exp2(torch.randint(-6, 6, (rows, k // 32, 1), generator=torch.Generator("cuda").manual_seed(seed + 1), device="cuda").float()).expand(-1, -1, 32).reshape(rows, k)
+        buffer = torch.full((rows * k // 32 + 1,), 255, dtype=torch.uint8, device="cuda")       # (NaN, should a neighbour be read)
+        scales = buffer[1:].view(rows, k // 32) if shifted else None
+        q, values = R.Mx4(rows, k, scales=scales), torch.empty(rows, k, device="cuda")
+        R.mx4_quantize(x, q)
+        R.mx4_dequantize(q, values)
+        return q, values.double()
+
+    (qa, a), (qw, w) = matrix(m, 81, 1.0), matrix(n, 83, 0.05)
+    want, size = a @ w.t().contiguous(), a.abs() @ w.abs().t().contiguous()
+    for dtype in (torch.float32, torch.bfloat16):
+        half = torch.finfo(dtype).eps / 2
+        bound = k * 2.0 ** -23 * size * (1 + half) + want.abs() * half + 2.0 ** -134
+        out = torch.empty(m, n, dtype=dtype, device="cuda")
+        R.mx4_matmul(qa, qw, out)
+        assert ((out.double() - want).abs() <= bound).all()
+    # NaN in one row of either: of that row and column only
+    qa.scales[m - 1, k // 32 - 1] = 255
+    qw.scales[n // 2, 0] = 255
+    out = torch.empty(m, n, device="cuda")
+    R.mx4_matmul(qa, qw, out)
+    bad = torch.isnan(out)
+    assert bad[m - 1].all() and bad[:, n // 2].all() and bad.sum().item() == m + n - 1
