@@ -422,6 +422,12 @@ def _same(ok, what):
         raise RoseError(ERR_SHAPE, what)
 
 
+def _on_gpu(what, *tensors):
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.is_contiguous()):
+            raise RoseError(ERR_SHAPE, "%s: contiguous memory on the GPU is wanted" % what)
+
+
 def embedding_lookup(table, tokens, out, scale=1.0, first_row=0, stream=None):
     """out[i] = scale * table[tokens[i] - first_row]; rows of zeros for tokens of other shards."""
     tp, tt, rows, cols, ts = _matrix(table, "embedding_lookup")
@@ -444,6 +450,7 @@ def embedding_grad(dy, tokens, grad, ws, scale=1.0, first_row=0, accumulate=Fals
     ip, ib, n = _tokens(tokens, "embedding_grad")
     gp, gt, rows, g_cols, gs = _matrix(grad, "embedding_grad")
     _same(n_dy == n and g_cols == cols, "embedding_grad")
+    _on_gpu("embedding_grad", ws)
     _check(_lib.rose_embedding_grad(dp, dt, ds, ip, ib, n, first_row, scale, gp, gt, rows, cols, gs, 1 if accumulate else 0,
                                     ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "embedding_grad")
 
@@ -460,14 +467,15 @@ def grad_workspace(device="cuda"):
     return torch.empty(GRAD_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
 
-def _grads(grad_tab, offsets, what):
+def _grads(grad_tab, offsets, what, *others):
+    _on_gpu(what, grad_tab, offsets, *others)
     _same(offsets.numel() == grad_tab.numel() + 1 and offsets.dtype == torch.int64 and grad_tab.dtype == torch.int64, what)
     return grad_tab.data_ptr(), offsets.data_ptr(), grad_tab.numel()
 
 
 def grad_sum_squares(grad_tab, offsets, total, dtype, out, ws, stream=None):
     """out (one float64): sum of the squares of all elements of the tensors of a pointer table; null pointers are left out."""
-    gp, fp, n = _grads(grad_tab, offsets, "grad_sum_squares")
+    gp, fp, n = _grads(grad_tab, offsets, "grad_sum_squares", out, ws)
     _same(out.dtype == torch.float64 and out.numel() == 1, "grad_sum_squares")
     _check(_lib.rose_grad_sum_squares(gp, fp, n, total, _dtype(dtype, "grad_sum_squares"), out.data_ptr(), ws.data_ptr(),
                                       ws.numel() * ws.element_size(), _stream(stream)), "grad_sum_squares")
@@ -475,7 +483,7 @@ def grad_sum_squares(grad_tab, offsets, total, dtype, out, ws, stream=None):
 
 def grad_clip(grad_tab, offsets, total, dtype, out_tab, sum_squares, max_norm, norm=None, stream=None):
     """Scales the tensors down to a norm of max_norm, given the sum of all squares; out_tab may be grad_tab."""
-    gp, fp, n = _grads(grad_tab, offsets, "grad_clip")
+    gp, fp, n = _grads(grad_tab, offsets, "grad_clip", out_tab, sum_squares, norm)
     _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and sum_squares.dtype == torch.float64 and
           (norm is None or norm.dtype == torch.float32), "grad_clip")
     _check(_lib.rose_grad_clip(gp, fp, n, total, _dtype(dtype, "grad_clip"), out_tab.data_ptr(), sum_squares.data_ptr(),
@@ -484,7 +492,7 @@ def grad_clip(grad_tab, offsets, total, dtype, out_tab, sum_squares, max_norm, n
 
 def grad_clip_norm(grad_tab, offsets, total, dtype, out_tab, max_norm, norm, ws, stream=None):
     """grad_sum_squares and grad_clip in one call, for a rank that holds everything."""
-    gp, fp, n = _grads(grad_tab, offsets, "grad_clip_norm")
+    gp, fp, n = _grads(grad_tab, offsets, "grad_clip_norm", out_tab, norm, ws)
     _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and (norm is None or norm.dtype == torch.float32), "grad_clip_norm")
     _check(_lib.rose_grad_clip_norm(gp, fp, n, total, _dtype(dtype, "grad_clip_norm"), out_tab.data_ptr(), max_norm,
                                     norm.data_ptr() if norm is not None else None, ws.data_ptr(),
@@ -507,6 +515,7 @@ def mx4_quantize(x, out, stream=None):
     """x (bf16 or float32) -> out, an Mx4 of the same shape"""
     xp, xt, rows, cols, xs = _matrix(x, "mx4_quantize")
     _same((out.rows, out.cols) == (rows, cols), "mx4_quantize")
+    _on_gpu("mx4_quantize", out.codes, out.scales)
     _check(_lib.rose_mx4_quantize(xp, xt, rows, cols, xs, out.codes.data_ptr(), out.scales.data_ptr(), _stream(stream)),
            "mx4_quantize")
 
@@ -514,6 +523,7 @@ def mx4_quantize(x, out, stream=None):
 def mx4_dequantize(q, out, stream=None):
     op, ot, rows, cols, os_ = _matrix(out, "mx4_dequantize")
     _same((q.rows, q.cols) == (rows, cols), "mx4_dequantize")
+    _on_gpu("mx4_dequantize", q.codes, q.scales)
     _check(_lib.rose_mx4_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), rows, cols, op, ot, os_, _stream(stream)),
            "mx4_dequantize")
 
@@ -522,6 +532,7 @@ def mx4_matmul(a, w, out, stream=None):
     """out = a @ w.T: a (m x k) and w (n x k, a stored [out, in] matrix) are Mx4"""
     op, ot, m, n, os_ = _matrix(out, "mx4_matmul")
     _same(a.cols == w.cols and (a.rows, w.rows) == (m, n), "mx4_matmul")
+    _on_gpu("mx4_matmul", a.codes, a.scales, w.codes, w.scales)
     _check(_lib.rose_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), m, w.codes.data_ptr(), w.scales.data_ptr(), n, a.cols,
                                 op, ot, os_, _stream(stream)), "mx4_matmul")
 
@@ -537,5 +548,6 @@ def mx4_linear(x, w, out, ws, stream=None):
     xp, xt, m, k, xs = _matrix(x, "mx4_linear")
     op, ot, m_out, n, os_ = _matrix(out, "mx4_linear")
     _same(m_out == m and w.cols == k and w.rows == n, "mx4_linear")
+    _on_gpu("mx4_linear", w.codes, w.scales, ws)
     _check(_lib.rose_mx4_linear(xp, xt, m, xs, w.codes.data_ptr(), w.scales.data_ptr(), n, k, op, ot, os_, ws.data_ptr(),
                                 ws.numel() * ws.element_size(), _stream(stream)), "mx4_linear")
