@@ -559,7 +559,7 @@ typedef uint64_t __attribute__((aligned(2))) u64_any2;
 
 constexpr int kRing = 3;                        // steps of 256 columns on the way
 constexpr int kChunk = 4;                       // steps whose scales (and activations, BF16) are made ready together
-constexpr int kBf16Rows = 4;                    // rows of activations that a product quantises itself
+constexpr int kBf16Rows = 4;                    // rows of activations that a product quantises together
 constexpr int kScaleRow = kChunk * 8 + 16;      // bytes of LDS for a row's scales of a chunk (and a gap: other banks for other rows)
 
 // bytes of LDS that a wave needs
@@ -766,7 +766,9 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
     return f32 ? go(float{}) : go(bf16_t{});
 }
 
-bool mx4_product_takes_bf16(int64_t m) { return m <= kBf16Rows; }
+// Twice as many rows where the columns are few: a launch less (8 x 1024 x 1024 9.4 us, 6.7 so, as part of a graph 7.1 and 6.6;
+// 8 x 4096 x 4096 in a graph 5.8 and 7.4, 16 x 1024 x 1024 7.2 and 9.5).
+bool mx4_product_takes_bf16(int64_t m, int64_t k) { return m <= kBf16Rows || (m <= 2 * kBf16Rows && k <= 2048); }
 
 template <int MT, int NT, bool BF16>
 static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {

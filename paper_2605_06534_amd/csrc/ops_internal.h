@@ -67,7 +67,7 @@ struct Mx4ProductArgs {
     int64_t m, n, k, out_stride;
 };
 // whether a product of this many rows quantises bf16 activations by itself
-bool mx4_product_takes_bf16(int64_t m);
+bool mx4_product_takes_bf16(int64_t m, int64_t k);
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream);
 
 }  // namespace rose

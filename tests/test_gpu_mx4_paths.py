@@ -92,3 +92,19 @@ def test_whole_groups_of_scales(m, n, k, shifted):
     R.mx4_matmul(qa, qw, out)
     bad = torch.isnan(out)
     assert bad[m - 1].all() and bad[:, n // 2].all() and bad.sum().item() == m + n - 1
+
+
+@pytest.mark.parametrize("m,k", [(4, 2049), (5, 2048), (5, 2080), (8, 2048), (8, 33), (9, 2048), (6, 1), (7, 1025)])
+def test_rows_that_a_product_rounds_itself(m, k):
+    """On either side of where the activations go through memory: the same values as through it."""
+    print("case: rounded on the way", m, k, flush=True)
+    n = 1003
+    x = torch.randn(m, k + 1, generator=torch.Generator("cuda").manual_seed(92), device="cuda").to(torch.bfloat16)[:, :k]
+    _, qw, w = rounded_matrix(n, k, 93)
+    q, values, out = R.Mx4(m, k), torch.empty(m, k, device="cuda"), torch.empty(m, n, device="cuda")
+    R.mx4_quantize(x, q)
+    R.mx4_dequantize(q, values)
+    R.mx4_linear(x, qw, out, R.mx4_linear_workspace(m, n, k))
+    a = values.double()
+    want, size = a @ w.t().contiguous(), a.abs() @ w.abs().t().contiguous()
+    assert ((out.double() - want).abs() <= k * 2.0 ** -23 * size * (1 + 2.0 ** -24) + want.abs() * 2.0 ** -24 + 2.0 ** -134).all()
