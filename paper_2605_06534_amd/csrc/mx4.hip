@@ -204,12 +204,13 @@ __device__ __forceinline__ f32x4 product(u32x4 w, uint32_t w_scale, u32x4 a, uin
 // lanes read together lie in eight different groups of LDS banks.
 // Scales go through registers: sixteen of a row (two slots) a thread, turned around so that a lane finds the four that it
 // needs for its quarter of four instructions in one word, of which the instruction picks a byte.
-// RAW, for rows of whole groups of 32 blocks (four slots): the scales go to LDS as the codes do, 32 of a row from two lanes, and
-// a lane reads the byte that it needs for each instruction: half the requests for scales, which are half as many as those for
-// codes otherwise, and no registers on the way, but an address for each fragment, for which only the smaller tiles have room (512
-// x 4096 x 4096 in tiles of 64 12.9 us, 11.6 so; 256 x 19008 x 5120 in tiles of 128 26.4, 25.3; 16384 x 6912 x 5120 300, 355).
-// 16384 x 6912 x 5120: 300 us, 3870 TFLOP/s (the simplest kernel: 7480 us; outputs written in half lines that caches keep 342);
-// 4096 x 4096 x 4096: 38 us, 3600.  What bounds it: either the loads from memory or the multiplications alone take three
+// WHOLE, for rows of whole groups of 32 blocks (four slots): a thread loads both halves of a group's scales together, so that
+// the second comes from the line that the first one brought.  That halves the requests for scales, which are half as many as
+// those for codes otherwise: 16384 x 6912 x 5120 302 us, 291 so; 256 x 19008 x 5120 in tiles of 128 26.4, 25.4; 512 x 4096 x 4096
+// in tiles of 64 12.9, 12.0.  (By loads to LDS and a byte for each instruction: the same in the small tiles, in the large one
+// there are no registers for the addresses, 355.)
+// 16384 x 6912 x 5120: 291 us, 3980 TFLOP/s (the simplest kernel: 7480 us; outputs written in half lines that caches keep 342);
+// 4096 x 4096 x 4096: 36 us, 3830.  What bounds it: either the loads from memory or the multiplications alone take three
 // quarters of that, and 7 us of each round of 256 tiles are outputs that leave and first slots that come, which nothing overlaps
 // where one workgroup fills a CU.  (Workgroups that take tile after tile and ask for the next one's first slots before they
 // write need more registers than there are: 380 us.)
@@ -324,15 +325,15 @@ __device__ __forceinline__ void store_some(bf16_t *p, int64_t left, const u32x4 
             if (e < left) p[e].bits = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
 }
 
-template <class OT, int BN, int BM, int WN, int WM, bool RAW>
+template <class OT, int BN, int BM, int WN, int WM, bool WHOLE>
 __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArgs a, int nb, int n_tiles, int m_tiles) {
     constexpr int kThr = 64 * WN * WM, FN = BN / WN / 16, FM = BM / WM / 16, kRows = BN + BM;
     constexpr int kPer = kThr / 8;                      // rows that one load of all threads takes
     constexpr int kLoadsW = BN / kPer, kLoads = kRows / kPer;
-    constexpr uint32_t kSlot = kRows * 128, kScaleSlot = kRows * 16;
+    constexpr uint32_t kSlot = kRows * 128, kScalePair = kRows * 16;       // a pair of slots has a vector of scales for each row
     static_assert(BN % kPer == 0 && BM % kPer == 0 && kPer % 16 == 0 && FN % 4 == 0 && kRows == kThr, "a row of scales a thread");
     __shared__ __attribute__((aligned(1024))) uint8_t codes[2][kSlot];
-    __shared__ __attribute__((aligned(1024))) u32x4 scales[2][RAW ? 2 * kRows : kRows];
+    __shared__ __attribute__((aligned(1024))) u32x4 scales[2][WHOLE ? 2 * kRows : kRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), of16 = lane & 15, quarter = lane >> 4;
     const int wn = wave % WN, wm = wave / WN;
     int nt, mt;
@@ -348,18 +349,9 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
     const uint32_t hop = kPer * (uint32_t)row_bytes;
     const uint32_t codes0 = lds_address(codes), scales0 = lds_address(scales);
     auto ask = [&](int d, int slot, int j) {
-        const bool is_w = j < kLoadsW, inside = d * 8 + (RAW ? 0 : is_w ? w_part : x_part) < nb;      // (RAW: whole slots)
+        const bool is_w = j < kLoadsW, inside = d * 8 + (WHOLE ? 0 : is_w ? w_part : x_part) < nb;
         const uint32_t off = is_w ? w_off + j * hop : x_off + (j - kLoadsW) * hop;
         load_to_lds(codes0 + slot * kSlot + j * kThr * 16 + wave * 1024, is_w ? w_res : x_res, inside ? off + d * 128 : kOutside);
-    };
-    // RAW: half of the 32 scales of row tid / 2 of either matrix
-    static_assert(!RAW || (kThr == 2 * BN && BN == BM), "a load of all threads for each matrix");
-    const u32x4 ws_res = resource_of(a.w_scales + n0 * nb, (a.n - n0) * nb), xs_res = resource_of(a.a_scales + m0 * nb, (a.m - m0) * nb);
-    const uint32_t s_off = (uint32_t)(tid >> 1) * (uint32_t)nb + (tid & 1) * 16;
-    auto ask_scales = [&](int g) {
-        const uint32_t off = g * 32 < nb ? s_off + g * 32 : kOutside, to = scales0 + (g & 1) * (kRows * 32) + wave * 1024;
-        load_to_lds(to, ws_res, off);
-        load_to_lds(to + kThr * 16, xs_res, off);
     };
     const int64_t s_row = tid < BN ? (n0 + tid < a.n ? n0 + tid : a.n - 1) : (m0 + tid - BN < a.m ? m0 + tid - BN : a.m - 1);
     const uint8_t *my_scales = (tid < BN ? a.w_scales : a.a_scales) + s_row * nb;
@@ -370,20 +362,21 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
     const int w_row = wn * (FN * 16) + (of16 >> 2) * 8 + (of16 & 3), x_row = BN + wm * (FM * 16) + of16;
     const uint32_t w_at = codes0 + w_row * 128 + (quarter ^ ((of16 & 3) | ((of16 >> 2) & 1) << 2)) * 16;
     const uint32_t x_at = codes0 + x_row * 128 + (quarter ^ (of16 & 7)) * 16;
-    const uint32_t ws_at = scales0 + (RAW ? w_row * 32 + quarter : w_row * 16 + quarter * 4);
-    const uint32_t xs_at = scales0 + (RAW ? x_row * 32 + quarter : x_row * 16 + quarter * 4);
+    const uint32_t ws_at = scales0 + w_row * 16 + quarter * 4, xs_at = scales0 + x_row * 16 + quarter * 4;
     u32x4 w[2][FN], x[FM], more_scales;
-    uint32_t ws[RAW ? 2 : 1][FN], xs[FM];
+    uint32_t ws[FN], xs[FM];
     auto get_w = [&](int slot, int half, u32x4 (&to)[FN]) {
 #pragma unroll
         for (int i = 0; i < FN; ++i) to[i] = from_lds<u32x4>((w_at ^ (half * 64)) + slot * kSlot + (i >> 1) * 4096 + (i & 1) * 512);
     };
     auto get_x = [&](int slot, int half, int j) { x[j] = from_lds<u32x4>((x_at ^ (half * 64)) + slot * kSlot + j * 2048); };
-    auto get_scales = [&](int slot) {
+    auto get_scales = [&](int pair) {
+        uint32_t ws_now = ws_at + pair * kScalePair, xs_now = xs_at + pair * kScalePair;
+        asm volatile("" : "+v"(ws_now), "+v"(xs_now));  // (two addresses, not one for each)
 #pragma unroll
-        for (int i = 0; i < FN; ++i) ws[0][i] = from_lds<uint32_t>(ws_at + slot * kScaleSlot + (i >> 1) * 512 + (i & 1) * 64);
+        for (int i = 0; i < FN; ++i) ws[i] = from_lds<uint32_t>(ws_now + (i >> 1) * 512 + (i & 1) * 64);
 #pragma unroll
-        for (int j = 0; j < FM; ++j) xs[j] = from_lds<uint32_t>(xs_at + slot * kScaleSlot + j * 256);
+        for (int j = 0; j < FM; ++j) xs[j] = from_lds<uint32_t>(xs_now + j * 256);
     };
     f32x4 sum[FN][FM];
 #pragma unroll
@@ -391,61 +384,62 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 #pragma unroll
         for (int j = 0; j < FM; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // RAW: a byte of the scales, of one half of a slot
-    auto get_ws = [&](uint32_t at, uint32_t (&to)[FN]) {
-#pragma unroll
-        for (int i = 0; i < FN; ++i) to[i] = from_lds<uint8_t>(ws_at + at + (i >> 1) * 1024 + (i & 1) * 128);
-    };
-    auto get_xs = [&](uint32_t at, int j) { xs[j] = from_lds<uint8_t>(xs_at + at + j * 512); };
     int d = 0;
     const int slots = (nb + 7) / 8;
-    if constexpr (RAW) {
-        ask_scales(0);
+    if constexpr (WHOLE) {
+        u32x4 more[2];
+        auto load_group = [&](int g) {                  // (behind the last one: any that is there)
+            const uint8_t *p = my_scales + (g * 32 < nb ? g * 32 : 0);
+            more[0] = reinterpret_cast<const u32x4_any *>(p)[0];
+            more[1] = reinterpret_cast<const u32x4_any *>(p)[1];
+        };
+        auto put_group = [&](int g) {
+            scales[g & 1][tid] = turned(more[0]);
+            scales[g & 1][kRows + tid] = turned(more[1]);
+        };
+        load_group(0);
+        put_group(0);
+        load_group(1);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) ask(0, 0, j);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) ask(1, 1, j);
         wait_and_meet<kLoads>();
         get_w(0, 0, w[0]);
-        get_ws(0, ws[0]);
 #pragma unroll
-        for (int j = 0; j < FM; ++j) {
-            get_x(0, 0, j);
-            get_xs(0, j);
-        }
-        // One slot of four, as below; the scales of the next four are asked for behind the first one's barrier, when those of
-        // the last four have been read, and have come at the last one's.
+        for (int j = 0; j < FM; ++j) get_x(0, 0, j);
+        get_scales(0);
+        // One slot of four, as below; the next group's scales are written behind the first one's barrier: those of the last
+        // group have been read.
         auto slot_of_four = [&](auto which) {
             constexpr int Q = decltype(which)::value, P = Q & 1;
-            asm volatile("" : "+s"(d));
+            asm volatile("" : "+s"(d));                 // (offsets are formed where they are used, not kept in registers)
             const int g = d >> 2;
-            const uint32_t at = (g & 1) * (kRows * 32), second = at + Q * 8 + 4, next = Q < 3 ? at + Q * 8 + 8 : kRows * 32 - at;
             get_w(P, 1, w[1]);
-            get_ws(second, ws[1]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
 #pragma unroll
-                for (int i = 0; i < FN; ++i) sum[i][j] = product<0>(w[0][i], ws[0][i], x[j], xs[j], sum[i][j]);
+                for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P>(w[0][i], ws[i], x[j], xs[j], sum[i][j]);
                 get_x(P, 1, j);
-                get_xs(second, j);
                 __builtin_amdgcn_sched_barrier(0);
             }
             wait_and_meet<0>();
-            if (Q == 0) ask_scales(g + 1);
+            if (Q == 0) put_group(g + 1);
             get_w(P ^ 1, 0, w[0]);
-            get_ws(next, ws[0]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
 #pragma unroll
-                for (int i = 0; i < FN; ++i) sum[i][j] = product<0>(w[1][i], ws[1][i], x[j], xs[j], sum[i][j]);
+                for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P + 1>(w[1][i], ws[i], x[j], xs[j], sum[i][j]);
                 get_x(P ^ 1, 0, j);
-                get_xs(next, j);
 #pragma unroll
                 for (int l = j * kLoads / FM; l < (j + 1) * kLoads / FM; ++l) ask(d + 2, P, l);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (Q == 3) load_group(g + 2);
+            if (Q == 1) get_scales((g & 1) * 2 + 1);
+            if (Q == 3) get_scales(((g + 1) & 1) * 2);
             ++d;
         };
         do {
@@ -477,7 +471,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
 #pragma unroll
-                for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P>(w[0][i], ws[0][i], x[j], xs[j], sum[i][j]);
+                for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P>(w[0][i], ws[i], x[j], xs[j], sum[i][j]);
                 get_x(P, 1, j);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -489,7 +483,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
 #pragma unroll
-                for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P + 1>(w[1][i], ws[0][i], x[j], xs[j], sum[i][j]);
+                for (int i = 0; i < FN; ++i) sum[i][j] = product<2 * P + 1>(w[1][i], ws[i], x[j], xs[j], sum[i][j]);
                 get_x(P ^ 1, 0, j);
 #pragma unroll
                 for (int l = j * kLoads / FM; l < (j + 1) * kLoads / FM; ++l) ask(d + 2, P, l);
@@ -795,13 +789,13 @@ static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     return (int)hipGetLastError();
 }
 
-template <int BN, int BM, int WN, int WM, bool RAW>
+template <int BN, int BM, int WN, int WM, bool WHOLE>
 static int launch_tiles(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     const int64_t n_tiles = (a.n + BN - 1) / BN, m_tiles = (a.m + BM - 1) / BM;
     if (n_tiles * m_tiles > 0x7FFFFFFF / 8) return (int)hipErrorInvalidValue;
     const dim3 grid((unsigned)(n_tiles * m_tiles)), block(64 * WN * WM);
-    if (out_f32) hipLaunchKernelGGL((mx4_tile_kernel<float, BN, BM, WN, WM, RAW>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
-    else hipLaunchKernelGGL((mx4_tile_kernel<bf16_t, BN, BM, WN, WM, RAW>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
+    if (out_f32) hipLaunchKernelGGL((mx4_tile_kernel<float, BN, BM, WN, WM, WHOLE>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
+    else hipLaunchKernelGGL((mx4_tile_kernel<bf16_t, BN, BM, WN, WM, WHOLE>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
     return (int)hipGetLastError();
 }
 
@@ -828,10 +822,10 @@ int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     // (256 x 19008 x 5120: 38.5 us with the large ones, 25.3 with the small; 4096 x 4096 x 4096: 37 and 45), and tiles of 64
     // where also those leave CUs idle (256 x 6912 x 5120 18.6 us, 14.4 with 64; 512 x 6912 x 5120 18.9 and 18.7).
     auto tiles = [&](int64_t b) { return ((a.n + b - 1) / b) * ((a.m + b - 1) / b); };
-    if (tiles(256) >= 192) return launch_tiles<256, 256, 4, 2, false>(a, out_f32, st);
-    const bool raw = a.k % 1024 == 0 && ((uintptr_t)a.w_scales | (uintptr_t)a.a_scales) % 16 == 0;      // (rows of scales in whole vectors)
-    if (tiles(128) >= 192) return raw ? launch_tiles<128, 128, 2, 2, true>(a, out_f32, st) : launch_tiles<128, 128, 2, 2, false>(a, out_f32, st);
-    return raw ? launch_tiles<64, 64, 1, 2, true>(a, out_f32, st) : launch_tiles<64, 64, 1, 2, false>(a, out_f32, st);
+    const bool whole = a.k % 1024 == 0;
+    if (tiles(256) >= 192) return whole ? launch_tiles<256, 256, 4, 2, true>(a, out_f32, st) : launch_tiles<256, 256, 4, 2, false>(a, out_f32, st);
+    if (tiles(128) >= 192) return whole ? launch_tiles<128, 128, 2, 2, true>(a, out_f32, st) : launch_tiles<128, 128, 2, 2, false>(a, out_f32, st);
+    return whole ? launch_tiles<64, 64, 1, 2, true>(a, out_f32, st) : launch_tiles<64, 64, 1, 2, false>(a, out_f32, st);
 }
 
 }  // namespace rose

@@ -108,3 +108,19 @@ def test_rows_that_a_product_rounds_itself(m, k):
     a = values.double()
     want, size = a @ w.t().contiguous(), a.abs() @ w.abs().t().contiguous()
     assert ((out.double() - want).abs() <= k * 2.0 ** -23 * size * (1 + 2.0 ** -24) + want.abs() * 2.0 ** -24 + 2.0 ** -134).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(3400, 3600, 1024), (3329, 3841, 2048), (3500, 3500, 5120), (300, 49000, 1024)])
+def test_large_tiles_of_whole_groups(m, n, k):
+    print("case: large tiles, whole groups", m, n, k, flush=True)
+    _, qa, a = rounded_matrix(m, k, 95)
+    _, qw, w = rounded_matrix(n, k, 96, 0.05)
+    qw.scales[n - 1, k // 32 - 1] = 255                           # NaN, of the last column only
+    want, size = a @ w.t().contiguous(), a.abs() @ w.abs().t().contiguous()
+    for dtype in (torch.float32, torch.bfloat16):
+        half = torch.finfo(dtype).eps / 2
+        bound = k * 2.0 ** -23 * size * (1 + half) + want.abs() * half + 2.0 ** -134
+        out = torch.empty(m, n, dtype=dtype, device="cuda")
+        R.mx4_matmul(qa, qw, out)
+        assert torch.isnan(out[:, n - 1]).all()
+        assert ((out.double() - want).abs() <= bound)[:, :n - 1].all()
