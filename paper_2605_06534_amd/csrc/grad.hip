@@ -205,8 +205,7 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
 
 template <class T>
 int64_t small_pieces(int64_t total) {
-    const int64_t n = (total + kSmallPiece<T> - 1) / kSmallPiece<T>;
-    return n < 1 ? 1 : n;
+    return total > 0 ? (total - 1) / kSmallPiece<T> + 1 : 1;
 }
 
 template <class T>
@@ -218,9 +217,10 @@ int squares(GradArgs &a, int64_t total, hipStream_t st) {
     return (int)hipGetLastError();
 }
 
+// (more pieces than a launch can have workgroups: each takes several)
 template <class T, bool FROM_PARTIALS>
 int clip(GradArgs &a, int64_t total, hipStream_t st) {
-    const int64_t n = small_pieces<T>(total), most = 1 << 30;
+    const int64_t n = small_pieces<T>(total), most = kMostThreads / kThreads;
     a.piece = kSmallPiece<T>;
     hipLaunchKernelGGL((grad_clip_kernel<T, FROM_PARTIALS>), dim3((unsigned)(n < most ? n : most)), dim3(kThreads), 0, st, a);
     return (int)hipGetLastError();

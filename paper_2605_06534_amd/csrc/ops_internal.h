@@ -9,6 +9,8 @@
 
 namespace rose {
 
+constexpr int64_t kMostThreads = 0xFFFFFFFF;        // of a launch in one dimension
+
 struct Tokens {
     const void *ids;
     int32_t wide;                       // 64-bit ids

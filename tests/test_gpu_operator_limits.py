@@ -1,0 +1,33 @@
+"""The operators at the limits of what a launch can hold: values that are known exactly, whatever is launched for them."""
+import pytest
+import torch
+
+import paper_2605_06534_amd as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("total", [0, 1, 50000, 1 << 37, 1 << 40, (1 << 63) - 1])
+def test_clipping_with_a_total_that_is_wrong(total, dtype):
+    """Gradients of ones and a factor of 1 / 4 (the norm and what 1e-6 adds to it are far from where that could round elsewhere)."""
+    print("case: clip with another total", total, dtype, flush=True)
+    numels = [70000, 3, 50001]
+    flat = torch.ones(sum(numels) + 1, dtype=dtype, device="cuda")
+    views = list(flat[1:].split(numels))
+    tab, offsets, norm, ws = R.ptr_table(views), R.offset_table(numels), torch.zeros(1, device="cuda"), R.grad_workspace()
+    exact = sum(numels) ** 0.5
+    for two_calls in (False, True):
+        out = torch.full_like(flat, 9.0)
+        out_tab = R.ptr_table(list(out[1:].split(numels)))
+        if two_calls:
+            s = torch.zeros(1, dtype=torch.float64, device="cuda")
+            R.grad_sum_squares(tab, offsets, total, dtype, s, ws)
+            assert s.item() == sum(numels)                        # (whole numbers add up exactly)
+            R.grad_clip(tab, offsets, total, dtype, out_tab, s, exact / 4, norm)
+        else:
+            R.grad_clip_norm(tab, offsets, total, dtype, out_tab, exact / 4, norm, ws)
+        assert abs(norm.item() - exact) <= exact * 2.0 ** -24
+        # the norm, the sum with 1e-6 and the quotient are rounded to fp32, then the result to its type
+        assert ((out[1:].double() - 0.25 * exact / (exact + 1e-6)).abs() <= 0.25 * (4 * 2.0 ** -24 + torch.finfo(dtype).eps / 2)).all()
+        assert out[0].item() == 9.0

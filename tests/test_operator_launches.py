@@ -1,0 +1,99 @@
+"""No launch of an operator asks for 2^32 threads or more in a dimension, which is more than a launch can have: shown on the
+host, with a stand-in for the runtime's launch function that notes the sizes and starts nothing.  The addresses are never read."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2605_06534_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, UNSUPPORTED = binding.OK, binding.ERR_UNSUPPORTED
+BF16, F32 = binding.DTYPE_BF16, binding.DTYPE_F32
+P = 1 << 20                                         # an aligned address
+MOST = (1 << 31) - 1                                # rows, columns and tokens that the operators take
+
+RECORDER = """
+#include <stddef.h>
+typedef struct { unsigned x, y, z; } dims;
+static unsigned long long noted[4096][3];
+static int launches;
+int hipLaunchKernel(const void *f, dims grid, dims block, void **args, size_t lds, void *stream) {
+    if (launches < 4096) {
+        noted[launches][0] = (unsigned long long)grid.x * block.x;
+        noted[launches][1] = (unsigned long long)grid.y * block.y;
+        noted[launches][2] = (unsigned long long)grid.z * block.z;
+    }
+    ++launches;
+    return 0;
+}
+int hipGetLastError(void) { return 0; }
+/* what a launch's sizes go through on their way there */
+static dims next_grid, next_block;
+static size_t next_lds;
+static void *next_stream;
+int __hipPushCallConfiguration(dims grid, dims block, size_t lds, void *stream) {
+    next_grid = grid, next_block = block, next_lds = lds, next_stream = stream;
+    return 0;
+}
+int __hipPopCallConfiguration(dims *grid, dims *block, size_t *lds, void **stream) {
+    *grid = next_grid, *block = next_block, *lds = next_lds, *stream = next_stream;
+    return 0;
+}
+int noted_launches(void) { return launches; }
+void forget_launches(void) { launches = 0; }
+unsigned long long noted_threads(int launch, int dimension) { return noted[launch][dimension]; }
+"""
+
+# The stand-in is loaded for everyone before the library is: its functions are the ones that the library finds.
+SCRIPT = """
+import ctypes, json, sys
+recorder = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+recorder.noted_threads.restype = ctypes.c_ulonglong
+sys.path.insert(0, sys.argv[2])
+from paper_2605_06534_amd import binding
+out = []
+for name, args in json.loads(sys.stdin.read()):
+    recorder.forget_launches()
+    status = getattr(binding._lib, name)(*args)
+    out.append((status, [[recorder.noted_threads(i, d) for d in range(3)] for i in range(recorder.noted_launches())]))
+print("launches " + json.dumps(out))
+"""
+
+
+@pytest.fixture(scope="module")
+def recorder(tmp_path_factory):
+    folder = tmp_path_factory.mktemp("recorder")
+    source, lib = folder / "recorder.c", folder / "recorder.so"
+    source.write_text(RECORDER)
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-O1", str(source), "-o", str(lib)])
+    return str(lib)
+
+
+def launched(recorder, calls):
+    """[(status, threads of each launch)] of calls [(name, arguments)]"""
+    done = subprocess.run([sys.executable, "-c", SCRIPT, recorder, ROOT], input=json.dumps(calls), capture_output=True, text=True, timeout=600)
+    assert done.returncode == 0, done.stderr
+    return json.loads([line for line in done.stdout.splitlines() if line.startswith("launches ")][-1][len("launches "):])
+
+
+def fits(launches):
+    return all(0 < threads < 1 << 32 for launch in launches for threads in launch)
+
+
+def test_the_stand_in_sees_the_launches(recorder):
+    (status, launches), = launched(recorder, [("rose_grad_sum_squares", (P, P, 3, 100, F32, P, P, binding.GRAD_WORKSPACE_BYTES, None))])
+    assert status == OK and launches == [[256, 1, 1], [256, 1, 1]]
+
+
+def test_clipping_with_any_total(recorder):
+    calls = []
+    for dtype in (BF16, F32):
+        for total in (0, 1, 1 << 32, 1 << 36, 1 << 37, 1 << 40, (1 << 63) - 1):
+            calls += [("rose_grad_sum_squares", (P, P, 3, total, dtype, P, P, binding.GRAD_WORKSPACE_BYTES, None)),
+                      ("rose_grad_clip", (P, P, 3, total, dtype, P, P, 1.0, P, None)),
+                      ("rose_grad_clip_norm", (P, P, 3, total, dtype, P, 1.0, P, P, binding.GRAD_WORKSPACE_BYTES, None))]
+    for call, (status, launches) in zip(calls, launched(recorder, calls)):
+        assert status == OK and launches and fits(launches), (call, launches)
