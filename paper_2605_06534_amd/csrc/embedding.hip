@@ -578,7 +578,30 @@ GradLayout grad_layout(int64_t rows, int64_t cols, int64_t n) {
     return l;
 }
 
+// how the sums go to waves, and what crosses the ends of blocks to workgroups that join it
+struct SumShape {
+    int64_t lanes, chunks, groups, join_chunks, joins;
+};
+SumShape sum_shape(const GradLayout &l, int64_t cols, bool grad_f32) {
+    SumShape s = {};
+    // waves of as many lanes as another, and none of a single one, which would share columns with another wave (see Columns)
+    const int64_t width = grad_f32 ? kSumWidth<float> : kSumWidth<bf16_t>, vectors = (cols + width - 1) / width;
+    s.chunks = (vectors + 63) / 64;
+    s.lanes = s.chunks ? (vectors + s.chunks - 1) / s.chunks : 1;
+    while (vectors > 1 && vectors % s.lanes == 1) --s.lanes;
+    s.chunks = (vectors + s.lanes - 1) / s.lanes;
+    s.groups = (l.blocks + 7) / 8 * 8 * s.chunks;
+    s.join_chunks = (cols + 1023) / 1024;
+    s.joins = l.blocks > 0 ? (l.blocks - 1) * s.join_chunks : 0;
+    return s;
+}
+
 }  // namespace
+
+bool embedding_grad_fits(int64_t rows, int64_t cols, int64_t n_tokens, bool grad_f32) {
+    const SumShape s = sum_shape(grad_layout(rows, cols, n_tokens), cols, grad_f32);
+    return s.groups <= kMostThreads / 64 && s.joins <= kMostThreads / 256;
+}
 
 size_t embedding_grad_workspace(int64_t rows, int64_t cols, int64_t n_tokens) { return grad_layout(rows, cols, n_tokens).total; }
 
@@ -608,6 +631,7 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     const int64_t n = a.tokens.n, rows = a.tokens.rows;
     if (rows == 0 || a.cols == 0 || (n == 0 && a.accumulate)) return 0;
     const GradLayout l = grad_layout(rows, a.cols, n);
+    const SumShape shape = sum_shape(l, a.cols, grad_f32);
     SortArgs s = {};
     s.tokens = a.tokens;
     for (int i = 0; i < 2; ++i) {
@@ -627,9 +651,12 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     int64_t fills = 0, fill_later = 0;
     if (!a.accumulate) {
         const int64_t size = grad_f32 ? 4 : 2, row_bytes = a.cols * size;
-        const int64_t blind = n == 0 ? rows : kBlindBytes / row_bytes < rows ? kBlindBytes / row_bytes : rows;
+        // (and no more in the launch of the sums than it has workgroups for: of 2^30 rows of one column some would be left)
+        const int64_t later = kBlindBytes / row_bytes < rows ? rows - kBlindBytes / row_bytes : 0;
+        const int64_t most_later = (kMostThreads / 64 - shape.groups) * kFillRows;
+        fill_later = n == 0 ? 0 : later < most_later ? later : most_later;
+        const int64_t blind = rows - fill_later;
         const bool whole = a.grad_stride == a.cols;
-        fill_later = rows - blind;
         s.fill.at = static_cast<char *>(a.grad) + fill_later * a.grad_stride * size;
         s.fill.rows = whole ? 1 : blind;
         s.fill.row_bytes = whole ? blind * row_bytes : row_bytes;
@@ -667,18 +694,12 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     u.scale = a.scale;
     u.accumulate = a.accumulate;
     u.run = l.run;
-    // waves of as many lanes as another, and none of a single one, which would share columns with another wave (see Columns)
-    const int64_t width = grad_f32 ? kSumWidth<float> : kSumWidth<bf16_t>, vectors = (a.cols + width - 1) / width;
-    int64_t chunks = (vectors + 63) / 64, lanes = (vectors + chunks - 1) / chunks;
-    while (vectors > 1 && vectors % lanes == 1) --lanes;
-    chunks = (vectors + lanes - 1) / lanes;
-    const int64_t join_chunks = (a.cols + 1023) / 1024;
-    u.lanes = (int32_t)lanes;
-    u.chunks = (uint32_t)chunks;
-    const int64_t sums = (l.blocks + 7) / 8 * 8 * chunks, grid = sums + (fill_later + kFillRows - 1) / kFillRows;
-    if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
+    u.lanes = (int32_t)shape.lanes;
+    u.chunks = (uint32_t)shape.chunks;
+    const int64_t width = grad_f32 ? kSumWidth<float> : kSumWidth<bf16_t>;
+    const int64_t grid = shape.groups + (fill_later + kFillRows - 1) / kFillRows;
     u.fill_rows = fill_later;
-    u.sum_groups = (uint32_t)sums;
+    u.sum_groups = (uint32_t)shape.groups;
     auto sum = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64), 0, st, u); };
     auto of_types = [&](auto d, auto g) {
         using DT = decltype(d);
@@ -688,10 +709,8 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     };
     if (dy_f32) grad_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});
     else grad_f32 ? of_types(bf16_t{}, float{}) : of_types(bf16_t{}, bf16_t{});
-    const int64_t joins = (l.blocks - 1) * join_chunks;
-    if (joins > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    if (joins > 0) {
-        auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)joins), dim3(256), 0, st, u, (uint32_t)join_chunks); };
+    if (shape.joins > 0) {
+        auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)shape.joins), dim3(256), 0, st, u, (uint32_t)shape.join_chunks); };
         grad_f32 ? join(embedding_join_kernel<float>) : join(embedding_join_kernel<bf16_t>);
     }
     return (int)hipGetLastError();

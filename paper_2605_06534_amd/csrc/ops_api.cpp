@@ -90,6 +90,7 @@ extern "C" rose_status rose_embedding_grad(const void *dy, int32_t dy_dtype, int
     ROSE_CHECK(check_tokens(tokens, token_bytes, n_tokens, first_row));
     ROSE_CHECK(check_matrix(grad, grad_dtype, rows, cols, grad_stride));
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::embedding_grad_workspace(rows, cols, n_tokens)));
+    if (!rose::embedding_grad_fits(rows, cols, n_tokens, grad_dtype == ROSE_DTYPE_F32)) return ROSE_ERR_UNSUPPORTED;
     rose::EmbeddingGradArgs a = {{tokens, token_bytes == 8, n_tokens, first_row, rows}, dy, grad, cols, dy_stride, grad_stride,
                                  scale, accumulate != 0, static_cast<char *>(workspace)};
     return status_of(rose::launch_embedding_grad(a, dy_dtype == ROSE_DTYPE_F32, grad_dtype == ROSE_DTYPE_F32, stream));

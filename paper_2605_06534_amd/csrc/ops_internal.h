@@ -37,6 +37,7 @@ struct EmbeddingGradArgs {
     int32_t accumulate;
     char *workspace;
 };
+bool embedding_grad_fits(int64_t rows, int64_t cols, int64_t n_tokens, bool grad_f32);      // its sums into launches
 size_t embedding_grad_workspace(int64_t rows, int64_t cols, int64_t n_tokens);
 int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32, void *stream);
 

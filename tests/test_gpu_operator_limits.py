@@ -31,3 +31,19 @@ def test_clipping_with_a_total_that_is_wrong(total, dtype):
         # the norm, the sum with 1e-6 and the quotient are rounded to fp32, then the result to its type
         assert ((out[1:].double() - 0.25 * exact / (exact + 1e-6)).abs() <= 0.25 * (4 * 2.0 ** -24 + torch.finfo(dtype).eps / 2)).all()
         assert out[0].item() == 9.0
+
+
+@pytest.mark.parametrize("n", [5, 20000])
+def test_a_gradient_of_more_rows_than_one_launch_clears(n):
+    """Rows that differ, so every value is one token's; all other rows become zero."""
+    print("case: gradient of 2^30 rows", n, flush=True)
+    rows, cols = (1 << 30) + 3, 1
+    tokens = torch.arange(n, device="cuda") * (rows // n)
+    tokens[-1], tokens[n // 2] = rows - 1, rows           # (the last row, and no row)
+    dy = (torch.arange(n, device="cuda") % 255 + 1).to(torch.bfloat16)[:, None]
+    grad = torch.full((rows, cols), 9.0, dtype=torch.bfloat16, device="cuda")
+    R.embedding_grad(dy, tokens, grad, R.embedding_grad_workspace(rows, cols, n), scale=2.0)
+    here = tokens < rows
+    assert torch.equal(grad[tokens[here]], dy[here] * 2)
+    grad[tokens[here]] = 0
+    assert not grad.any().item()

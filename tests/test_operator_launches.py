@@ -97,3 +97,21 @@ def test_clipping_with_any_total(recorder):
                       ("rose_grad_clip_norm", (P, P, 3, total, dtype, P, 1.0, P, P, binding.GRAD_WORKSPACE_BYTES, None))]
     for call, (status, launches) in zip(calls, launched(recorder, calls)):
         assert status == OK and launches and fits(launches), (call, launches)
+
+
+@pytest.mark.parametrize("grad", [BF16, F32], ids=["bf16", "f32"])
+def test_gradients_of_very_many_rows(recorder, grad):
+    """Narrow gradients whose rows without tokens are more than one launch takes eight of a workgroup."""
+    calls = [("rose_embedding_grad", (P, BF16, cols, P, 8, n, 0, 1.0, P, grad, rows, cols, stride, 0, P, 1 << 62, None))
+             for rows in (1 << 20, (1 << 29) + 1, 600000000, 1 << 30, MOST) for cols, stride in ((1, 1), (1, 2), (7, 7), (9, 9))
+             for n in (0, 1, 5, 20000, MOST)]
+    for call, (status, launches) in zip(calls, launched(recorder, calls)):
+        assert status == OK and launches and fits(launches), (call, launches)
+
+
+def test_gradients_of_more_than_launches_hold_queue_nothing(recorder):
+    """No memory holds these; what is refused is refused before the tokens are sorted."""
+    calls = [("rose_embedding_grad", (P, BF16, cols, P, 8, n, 0, 1.0, P, F32, 10, cols, cols, accumulate, P, 1 << 62, None))
+             for n, cols in ((MOST, MOST), (1 << 27, MOST), (MOST, 1 << 27)) for accumulate in (0, 1)]
+    for call, (status, launches) in zip(calls, launched(recorder, calls)):
+        assert status == UNSUPPORTED and not launches, (call, status, launches)
