@@ -612,14 +612,22 @@ int launch_embedding_lookup(const LookupArgs &a, bool table_f32, bool out_f32, v
         using TT = decltype(t);
         using OT = decltype(o);
         constexpr int W = kLookupWidth<OT>;
-        const int64_t row_vectors = (a.cols + W - 1) / W, vectors = a.tokens.n * row_vectors;
-        const bool many = a.cols >= W && vectors >= (int64_t)kLookupThreads * 2 * 1024;   // enough for every CU also at two a lane
-        const int64_t per = kLookupThreads * (many ? 2 : 1), groups = (vectors + per - 1) / per;
-        if (groups > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-        const Rows rows = rows_of(a.tokens.n, row_vectors);
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kLookupThreads), 0, st, a, rows); };
-        if (a.cols < W) go(embedding_lookup_kernel<TT, OT, 1, true>);
-        else many ? go(embedding_lookup_kernel<TT, OT, 2, false>) : go(embedding_lookup_kernel<TT, OT, 1, false>);
+        const int64_t row_vectors = (a.cols + W - 1) / W;
+        const bool many = a.cols >= W && a.tokens.n * row_vectors >= (int64_t)kLookupThreads * 2 * 1024;   // enough for every CU also at two a lane
+        const int64_t per = kLookupThreads * (many ? 2 : 1);
+        // (outputs of more than 2^33 vectors are more than a launch has threads for: as many tokens at a time as it has)
+        const int64_t most = kMostThreads / kLookupThreads * per / row_vectors;
+        for (int64_t first = 0; first < a.tokens.n; first += most) {
+            LookupArgs part = a;
+            part.tokens.ids = static_cast<const char *>(a.tokens.ids) + first * (a.tokens.wide ? 8 : 4);
+            part.tokens.n = a.tokens.n - first < most ? a.tokens.n - first : most;
+            part.out = static_cast<OT *>(a.out) + first * a.out_stride;
+            const Rows rows = rows_of(part.tokens.n, row_vectors);
+            const int64_t groups = (rows.vectors + per - 1) / per;
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kLookupThreads), 0, st, part, rows); };
+            if (a.cols < W) go(embedding_lookup_kernel<TT, OT, 1, true>);
+            else many ? go(embedding_lookup_kernel<TT, OT, 2, false>) : go(embedding_lookup_kernel<TT, OT, 1, false>);
+        }
         return (int)hipGetLastError();
     };
     if (table_f32) return out_f32 ? of_types(float{}, float{}) : of_types(float{}, bf16_t{});

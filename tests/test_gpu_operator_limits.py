@@ -47,3 +47,26 @@ def test_a_gradient_of_more_rows_than_one_launch_clears(n):
     assert torch.equal(grad[tokens[here]], dy[here] * 2)
     grad[tokens[here]] = 0
     assert not grad.any().item()
+
+
+def room_for(gigabytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gigabytes << 30:
+        pytest.skip("needs %d GB of free GPU memory" % gigabytes)
+
+
+def test_a_lookup_of_more_vectors_than_a_launch_has_threads_for():
+    print("case: lookup of 2^33 vectors", flush=True)
+    room_for(130)
+    n, cols = (1 << 31) - 1, 25
+    tokens = torch.arange(n, dtype=torch.int32, device="cuda").remainder_(251).sub_(1)       # (a token of no row among them)
+    table = torch.randn(250, cols, generator=torch.Generator("cuda").manual_seed(3), device="cuda").to(torch.bfloat16)
+    out = torch.empty(n, cols, dtype=torch.bfloat16, device="cuda")
+    R.embedding_lookup(table, tokens, out, scale=0.5)
+    ends = torch.cat([torch.zeros(1, cols, dtype=torch.bfloat16, device="cuda"), table * 0.5])
+    for at in (0, 1 << 30, n - 100000, n - 1000):
+        part = slice(at, min(n, at + 100000))
+        assert torch.equal(out[part], ends[tokens[part].long() + 1])
+    assert torch.equal(out[:, 24], ends[:, 24].repeat(n // 251 + 1)[:n])
+    del out, tokens
+    torch.cuda.empty_cache()

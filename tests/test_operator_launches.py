@@ -115,3 +115,14 @@ def test_gradients_of_more_than_launches_hold_queue_nothing(recorder):
              for n, cols in ((MOST, MOST), (1 << 27, MOST), (MOST, 1 << 27)) for accumulate in (0, 1)]
     for call, (status, launches) in zip(calls, launched(recorder, calls)):
         assert status == UNSUPPORTED and not launches, (call, status, launches)
+
+
+@pytest.mark.parametrize("out", [BF16, F32], ids=["bf16", "f32"])
+def test_lookups_of_very_many_vectors(recorder, out):
+    calls = [("rose_embedding_lookup", (P, BF16, 100, cols, cols, P, 4, n, 0, 1.0, P, out, cols, None))
+             for n, cols in ((1, MOST), (1, 1), (MOST, 1), (MOST, 9), (MOST, 25), (1 << 30, 200), (1 << 24, 5120), (20000, MOST))]
+    for call, (status, launches) in zip(calls, launched(recorder, calls)):
+        assert status == OK and launches and fits(launches), (call, launches)
+        _, (_, _, _, cols, _, _, _, n, *_) = call
+        vectors = n * -(-cols // (8 if out == BF16 else 4))
+        assert vectors <= 2 * sum(threads for threads, _, _ in launches) < 2 * vectors + 1024 * len(launches)     # one or two a thread
