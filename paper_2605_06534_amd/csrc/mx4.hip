@@ -726,13 +726,27 @@ int64_t blocks_of(int64_t cols) { return (cols + ROSE_MX4_BLOCK - 1) / ROSE_MX4_
 
 }  // namespace
 
+// width: elements of a vector, size: bytes of an element.  (Matrices of more than 2^33 vectors are more than a launch has threads
+// for: as many rows at a time as it has)
 template <class Kernel>
-static int launch_quant(QuantArgs a, int64_t rows, int64_t width, Kernel kernel, hipStream_t st) {
-    const int64_t row_vectors = blocks_of(a.cols) * (ROSE_MX4_BLOCK / width), per = kThreads * kUnits, groups = (rows * row_vectors + per - 1) / per;
-    if (groups == 0) return 0;
-    if (groups > 0x7FFFFFFF) return (int)hipErrorInvalidValue;
-    a.rows = rows_of(rows, row_vectors);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, st, a);
+static int launch_quant(const QuantArgs &a, int64_t rows, int64_t width, int64_t size, Kernel kernel, hipStream_t st) {
+    const int64_t blocks = blocks_of(a.cols), row_vectors = blocks * (ROSE_MX4_BLOCK / width), per = kThreads * kUnits;
+    if (rows == 0 || blocks == 0) return 0;
+    const int64_t most = kMostThreads / kThreads * per / row_vectors;
+    for (int64_t first = 0; first < rows; first += most) {
+        QuantArgs part = a;
+        if (a.x) {
+            part.x = static_cast<const char *>(a.x) + first * a.stride * size;
+            part.codes = a.codes + first * blocks * 16;
+            part.scales = a.scales + first * blocks;
+        } else {
+            part.out = static_cast<char *>(a.out) + first * a.stride * size;
+            part.codes_in = a.codes_in + first * blocks * 16;
+            part.scales_in = a.scales_in + first * blocks;
+        }
+        part.rows = rows_of(rows - first < most ? rows - first : most, row_vectors);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((part.rows.vectors + per - 1) / per)), dim3(kThreads), 0, st, part);
+    }
     return (int)hipGetLastError();
 }
 
@@ -743,7 +757,8 @@ int launch_mx4_quantize(const void *x, bool f32, int64_t rows, int64_t cols, int
     auto go = [&](auto t) {
         using T = decltype(t);
         constexpr int64_t W = kWidth<T>;
-        return cols < W ? launch_quant(a, rows, W, mx4_quantize_kernel<T, true>, st) : launch_quant(a, rows, W, mx4_quantize_kernel<T, false>, st);
+        return cols < W ? launch_quant(a, rows, W, sizeof(T), mx4_quantize_kernel<T, true>, st)
+                        : launch_quant(a, rows, W, sizeof(T), mx4_quantize_kernel<T, false>, st);
     };
     return f32 ? go(float{}) : go(bf16_t{});
 }
@@ -755,7 +770,8 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
     auto go = [&](auto t) {
         using T = decltype(t);
         constexpr int64_t W = kWidth<T>;
-        return cols < W ? launch_quant(a, rows, W, mx4_dequantize_kernel<T, true>, st) : launch_quant(a, rows, W, mx4_dequantize_kernel<T, false>, st);
+        return cols < W ? launch_quant(a, rows, W, sizeof(T), mx4_dequantize_kernel<T, true>, st)
+                        : launch_quant(a, rows, W, sizeof(T), mx4_dequantize_kernel<T, false>, st);
     };
     return f32 ? go(float{}) : go(bf16_t{});
 }

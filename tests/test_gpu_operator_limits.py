@@ -70,3 +70,30 @@ def test_a_lookup_of_more_vectors_than_a_launch_has_threads_for():
     assert torch.equal(out[:, 24], ends[:, 24].repeat(n // 251 + 1)[:n])
     del out, tokens
     torch.cuda.empty_cache()
+
+
+def test_a_4_bit_matrix_of_more_vectors_than_a_launch_has_threads_for():
+    """Whole numbers up to 4 and a power of two for every row come back as they were."""
+    print("case: mx4 of 2^33 vectors", flush=True)
+    room_for(110)
+    rows, cols = (1 << 29) + 5, 33
+    small = torch.randint(-4, 5, (255, cols), generator=torch.Generator("cuda").manual_seed(4), device="cuda").float()
+    small[:, 0] = 4.0
+    small[:, 32] = 4.0
+    small *= torch.exp2(torch.arange(255, device="cuda") % 20 - 10.0)[:, None]
+    x = small.repeat(rows // 255 + 1, 1)[:rows]
+    q = R.Mx4(rows, cols)
+    R.mx4_quantize(x, q)
+    want = R.Mx4(255, cols)
+    R.mx4_quantize(small, want)
+    for at in (0, 1 << 28, (1 << 29) - 700, rows - 600):
+        part = slice(at, min(rows, at + 600))
+        which = torch.arange(part.start, part.stop, device="cuda") % 255
+        assert torch.equal(q.codes[part], want.codes[which]) and torch.equal(q.scales[part], want.scales[which])
+    x.fill_(77.0)
+    R.mx4_dequantize(q, x)
+    for at in range(0, rows, 255 * 100000):
+        part = x[at:at + 255 * 100000]
+        assert torch.equal(part, small.repeat(100001, 1)[:len(part)])
+    del x, q
+    torch.cuda.empty_cache()

@@ -126,3 +126,14 @@ def test_lookups_of_very_many_vectors(recorder, out):
         _, (_, _, _, cols, _, _, _, n, *_) = call
         vectors = n * -(-cols // (8 if out == BF16 else 4))
         assert vectors <= 2 * sum(threads for threads, _, _ in launches) < 2 * vectors + 1024 * len(launches)     # one or two a thread
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_4_bit_matrices_of_very_many_vectors(recorder, dtype):
+    sizes = [(1, 1), (MOST, 1), (MOST, 33), (1 << 29, 33), (1 << 30, 64), (5, MOST), (1 << 24, 28000)]
+    calls = [("rose_mx4_quantize", (P, dtype, rows, cols, cols, P, P, None)) for rows, cols in sizes]
+    calls += [("rose_mx4_dequantize", (P, P, rows, cols, P, dtype, cols, None)) for rows, cols in sizes]
+    for call, (status, launches), (rows, cols) in zip(calls, launched(recorder, calls), sizes * 2):
+        assert status == OK and launches and fits(launches), (call, launches)
+        vectors = rows * -(-cols // 32) * (4 if dtype == BF16 else 8)
+        assert vectors <= 2 * sum(threads for threads, _, _ in launches) < vectors + 1024 * len(launches)     # two a thread
