@@ -515,7 +515,8 @@ rose_status rose_embedding_lookup(const void *table, int32_t table_dtype, int64_
  * joined in order; scale and an accumulated gradient come in at the end, in fp32, before the one rounding.
  *   workspace    rose_embedding_grad_workspace_bytes, 256-byte aligned; contents before the call do not
  *                matter; calls that share one must be ordered on one stream
- * Errors as rose_embedding_lookup; ROSE_ERR_ARG for a workspace that is too small.
+ * Errors as rose_embedding_lookup; ROSE_ERR_ARG for a workspace that is too small; ROSE_ERR_UNSUPPORTED also for sums that
+ * need 2^26 waves or more (about 2^31 columns, or 2^45 elements of dy).
  */
 rose_status rose_embedding_grad_workspace_bytes(int64_t rows, int64_t cols, int64_t n_tokens, size_t *bytes);
 rose_status rose_embedding_grad(const void *dy, int32_t dy_dtype, int64_t dy_stride, const void *tokens, int32_t token_bytes,
@@ -569,7 +570,8 @@ rose_status rose_grad_clip_norm(const void *const *grad_ptrs, const int64_t *off
  *                       workspace: rose_mx4_linear_workspace_bytes (may be 0: then NULL is fine), 256-byte aligned;
  *                       calls that share one must be ordered on one stream
  * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too
- * small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, or products with k >= 2^24.
+ * small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, products with k >= 2^24, or products of more than 64
+ * rows with 2^23 or more squares of 256 x 256 outputs.
  */
 #define ROSE_MX4_BLOCK 32
 rose_status rose_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t *codes,

@@ -780,6 +780,9 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
 // 8 x 4096 x 4096 in a graph 5.8 and 7.4, 16 x 1024 x 1024 7.2 and 9.5).
 bool mx4_product_takes_bf16(int64_t m, int64_t k) { return m <= kBf16Rows || (m <= 2 * kBf16Rows && k <= 2048); }
 
+// (of 64 rows and fewer any number of weights, see launch_few; of more, 256 x 256 outputs a workgroup of 512 threads where there are that many)
+bool mx4_product_fits(int64_t m, int64_t n, int64_t k) { return k == 0 || m <= 64 || (n + 255) / 256 * ((m + 255) / 256) <= kMostThreads / 512; }
+
 template <int MT, int NT, bool BF16>
 static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     const int64_t n_groups = (a.n + NT * 16 - 1) / (NT * 16), m_groups = (a.m + MT * 16 - 1) / (MT * 16), groups = n_groups * m_groups;
@@ -799,16 +802,24 @@ static int launch_few(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     };
     divide(79 << 10);
     if (groups <= 256 && each > kChunk * 3 / 2) divide(148 << 10);
-    const dim3 grid((unsigned)n_groups, (unsigned)m_groups), block((unsigned)(64 * waves));
-    if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
-    else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, waves * wave_lds, st, a, (int)blocks_of(a.k), (int)each, (uint32_t)wave_lds);
+    // (2^30 rows of the weights are more than a launch has threads for: as many at a time as it has)
+    const int64_t blocks = blocks_of(a.k), most = kMostThreads / (64 * waves) * NT * 16;
+    for (int64_t first = 0; first < a.n; first += most) {
+        Mx4ProductArgs part = a;
+        part.n = a.n - first < most ? a.n - first : most;
+        part.w_codes = a.w_codes + first * blocks * 16;
+        part.w_scales = a.w_scales + first * blocks;
+        part.out = static_cast<char *>(a.out) + first * (out_f32 ? 4 : 2);
+        const dim3 grid((unsigned)((part.n + NT * 16 - 1) / (NT * 16)), (unsigned)m_groups), block((unsigned)(64 * waves));
+        if (out_f32) hipLaunchKernelGGL((mx4_few_kernel<float, MT, NT, BF16>), grid, block, waves * wave_lds, st, part, (int)blocks, (int)each, (uint32_t)wave_lds);
+        else hipLaunchKernelGGL((mx4_few_kernel<bf16_t, MT, NT, BF16>), grid, block, waves * wave_lds, st, part, (int)blocks, (int)each, (uint32_t)wave_lds);
+    }
     return (int)hipGetLastError();
 }
 
 template <int BN, int BM, int WN, int WM, bool WHOLE>
 static int launch_tiles(const Mx4ProductArgs &a, bool out_f32, hipStream_t st) {
     const int64_t n_tiles = (a.n + BN - 1) / BN, m_tiles = (a.m + BM - 1) / BM;
-    if (n_tiles * m_tiles > 0x7FFFFFFF / 8) return (int)hipErrorInvalidValue;
     const dim3 grid((unsigned)(n_tiles * m_tiles)), block(64 * WN * WM);
     if (out_f32) hipLaunchKernelGGL((mx4_tile_kernel<float, BN, BM, WN, WM, WHOLE>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);
     else hipLaunchKernelGGL((mx4_tile_kernel<bf16_t, BN, BM, WN, WM, WHOLE>), grid, block, 0, st, a, (int)blocks_of(a.k), (int)n_tiles, (int)m_tiles);

@@ -45,7 +45,9 @@ rose_status check_mx4(const void *codes, const void *scales, int64_t rows, int64
 
 // What a product can address: a tile of 256 rows within 32 bits of bytes.
 constexpr int64_t kMostProductCols = (int64_t)1 << 24;
-rose_status check_product_cols(int64_t k) { return k < kMostProductCols ? ROSE_OK : ROSE_ERR_UNSUPPORTED; }
+rose_status check_product(int64_t m, int64_t n, int64_t k) {
+    return k < kMostProductCols && rose::mx4_product_fits(m, n, k) ? ROSE_OK : ROSE_ERR_UNSUPPORTED;
+}
 
 rose_status status_of(int hip_error) { return hip_error == 0 ? ROSE_OK : ROSE_ERR_HIP; }
 
@@ -147,7 +149,7 @@ extern "C" rose_status rose_mx4_matmul(const uint8_t *a_codes, const uint8_t *a_
                                        int64_t out_stride, void *stream) {
     ROSE_CHECK(check_mx4(a_codes, a_scales, m, k));
     ROSE_CHECK(check_mx4(w_codes, w_scales, n, k));
-    ROSE_CHECK(check_product_cols(k));
+    ROSE_CHECK(check_product(m, n, k));
     ROSE_CHECK(check_matrix(out, out_dtype, m, n, out_stride));
     rose::Mx4ProductArgs a = {nullptr, 0, a_codes, a_scales, w_codes, w_scales, out, m, n, k, out_stride};
     return status_of(rose::launch_mx4_product(a, out_dtype == ROSE_DTYPE_F32, stream));
@@ -165,7 +167,7 @@ extern "C" rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m
                                        int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream) {
     ROSE_CHECK(check_matrix(x, x_dtype, m, k, x_stride));
     ROSE_CHECK(check_mx4(w_codes, w_scales, n, k));
-    ROSE_CHECK(check_product_cols(k));
+    ROSE_CHECK(check_product(m, n, k));
     ROSE_CHECK(check_matrix(out, out_dtype, m, n, out_stride));
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, linear_workspace(m, k)));
     rose::Mx4ProductArgs a = {nullptr, 0, nullptr, nullptr, w_codes, w_scales, out, m, n, k, out_stride};

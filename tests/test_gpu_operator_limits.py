@@ -97,3 +97,20 @@ def test_a_4_bit_matrix_of_more_vectors_than_a_launch_has_threads_for():
         assert torch.equal(part, small.repeat(100001, 1)[:len(part)])
     del x, q
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_a_product_with_more_rows_of_weights_than_a_launch_has_threads_for(dtype):
+    """One activation of ones, weights of one value a row: sums of whole numbers."""
+    print("case: product with 2^30 rows of weights", dtype, flush=True)
+    room_for(70)
+    n, k = (1 << 30) + 50, 32
+    q = R.Mx4(n, k)
+    q.codes.copy_((torch.arange(n, device="cuda") % 8 * 0x11).to(torch.uint8)[:, None].expand(n, 16))
+    q.scales.fill_(127)
+    out = torch.empty(1, n, dtype=dtype, device="cuda")
+    R.mx4_linear(torch.ones(1, k, dtype=torch.bfloat16, device="cuda"), q, out, R.mx4_linear_workspace(1, n, k))
+    values = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device="cuda").to(dtype) * k
+    assert torch.equal(out[0], values.repeat(n // 8 + 1)[:n])
+    del q, out
+    torch.cuda.empty_cache()

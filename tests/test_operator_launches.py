@@ -137,3 +137,20 @@ def test_4_bit_matrices_of_very_many_vectors(recorder, dtype):
         assert status == OK and launches and fits(launches), (call, launches)
         vectors = rows * -(-cols // 32) * (4 if dtype == BF16 else 8)
         assert vectors <= 2 * sum(threads for threads, _, _ in launches) < vectors + 1024 * len(launches)     # two a thread
+
+
+def test_products_with_very_many_rows_of_weights(recorder):
+    calls = [("rose_mx4_matmul", (P, P, m, P, P, n, k, P, out, n, None))
+             for m in (1, 16, 17, 40, 64) for n in (1, 6143, 1 << 30, MOST) for k in (32, 4096) for out in (BF16, F32)]
+    calls += [("rose_mx4_linear", (P, BF16, m, 33, P, P, n, 33, P, BF16, n, P, 1 << 40, None)) for m in (1, 8) for n in (1 << 30, MOST)]
+    calls += [("rose_mx4_matmul", (P, P, 65, P, P, MOST - 255, 64, P, BF16, MOST, None)), ("rose_mx4_matmul", (P, P, MOST, P, P, MOST, 0, P, F32, MOST, None))]
+    for call, (status, launches) in zip(calls, launched(recorder, calls)):
+        assert status == OK and launches and fits(launches), (call, status, launches)
+
+
+def test_products_of_more_tiles_than_a_launch_holds_queue_nothing(recorder):
+    """No memory holds these; what is refused is refused before the activations are quantised."""
+    calls = [("rose_mx4_linear", (P, F32, m, 64, P, P, n, 64, P, BF16, n, P, 1 << 50, None)) for m, n in ((MOST, MOST), (MOST, 65), (1 << 20, 1 << 20))]
+    calls += [("rose_mx4_matmul", (P, P, m, P, P, n, 64, P, BF16, n, None)) for m, n in ((MOST, MOST), (65, MOST), (1 << 20, 1 << 20))]
+    for call, (status, launches) in zip(calls, launched(recorder, calls)):
+        assert status == UNSUPPORTED and not launches, (call, status, launches)
