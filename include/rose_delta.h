@@ -513,8 +513,9 @@ rose_status rose_embedding_lookup(const void *table, int32_t table_dtype, int64_
  * accumulate == 0: they become zero).  The tokens are sorted by row, equal ones in their order, and the
  * rows of dy that belong together are summed in fp32 in that order, in blocks of fixed size whose sums are then
  * joined in order; scale and an accumulated gradient come in at the end, in fp32, before the one rounding.
- *   workspace    rose_embedding_grad_workspace_bytes, 256-byte aligned; contents before the call do not
- *                matter; calls that share one must be ordered on one stream
+ *   workspace    rose_embedding_grad_workspace_bytes, 256-byte aligned: never fewer for more rows, columns or tokens, so
+ *                that the largest call's does for all; contents before the call do not matter; calls that share one
+ *                must be ordered on one stream
  * Errors as rose_embedding_lookup; ROSE_ERR_ARG for a workspace that is too small; ROSE_ERR_UNSUPPORTED also for sums that
  * need 2^26 waves or more (about 2^31 columns, or 2^45 elements of dy).
  */

@@ -15,7 +15,8 @@ constexpr int64_t kSmallTokens = (int64_t)kSortThreads * kSmallItems;
 constexpr int kTileItems = 2, kTile = kSortThreads * kTileItems;   // tokens that a workgroup of the large sort takes at a time
 constexpr int kMostTiles = 256;
 constexpr int64_t kBlindBytes = 128 << 20;       // of a gradient that is filled with zeros while one workgroup sorts
-constexpr int64_t kShortestRun = 32;            // sorted tokens that are summed in one go
+constexpr int64_t kShortestRun = 32, kLongestRun = 4096;    // sorted tokens that are summed in one go
+constexpr int64_t kBlockWaves = 16384;          // waves that sum, more or less: blocks times the waves of a row
 
 // row of the table that a token names, rows if none
 __device__ __forceinline__ uint32_t row_of(const Tokens &t, int64_t i) {
@@ -538,7 +539,7 @@ struct GradLayout {
     int64_t run, blocks, parts_stride;
     int32_t tiles, subtiles;
     bool small;
-    size_t keys[2], places[2], counts, parts, total;
+    size_t keys[2], places[2], counts, parts;
 };
 int bits_of(int64_t v) {
     int bits = 1;
@@ -570,12 +571,26 @@ GradLayout grad_layout(int64_t rows, int64_t cols, int64_t n) {
     // columns: blocks of 256 tokens 296 us, of 128 264, of 64 261, of 32 275)
     const int64_t waves = (cols + 511) / 512;
     l.run = kShortestRun;
-    while (l.run * 16384 < n * waves && l.run < 4096) l.run *= 2;
+    while (l.run * kBlockWaves < n * waves && l.run < kLongestRun) l.run *= 2;
     l.blocks = (n + l.run - 1) / l.run;
     l.parts_stride = (cols + 7) / 8 * 8;
     l.parts = take(l.blocks > 1 ? (size_t)l.blocks * 2 * (size_t)l.parts_stride * 4 : 0);
-    l.total = at;
     return l;
+}
+// Bytes of it that do for every gradient of at most so many rows, columns and tokens: a program has one for its largest.  What a layout takes
+// does not grow with its tokens and columns everywhere: where blocks double there are half as many of them, and of tiles of the
+// sort the same.  But before the longest run blocks are less than kBlockWaves / waves and one, of at most 512 columns a wave.
+size_t grad_workspace(int64_t rows, int64_t cols, int64_t n) {
+    const size_t list = ((size_t)n * 4 + 255) / 256 * 256, stride = (size_t)((cols + 7) / 8 * 8);
+    size_t bytes = 2 * list;
+    if (!small_sort(rows, n)) {
+        const int64_t tiles = (n + kTile - 1) / kTile;
+        bytes += 2 * list + (size_t)4 * (tiles < kMostTiles ? tiles : kMostTiles) * kBins * 4;
+    }
+    if (n <= kShortestRun) return bytes;
+    const size_t shortest = (size_t)((n + kShortestRun - 1) / kShortestRun) * stride, longest = (size_t)((n + kLongestRun - 1) / kLongestRun) * stride;
+    const size_t between = (size_t)kBlockWaves * 512 + stride, most = between > longest ? between : longest;
+    return bytes + ((shortest < most ? shortest : most) * 2 * 4 + 255) / 256 * 256;
 }
 
 // how the sums go to waves, and what crosses the ends of blocks to workgroups that join it
@@ -603,7 +618,7 @@ bool embedding_grad_fits(int64_t rows, int64_t cols, int64_t n_tokens, bool grad
     return s.groups <= kMostThreads / 64 && s.joins <= kMostThreads / 256;
 }
 
-size_t embedding_grad_workspace(int64_t rows, int64_t cols, int64_t n_tokens) { return grad_layout(rows, cols, n_tokens).total; }
+size_t embedding_grad_workspace(int64_t rows, int64_t cols, int64_t n_tokens) { return grad_workspace(rows, cols, n_tokens); }
 
 int launch_embedding_lookup(const LookupArgs &a, bool table_f32, bool out_f32, void *stream) {
     if (a.tokens.n == 0 || a.cols == 0) return 0;
