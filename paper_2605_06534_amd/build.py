@@ -35,6 +35,17 @@ def _encode_kernel_bodies(asm):
     return out
 
 
+def _assembly(source, extra):
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    with tempfile.TemporaryDirectory() as tmp:
+        s_path = os.path.join(tmp, "kernels.s")
+        subprocess.check_call([hipcc] + DEVICE_FLAGS + list(extra) +
+                              ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "--cuda-device-only", "-S",
+                               os.path.join(CSRC, source), "-o", s_path], stderr=subprocess.DEVNULL)
+        with open(s_path) as f:
+            return f.read()
+
+
 def check_reserved_vgpr(extra=()):
     """The encode kernels keep one VGPR out of the compiler's hands for the ticket that is in flight
     across iterations (see ticket_request in csrc/kernels.hip); the compiler is only ASKED to stay below
@@ -42,15 +53,7 @@ def check_reserved_vgpr(extra=()):
     instructions ever names that register, that no kernel exceeds its register budget and that none
     spills: a toolchain or flag change that broke the reservation would hand out corrupt tickets.
     Raises RuntimeError on a violation."""
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    with tempfile.TemporaryDirectory() as tmp:
-        s_path = os.path.join(tmp, "kernels.s")
-        subprocess.check_call([hipcc] + DEVICE_FLAGS + list(extra) +
-                              ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "--cuda-device-only", "-S",
-                               os.path.join(CSRC, "kernels.hip"), "-o", s_path], stderr=subprocess.DEVNULL)
-        with open(s_path) as f:
-            asm = f.read()
-    bodies = _encode_kernel_bodies(asm)
+    bodies = _encode_kernel_bodies(_assembly("kernels.hip", extra))
     elements = bodies.pop(_ELEMENTS, None)
     if set(bodies) != {(f, r, a) for f in (0, 1) for r in (0, 1) for a in (0, 1)}:
         raise RuntimeError("not all eight encode kernels were found in the assembly: %s" % sorted(bodies))
@@ -87,12 +90,36 @@ def _check_body(what, body, reg):
         raise RuntimeError("%s: the ticket routines are missing (%d uses of v%d)" % (what, uses, reg))
 
 
+def check_m0(extra=()):
+    """The products' loads to LDS set M0 in hand-written assembly (load_to_lds in csrc/mx4.hip).  It is not a register that the
+    compiler lets assembly name as clobbered, so a use of its own that it sets up before such a load would find another
+    value.  Make sure that nothing outside the hand-written assembly touches M0.  Raises RuntimeError on a violation."""
+    _check_m0(_assembly("mx4.hip", extra))
+
+
+def _check_m0(asm):
+    by_hand, sets = False, 0
+    for line in asm.splitlines():
+        if "#ASMSTART" in line or "#ASMEND" in line:
+            by_hand = "#ASMSTART" in line
+            continue
+        code = line.split(";")[0].strip()
+        # by name, or by instructions that always read it: indexed moves, messages, counters, loads to LDS
+        if re.search(r"\bm0\b|^s_movrel|^v_movrel|^s_set_gpr_idx|^s_sendmsg|^ds_gws|^ds_ordered|\blds$", code):
+            if not by_hand:
+                raise RuntimeError("the compiler uses M0: %s" % code)
+            sets += code.startswith("s_mov_b32 m0")
+    if not sets:
+        raise RuntimeError("the loads to LDS are missing")
+
+
 def build(verbose=False, extra=(), out=None, check=True):
-    """Compile the library; with check (the default) also verify the reserved-register assumption of
-    the encode kernels and refuse to leave a library behind that breaks it."""
+    """Compile the library; with check (the default) also verify what its hand-written assembly assumes
+    of the compiler and refuse to leave a library behind that breaks it."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     if check:
         check_reserved_vgpr(extra)
+        check_m0(extra)
     cmd = [hipcc] + DEVICE_FLAGS + ["-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     cmd += list(extra)
     for s in SOURCES:

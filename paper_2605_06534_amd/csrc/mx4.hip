@@ -237,7 +237,8 @@ __device__ __forceinline__ void put_lds(uint32_t at, T v) {
 }
 
 // 16 bytes a lane from a resource to LDS, lane after lane from `to` on.  Written in assembly because the compiler, told of a
-// load that writes LDS, waits for it before every read of LDS; here the kernel waits (load_wait) where it has to.
+// load that writes LDS, waits for it before every read of LDS; here the kernel waits where it has to.
+// (M0 cannot be named as clobbered, the compiler has it reserved; the build makes sure that it makes no use of M0 itself.)
 __device__ __forceinline__ void load_to_lds(uint32_t to, u32x4 resource, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(resource) : "memory");
 }
