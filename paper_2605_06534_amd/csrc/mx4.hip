@@ -778,8 +778,13 @@ int launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
 }
 
 // Twice as many rows where the columns are few: a launch less (8 x 1024 x 1024 9.4 us, 6.7 so, as part of a graph 7.1 and 6.6;
-// 8 x 4096 x 4096 in a graph 5.8 and 7.4, 16 x 1024 x 1024 7.2 and 9.5).
-bool mx4_product_takes_bf16(int64_t m, int64_t k) { return m <= kBf16Rows || (m <= 2 * kBf16Rows && k <= 2048); }
+// 8 x 4096 x 4096 in a graph 5.8 and 7.4, 16 x 1024 x 1024 7.2 and 9.5).  Not with many rows of weights: each workgroup quantises
+// all activations again, and where there are more workgroups than run at once that time adds up (8 x 32768 x 1024 10.1 us, 8.3 so,
+// and 8 x 16384 x 2048 10.1 and 8.3; but 8 x 65536 x 512 10.9 and 13.6, 8 x 32768 x 2048 11.7 and 14.1, 8 x 151936 x 2048 29.3
+// and 41.6.  Four rows and fewer gain or lose a tenth with any number: 4 x 151936 x 1024 18.0 and 17.8, x 4096 63.7 and 69.6).
+bool mx4_product_takes_bf16(int64_t m, int64_t n, int64_t k) {
+    return m <= kBf16Rows || (m <= 2 * kBf16Rows && k <= 2048 && n <= 32768 && n * k <= 1 << 25);
+}
 
 // (of 64 rows and fewer any number of weights, see launch_few; of more, 256 x 256 outputs a workgroup of 512 threads where there are that many)
 bool mx4_product_fits(int64_t m, int64_t n, int64_t k) { return k == 0 || m <= 64 || (n + 255) / 256 * ((m + 255) / 256) <= kMostThreads / 512; }

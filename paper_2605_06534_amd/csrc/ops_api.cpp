@@ -172,7 +172,7 @@ extern "C" rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, linear_workspace(m, k)));
     rose::Mx4ProductArgs a = {nullptr, 0, nullptr, nullptr, w_codes, w_scales, out, m, n, k, out_stride};
     if (m == 0 || n == 0) return ROSE_OK;
-    if (x_dtype == ROSE_DTYPE_BF16 && rose::mx4_product_takes_bf16(m, k)) {
+    if (x_dtype == ROSE_DTYPE_BF16 && rose::mx4_product_takes_bf16(m, n, k)) {
         a.x = x;
         a.x_stride = x_stride;
     } else {

@@ -69,8 +69,8 @@ struct Mx4ProductArgs {
     void *out;
     int64_t m, n, k, out_stride;
 };
-// whether a product of this many rows quantises bf16 activations by itself
-bool mx4_product_takes_bf16(int64_t m, int64_t k);
+// whether a product of this size quantises bf16 activations by itself
+bool mx4_product_takes_bf16(int64_t m, int64_t n, int64_t k);
 bool mx4_product_fits(int64_t m, int64_t n, int64_t k);        // into launches
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream);
 

@@ -154,3 +154,12 @@ def test_products_of_more_tiles_than_a_launch_holds_queue_nothing(recorder):
     calls += [("rose_mx4_matmul", (P, P, m, P, P, n, 64, P, BF16, n, None)) for m, n in ((MOST, MOST), (65, MOST), (1 << 20, 1 << 20))]
     for call, (status, launches) in zip(calls, launched(recorder, calls)):
         assert status == UNSUPPORTED and not launches, (call, status, launches)
+
+
+def test_activations_are_not_quantised_again_for_very_many_rows_of_weights(recorder):
+    """Five to eight rows: by the product itself up to where that costs more than a launch, once for all beyond."""
+    alone = [(8, 1024, 1024), (8, 32768, 1024), (8, 16384, 2048), (5, 32768, 33), (4, 151936, 2048), (1, 1 << 20, 8192)]
+    before = [(8, 32769, 1024), (8, 32769, 33), (8, 16400, 2048), (5, 151936, 2048), (8, 1024, 2049), (9, 1024, 1024)]
+    calls = [("rose_mx4_linear", (P, BF16, m, k, P, P, n, k, P, BF16, n, P, 1 << 40, None)) for m, n, k in alone + before]
+    for (status, launches), size, want in zip(launched(recorder, calls), alone + before, [1] * len(alone) + [2] * len(before)):
+        assert status == OK and len(launches) == want, (size, launches)
