@@ -473,6 +473,11 @@ def _grads(grad_tab, offsets, what, *others):
     return grad_tab.data_ptr(), offsets.data_ptr(), grad_tab.numel()
 
 
+def _holds_norm(norm):
+    # (an empty tensor's address is null, which would say that no norm is wanted)
+    return norm is None or (norm.dtype == torch.float32 and norm.numel() > 0)
+
+
 def grad_sum_squares(grad_tab, offsets, total, dtype, out, ws, stream=None):
     """out (one float64): sum of the squares of all elements of the tensors of a pointer table; null pointers are left out."""
     gp, fp, n = _grads(grad_tab, offsets, "grad_sum_squares", out, ws)
@@ -484,8 +489,8 @@ def grad_sum_squares(grad_tab, offsets, total, dtype, out, ws, stream=None):
 def grad_clip(grad_tab, offsets, total, dtype, out_tab, sum_squares, max_norm, norm=None, stream=None):
     """Scales the tensors down to a norm of max_norm, given the sum of all squares; out_tab may be grad_tab."""
     gp, fp, n = _grads(grad_tab, offsets, "grad_clip", out_tab, sum_squares, norm)
-    _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and sum_squares.dtype == torch.float64 and
-          (norm is None or norm.dtype == torch.float32), "grad_clip")
+    _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and sum_squares.dtype == torch.float64 and sum_squares.numel() > 0 and
+          _holds_norm(norm), "grad_clip")
     _check(_lib.rose_grad_clip(gp, fp, n, total, _dtype(dtype, "grad_clip"), out_tab.data_ptr(), sum_squares.data_ptr(),
                                max_norm, norm.data_ptr() if norm is not None else None, _stream(stream)), "grad_clip")
 
@@ -493,7 +498,7 @@ def grad_clip(grad_tab, offsets, total, dtype, out_tab, sum_squares, max_norm, n
 def grad_clip_norm(grad_tab, offsets, total, dtype, out_tab, max_norm, norm, ws, stream=None):
     """grad_sum_squares and grad_clip in one call, for a rank that holds everything."""
     gp, fp, n = _grads(grad_tab, offsets, "grad_clip_norm", out_tab, norm, ws)
-    _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and (norm is None or norm.dtype == torch.float32), "grad_clip_norm")
+    _same(out_tab.numel() == n and out_tab.dtype == torch.int64 and _holds_norm(norm), "grad_clip_norm")
     _check(_lib.rose_grad_clip_norm(gp, fp, n, total, _dtype(dtype, "grad_clip_norm"), out_tab.data_ptr(), max_norm,
                                     norm.data_ptr() if norm is not None else None, ws.data_ptr(),
                                     ws.numel() * ws.element_size(), _stream(stream)), "grad_clip_norm")

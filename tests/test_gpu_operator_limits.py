@@ -114,3 +114,16 @@ def test_a_product_with_more_rows_of_weights_than_a_launch_has_threads_for(dtype
     assert torch.equal(out[0], values.repeat(n // 8 + 1)[:n])
     del q, out
     torch.cuda.empty_cache()
+
+
+def test_places_for_a_norm_that_hold_none_are_refused():
+    """The address of an empty tensor is null, as where no norm is asked for."""
+    print("case: empty places for results", flush=True)
+    x, s, empty = torch.ones(8, device="cuda"), torch.ones(1, dtype=torch.float64, device="cuda"), torch.empty(0, device="cuda")
+    tab, offsets = R.ptr_table([x]), R.offset_table([8])
+    for call in (lambda: R.grad_clip(tab, offsets, 8, torch.float32, tab, s, 0.5, empty),
+                 lambda: R.grad_clip(tab, offsets, 8, torch.float32, tab, s[:0], 0.5),
+                 lambda: R.grad_clip_norm(tab, offsets, 8, torch.float32, tab, 0.5, empty, R.grad_workspace())):
+        with pytest.raises(R.RoseError):
+            call()
+    assert (x == 1).all()
