@@ -31,7 +31,7 @@ rose_status check_workspace(const void *workspace, size_t bytes, size_t need) {
 }
 
 rose_status check_grads(const void *const *ptrs, const int64_t *offsets, int32_t n_tensors, int64_t total, int32_t dtype) {
-    if (!ptrs || !offsets || n_tensors < 0 || total < 0 || !known(dtype)) return ROSE_ERR_ARG;
+    if ((n_tensors > 0 && !ptrs) || !offsets || n_tensors < 0 || total < 0 || !known(dtype)) return ROSE_ERR_ARG;
     return aligned(ptrs, 8) && aligned(offsets, 8) ? ROSE_OK : ROSE_ERR_ALIGN;
 }
 
@@ -113,7 +113,7 @@ extern "C" rose_status rose_grad_clip(const void *const *grad_ptrs, const int64_
                                       int32_t dtype, void *const *out_ptrs, const double *sum, float max_norm, float *norm,
                                       void *stream) {
     ROSE_CHECK(check_grads(grad_ptrs, offsets, n_tensors, total, dtype));
-    if (!out_ptrs || !sum || !(max_norm >= 0.f)) return ROSE_ERR_ARG;
+    if ((n_tensors > 0 && !out_ptrs) || !sum || !(max_norm >= 0.f)) return ROSE_ERR_ARG;
     if (!aligned(out_ptrs, 8) || !aligned(sum, 8) || !aligned(norm, 4)) return ROSE_ERR_ALIGN;
     rose::GradArgs a = {grad_ptrs, out_ptrs, offsets, n_tensors, 0, nullptr, 0, const_cast<double *>(sum), max_norm, norm};
     return status_of(rose::launch_grad_clip(a, total, dtype == ROSE_DTYPE_F32, stream));
@@ -123,7 +123,7 @@ extern "C" rose_status rose_grad_clip_norm(const void *const *grad_ptrs, const i
                                            int64_t total, int32_t dtype, void *const *out_ptrs, float max_norm, float *norm,
                                            void *workspace, size_t workspace_bytes, void *stream) {
     ROSE_CHECK(check_grads(grad_ptrs, offsets, n_tensors, total, dtype));
-    if (!out_ptrs || !(max_norm >= 0.f)) return ROSE_ERR_ARG;
+    if ((n_tensors > 0 && !out_ptrs) || !(max_norm >= 0.f)) return ROSE_ERR_ARG;
     if (!aligned(out_ptrs, 8) || !aligned(norm, 4)) return ROSE_ERR_ALIGN;
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, ROSE_GRAD_WORKSPACE_BYTES));
     rose::GradArgs a = {grad_ptrs, out_ptrs, offsets, n_tensors, 0, static_cast<double *>(workspace), 0, nullptr, max_norm, norm};

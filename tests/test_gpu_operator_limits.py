@@ -127,3 +127,15 @@ def test_places_for_a_norm_that_hold_none_are_refused():
         with pytest.raises(R.RoseError):
             call()
     assert (x == 1).all()
+
+
+def test_the_norm_of_no_tensors_is_zero():
+    print("case: no tensors", flush=True)
+    none, offsets = R.ptr_table([]), R.offset_table([])
+    s, norm = torch.full((1,), 5.0, dtype=torch.float64, device="cuda"), torch.full((1,), 5.0, device="cuda")
+    R.grad_sum_squares(none, offsets, 0, torch.float32, s, R.grad_workspace())
+    R.grad_clip(none, offsets, 0, torch.float32, none, s, 1.0, norm)
+    assert s.item() == 0 and norm.item() == 0
+    norm.fill_(5.0)
+    R.grad_clip_norm(none, offsets, 0, torch.bfloat16, none, 1.0, norm, R.grad_workspace())
+    assert norm.item() == 0

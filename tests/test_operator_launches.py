@@ -163,3 +163,11 @@ def test_activations_are_not_quantised_again_for_very_many_rows_of_weights(recor
     calls = [("rose_mx4_linear", (P, BF16, m, k, P, P, n, k, P, BF16, n, P, 1 << 40, None)) for m, n, k in alone + before]
     for (status, launches), size, want in zip(launched(recorder, calls), alone + before, [1] * len(alone) + [2] * len(before)):
         assert status == OK and len(launches) == want, (size, launches)
+
+
+def test_no_tensors_need_no_table(recorder):
+    """An empty table's address is null; the offsets still say that there is nothing."""
+    W = binding.GRAD_WORKSPACE_BYTES
+    calls = [("rose_grad_sum_squares", (None, P, 0, 0, F32, P, P, W, None)), ("rose_grad_clip", (None, P, 0, 0, F32, None, P, 1.0, P, None)),
+             ("rose_grad_clip_norm", (None, P, 0, 0, BF16, None, 1.0, P, P, W, None))]
+    assert all(status == OK and launches for status, launches in launched(recorder, calls))
