@@ -485,8 +485,9 @@ rose_status rose_bw_probe_lines(void *dst, size_t bytes, uint32_t touched_per_2_
  * see are returned before anything is queued.  Sizes of zero are allowed where nothing is then read.
  * Matrices are row-major with rows `stride` elements apart (stride >= columns; what lies between is
  * neither read nor written); pointers need the alignment of their element type only, unless stated.
- * Every result is a function of the inputs alone: two calls give the same bits.  (Of the norm of gradients the 64-bit
- * sum's last bits also depend on how the tensors lie to lines of 128 bytes.)
+ * Every result is a function of the inputs alone, their sizes among them: two calls give the same bits.  (Of
+ * the norm of gradients the 64-bit sum's last bits also depend on `total` and on how the tensors lie to lines of
+ * 128 bytes.)
  * ---------------------------------------------------------------------------------------------
  */
 typedef enum {
@@ -532,7 +533,8 @@ rose_status rose_embedding_grad(const void *dy, int32_t dy_dtype, int64_t dy_str
  *                rose_grad_sum_squares (rose_plan_tensor_is_read says who sends, and may count, which).
  *   offsets      DEVICE array of n_tensors + 1 int64: offsets[0] = 0, tensor t has offsets[t+1] - offsets[t] elements
  *   total        offsets[n_tensors], for the host to size the launch by (a wrong value costs speed, nothing else)
- *   workspace    ROSE_GRAD_WORKSPACE_BYTES, 256-byte aligned; contents before the call do not matter
+ *   workspace    ROSE_GRAD_WORKSPACE_BYTES, 256-byte aligned; contents before the call do not matter; calls that share one
+ *                must be ordered on one stream
  * rose_grad_sum_squares   *sum (device, 8-byte aligned) = sum of all squares, formed and added in 64 bits: ranks that
  *                         hold different tensors or shards add their sums up before they clip.
  * rose_grad_clip          out = grad * min(1, max_norm / (norm + 1e-6)), norm = sqrt(*sum), rounded once to the
@@ -568,8 +570,11 @@ rose_status rose_grad_clip_norm(const void *const *grad_ptrs, const int64_t *off
  * rose_mx4_matmul       out[i][j] = sum over k of a[i][k] * w[j][k]: a is m x k (activations), w is n x k (a stored
  *                       [out, in] matrix), both quantised; products are exact, sums fp32, rounded once to out's type
  * rose_mx4_linear       the same with a quantised on the way from x (m x k, bf16 or fp32).
- *                       workspace: rose_mx4_linear_workspace_bytes (may be 0: then NULL is fine), 256-byte aligned;
- *                       calls that share one must be ordered on one stream
+ *                       workspace: rose_mx4_linear_workspace_bytes (may be 0: then NULL is fine), 256-byte aligned,
+ *                       wanted also for sizes whose few activations go without it; calls that share one must be ordered
+ *                       on one stream
+ * How a sum is divided depends on m, n and k: a row of activations alone and the same row among others may differ in the last
+ * bits of its fp32 sums.
  * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too
  * small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, products with k >= 2^24, or products of more than 64
  * rows with 2^23 or more squares of 256 x 256 outputs.

@@ -668,9 +668,10 @@ int launch_embedding_grad(const EmbeddingGradArgs &a, bool dy_f32, bool grad_f32
     s.width = (s.bits + s.passes - 1) / s.passes;
     s.tiles = l.tiles;
     s.subtiles = l.subtiles;
-    // Zeros for rows without tokens: as much as the sort takes the time of goes blindly with it (the last rows, of which tokens
-    // name the fewest), the rest in the launch of the sums, past the rows that have some.  (All of it with the sort: 8191 tokens
-    // and a gradient of 524 MB 133 us, 114 this way.)
+    // Zeros for rows without tokens: kBlindBytes, about what 8191 tokens' sort takes the time of, go blindly with it (the last rows: in a
+    // vocabulary in order of frequency tokens name the fewest of those; a row that has some is written again by the sums), the
+    // rest in the launch of the sums, past the rows that have some.  (All of it with the sort: 8191 tokens and a gradient of
+    // 524 MB 133 us, 114 this way.)
     int64_t fills = 0, fill_later = 0;
     if (!a.accumulate) {
         const int64_t size = grad_f32 ? 4 : 2, row_bytes = a.cols * size;

@@ -23,7 +23,7 @@ __device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_
 
 // -------------------------------------------------------------------------------------------------
 // quantisation: four lanes a block of bf16, eight of fp32, 16 bytes each, kUnits times so many a lane.  HBM traffic bounds it
-// and its inverse: 151936 x 4096 bf16 247 us and 243, 6.4 TB/s (fp32 6.3 and 5.9); 6912 x 5120 17 us and 14
+// and its inverse: 151936 x 4096 bf16 249 us and 242, 6.3 TB/s and 6.5 (fp32 6.4 and 5.9); 6912 x 5120 18 us and 16
 // -------------------------------------------------------------------------------------------------
 constexpr int kUnits = 2;
 
@@ -206,14 +206,16 @@ __device__ __forceinline__ f32x4 product(u32x4 w, uint32_t w_scale, u32x4 a, uin
 // needs for its quarter of four instructions in one word, of which the instruction picks a byte.
 // WHOLE, for rows of whole groups of 32 blocks (four slots): a thread loads both halves of a group's scales together, so that
 // the second comes from the line that the first one brought.  That halves the requests for scales, which are half as many as
-// those for codes otherwise: 16384 x 6912 x 5120 302 us, 291 so; 256 x 19008 x 5120 in tiles of 128 26.4, 25.4; 512 x 4096 x 4096
-// in tiles of 64 12.9, 12.0.  (By loads to LDS and a byte for each instruction: the same in the small tiles, in the large one
-// there are no registers for the addresses, 355.)
-// 16384 x 6912 x 5120: 291 us, 3980 TFLOP/s (the simplest kernel: 7480 us; outputs written in half lines that caches keep 342);
-// 4096 x 4096 x 4096: 36 us, 3830.  What bounds it: either the loads from memory or the multiplications alone take three
-// quarters of that, and 7 us of each round of 256 tiles are outputs that leave and first slots that come, which nothing overlaps
+// those for codes otherwise (products alone, one behind the other, without and with: 16384 x 6912 x 5120 284 and 275 us; 256 x 19008
+// x 5120 in tiles of 128 28.2 and 27.3; 512 x 4096 x 4096 in tiles of 64 12.9 and 12.0).  (By loads to LDS and a byte for each
+// instruction: the same in the small tiles, in the large one there are no registers for the addresses, 355.)
+// 16384 x 6912 x 5120 behind the quantisation of its activations: 304 us, 3810 TFLOP/s (the simplest kernel: 7480 us; outputs written
+// in half lines that caches keep 342 where these took 305); 4096 x 4096 x 4096 alone: 35 us, 3920.  What bounds it: the matrix units are busy half of
+// the time, at the 1.9 GHz that the chip runs at then.  Either the loads from memory or the multiplications alone take 55 to 62 % of a
+// slot's time, and 7 us of each round of 256 tiles are outputs that leave and first slots that come, which nothing overlaps
 // where one workgroup fills a CU.  (Workgroups that take tile after tile and ask for the next one's first slots before they
-// write need more registers than there are: 380 us.)
+// write need more registers than there are: 380 us.)  The tiles of 256 take all 256 registers and spill: two that are read again
+// behind the main loop, and with WHOLE a third, which is read again once in every four slots of the loop.
 constexpr uint32_t kOutside = 0xFFFFF000u;      // an offset behind every resource: such loads give zeros
 
 __device__ __forceinline__ u32x4 resource_of(const uint8_t *p, int64_t bytes) {
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void mx4_tile_kernel(Mx4ProductArg
 // reads, without barriers.  (Loads straight to registers, each lane its row's: 64 lines an instruction where eight lanes of
 // a row next to each other make 8; 6912 x 5120 took 10.1 us that way.)
 // With BF16 the wave quantises the activations that it needs by itself, a chunk of columns ahead of the multiplications.
-// 1 x 6912 x 5120: 6.0 us, of which 2.6 are the least launch; 1 x 151936 x 4096 61 us, 5.4 TB/s.
+// 1 x 6912 x 5120: 5.9 us, of which 2.6 are the least launch; 1 x 151936 x 4096 59 us, 5.6 TB/s.
 typedef uint64_t __attribute__((aligned(2))) u64_any2;
 
 constexpr int kRing = 3;                        // steps of 256 columns on the way
@@ -852,8 +854,8 @@ int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream) {
     const int64_t across = (a.n + 31) / 32 * ((a.m + 63) / 64);
     if (across <= 256 && a.k > 2048) return launch_few<4, 2, false>(a, out_f32, st);
     // 256 x 256 tiles move half of what 128 x 128 ones do but fill a CU each; the smaller ones, two a CU, where there are few
-    // (256 x 19008 x 5120: 38.5 us with the large ones, 25.3 with the small; 4096 x 4096 x 4096: 37 and 45), and tiles of 64
-    // where also those leave CUs idle (256 x 6912 x 5120 18.6 us, 14.4 with 64; 512 x 6912 x 5120 18.9 and 18.7).
+    // (256 x 19008 x 5120: 37.7 us with the large ones, 27.3 with the small; 4096 x 4096 x 4096: 35 and 43), and tiles of 64
+    // where also those leave CUs idle (256 x 6912 x 5120 18.6 us, 14.2 with 64; 512 x 6912 x 5120 18.9 and 18.7).
     auto tiles = [&](int64_t b) { return ((a.n + b - 1) / b) * ((a.m + b - 1) / b); };
     const bool whole = a.k % 1024 == 0;
     if (tiles(256) >= 192) return whole ? launch_tiles<256, 256, 4, 2, true>(a, out_f32, st) : launch_tiles<256, 256, 4, 2, false>(a, out_f32, st);

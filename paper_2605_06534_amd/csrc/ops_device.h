@@ -124,7 +124,7 @@ __device__ __forceinline__ void store(T *p, int n, const float (&f)[W]) {
 
 // The vectors of a matrix, so many elements each, row after row, in groups of PER neighbouring ones, a group a workgroup: so that no lane is
 // idle whatever the columns are.  (A workgroup a group, not workgroups that walk: stores count as loads do among what a wave waits
-// for, and one that goes on waits for its stores.  Quantising 151936 x 4096 247 us, 357 with 2048 workgroups that ask ahead.)
+// for, and one that goes on waits for its stores.  Quantising 151936 x 4096 249 us, 357 with 2048 workgroups that ask ahead.)
 struct Rows {
     int64_t vectors;                            // of all rows together
     uint64_t reciprocal64;                      // 2^64 over the vectors of a row, rounded up
