@@ -90,20 +90,32 @@ def _check_body(what, body, reg):
         raise RuntimeError("%s: the ticket routines are missing (%d uses of v%d)" % (what, uses, reg))
 
 
-def check_m0(extra=()):
-    """The products' loads to LDS set M0 in hand-written assembly (load_to_lds in csrc/mx4.hip).  It is not a register that the
-    compiler lets assembly name as clobbered, so a use of its own that it sets up before such a load would find another
-    value.  Make sure that nothing outside the hand-written assembly touches M0.  Raises RuntimeError on a violation."""
-    _check_m0(_assembly("mx4.hip", extra))
+def check_loads_to_lds(extra=()):
+    """What the products' hand-written loads to LDS (load_to_lds in csrc/mx4.hip) assume of the compiler.  They set M0, which is
+    not a register that the compiler lets assembly name as clobbered, so a use of its own that it sets up before such a load would
+    find another value: make sure that nothing outside the hand-written assembly touches M0.  And they read scalar registers,
+    which takes five wait states after a vector instruction has written them, inside assembly that the compiler does not
+    look into: make sure that no such write is nearer.  Raises RuntimeError on a violation."""
+    asm = _assembly("mx4.hip", extra)
+    _check_m0(asm)
+    _check_scalar_operands(asm)
 
 
-def _check_m0(asm):
-    by_hand, sets = False, 0
+def _by_hand(asm):
+    """(whether it is hand-written, instruction or label) of the lines of an assembly"""
+    by_hand = False
     for line in asm.splitlines():
         if "#ASMSTART" in line or "#ASMEND" in line:
             by_hand = "#ASMSTART" in line
             continue
         code = line.split(";")[0].strip()
+        if code and (code.endswith(":") or not code.startswith(".")):
+            yield by_hand, code
+
+
+def _check_m0(asm):
+    sets = 0
+    for by_hand, code in _by_hand(asm):
         # by name, or by instructions that always read it: indexed moves, messages, counters, loads to LDS
         if re.search(r"\bm0\b|^s_movrel|^v_movrel|^s_set_gpr_idx|^s_sendmsg|^ds_gws|^ds_ordered|\blds$", code):
             if not by_hand:
@@ -113,13 +125,60 @@ def _check_m0(asm):
         raise RuntimeError("the loads to LDS are missing")
 
 
+_SCALAR_WAIT = 5
+
+
+def _scalars(operand):
+    out = set()
+    for m in re.finditer(r"\bs(\d+)\b|\bs\[(\d+):(\d+)\]", operand):
+        out.update(range(int(m.group(1) or m.group(2)), int(m.group(1) or m.group(3)) + 1))
+    return out
+
+
+def _check_scalar_operands(asm):
+    code = list(_by_hand(asm))
+    # wait states since a vector instruction wrote each scalar register, where that is fewer than it takes; where branches meet the fewest
+    at_label, changed = {}, True
+
+    def meet(label, since):
+        there = at_label.setdefault(label, {})
+        nearer = {s: n for s, n in since.items() if n < there.get(s, _SCALAR_WAIT)}
+        there.update(nearer)
+        return bool(nearer)
+
+    while changed:
+        changed, since = False, {}
+        for by_hand, line in code:
+            if line.endswith(":"):
+                changed |= meet(line[:-1], since)
+                since = dict(at_label[line[:-1]])
+                continue
+            name, _, operands = line.partition(" ")
+            operands = operands.split(",")
+            if by_hand and name.startswith("buffer_load"):
+                near = [s for s in set().union(*map(_scalars, operands)) if s in since]
+                if near:
+                    raise RuntimeError("a vector instruction wrote s%d too shortly before: %s" % (near[0], line))
+            wait = int(operands[0], 0) + 1 if name == "s_nop" else 1
+            since = {s: n + wait for s, n in since.items() if n + wait < _SCALAR_WAIT}
+            if name.startswith("v_"):
+                # (some have a carry or a flag for their second result)
+                written = _scalars(operands[0]) | (_scalars(operands[1]) if len(operands) > 1 and re.search(r"_co_|div_scale|mad_[iu]64", name) else set())
+                since.update((s, 0) for s in written)
+            branch = re.match(r"s_c?branch\S*$", name)
+            if branch:
+                changed |= meet(operands[0].strip(), since)
+                if name == "s_branch":
+                    since = {}
+
+
 def build(verbose=False, extra=(), out=None, check=True):
     """Compile the library; with check (the default) also verify what its hand-written assembly assumes
     of the compiler and refuse to leave a library behind that breaks it."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     if check:
         check_reserved_vgpr(extra)
-        check_m0(extra)
+        check_loads_to_lds(extra)
     cmd = [hipcc] + DEVICE_FLAGS + ["-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     cmd += list(extra)
     for s in SOURCES:
