@@ -368,7 +368,7 @@ def _kernels(s):
     else:
         if "weights" not in s:
             s["weights"] = R.Adapters(s["down"], s["up"], s["scales"])
-            s["ws"] = R.adapter_linear_workspace(c["m"], c["rank"])
+            s["ws"] = R.adapter_linear_workspace(c["m"], s["weights"])
         R.adapter_linear(s["x"], s["weights"], s["chosen"], s["out"], s["ws"])
 
 
