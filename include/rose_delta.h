@@ -592,6 +592,125 @@ rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m, int64_t x
                             const uint8_t *w_scales, int64_t n, int64_t k, void *out, int32_t out_dtype, int64_t out_stride,
                             void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Operators between hidden states and tokens, under the same conventions.
+ * ---------------------------------------------------------------------------------------------
+ */
+
+/*
+ * Layer norm of rows, and its gradient.
+ *   out = (x - mean) * rstd * weight + bias;  rstd = 1 / sqrt(mean of (x - mean)^2 + eps)
+ *   center       nonzero: mean is the row's; 0: it is zero (root mean square norm), and a bias is refused
+ *   weight, bias cols elements of weight_dtype; bias may be NULL
+ *   mean, rstd   device, one fp32 a row, what the gradient needs; either may be NULL
+ * Sums are fp32, of deviations from the mean; one rounding to out's type.  out may be x (same address, type and stride).  Rows
+ * with an infinity or a NaN follow the formula.
+ * Its gradient for g = dy * weight, xhat = (x - mean) * rstd:
+ *   dx      = rstd * (g - mean of g - xhat * mean of (g * xhat));  mean == NULL: not centred, without the mean of g
+ *   dweight = sum over the rows of dy * xhat, dbias = sum over the rows of dy  (accumulate != 0: added to what is there)
+ *   dx           of x's type; may be x, or dy where that has the same type (same address and stride)
+ *   dweight, dbias  cols fp32; either may be NULL.  No rows: zeros, or left alone.
+ *   workspace    rose_layer_norm_grad_workspace_bytes, 256-byte aligned: never fewer for more rows or columns; contents before the
+ *                call do not matter; calls that share one must be ordered on one stream
+ * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, an eps that is negative or NaN, a
+ * workspace that is too small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns.
+ */
+rose_status rose_layer_norm(const void *x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t x_stride, const void *weight,
+                            const void *bias, int32_t weight_dtype, float eps, int32_t center, void *out, int32_t out_dtype,
+                            int64_t out_stride, float *mean, float *rstd, void *stream);
+rose_status rose_layer_norm_grad_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes);
+rose_status rose_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_stride, const void *x, int32_t x_dtype,
+                                 int64_t x_stride, int64_t rows, int64_t cols, const void *weight, int32_t weight_dtype,
+                                 const float *mean, const float *rstd, void *dx, int64_t dx_stride, float *dweight,
+                                 float *dbias, int32_t accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * What a student learns from the top logits that a teacher kept of each row: the divergence of q = softmax(logits / T) over all columns
+ * from p = softmax(teacher / T) over the row's entries, and its gradient:
+ *   loss = sum over the entries of p * (log p - log q);  lse = log of the sum of exp(logits / T);  d_logits = d_loss * (q - p) / T
+ *   logits       rows x cols, the whole vocabulary, bf16 or fp32
+ *   ids, teacher [rows][top]: the entries' columns (int32 or int64, id_bytes 4 or 8) and logits (fp32), in any order.  An id outside
+ *                0 .. cols - 1 or a logit of minus infinity says that there is no entry (rows with fewer than `top`).  A row without
+ *                any has loss 0 and a gradient of zeros, whatever its logits and d_loss are (a prompt's tokens, padding).  A column
+ *                that is named twice counts with both its probabilities.
+ *   loss, lse, d_loss  one fp32 a row
+ *   d_logits     of the logits' type; may be logits (same address and stride)
+ *   workspace    rose_distill_workspace_bytes, 256-byte aligned: never fewer for more rows or columns; contents before the call do not
+ *                matter; calls that share one must be ordered on one stream
+ * rose_distill_loss       loss and lse
+ * rose_distill_grad       d_logits, from the lse that the loss left behind
+ * rose_distill_loss_grad  all of them in one call, d_loss being known beforehand (1 / number of tokens)
+ * Sums over the columns are fp32, each relative to the largest logit of what it sums; the entries' p and the loss are formed in 64 bits, one
+ * rounding each.  Columns of minus infinity have q = 0 (an entry there makes the loss infinite); rows whose logits hold a NaN or an
+ * infinity, or minus infinities only, have no number for loss and gradient.
+ * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a temperature that is not above zero or
+ * infinite, a workspace that is too small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^22 or more rows, 2^31 or more columns, or more than
+ * ROSE_DISTILL_MOST_TOP entries.
+ */
+#define ROSE_DISTILL_MOST_TOP 1024
+rose_status rose_distill_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes);
+rose_status rose_distill_loss(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids,
+                              int32_t id_bytes, const float *teacher, int64_t top, double temperature, float *loss, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream);
+rose_status rose_distill_grad(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids,
+                              int32_t id_bytes, const float *teacher, int64_t top, double temperature, const float *lse,
+                              const float *d_loss, void *d_logits, int64_t d_stride, void *stream);
+rose_status rose_distill_loss_grad(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids,
+                                   int32_t id_bytes, const float *teacher, int64_t top, double temperature, const float *d_loss,
+                                   float *loss, float *lse, void *d_logits, int64_t d_stride, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
+/*
+ * Drafted tokens against the target's probabilities.  Request r drafted tokens offsets[r] .. offsets[r+1] - 1; the target gave a row of
+ * probabilities for each of them and one more behind the last, so request r's rows of `target`, `uniforms` and `tokens` begin at
+ * offsets[r] + r.  With p the target's row, q the draft's and u the uniform number of a drafted token d:
+ *   d stays      if u * q[d] < p[d], up to the first that does not
+ *   then         one more token: in the place of the first that does not stay, a sample of max(p - q, 0) (of p where that is zero
+ *                everywhere); where all stay, a sample of p behind them.  The sample is the first column whose running sum of weights
+ *                exceeds the sum of all times the uniform number of the request's LAST row.
+ *   draft        n_drafted rows, or NULL: the drafts come without probabilities (looked up), q is 1 at the token and 0 elsewhere
+ *   target       n_drafted + requests rows, of dtype like draft; probabilities, not negative; rows need not add up to 1 exactly
+ *   drafted, tokens  int32 or int64 (token_bytes 4 or 8).  A drafted token outside 0 .. cols - 1 does not stay.
+ *   offsets      DEVICE array of requests + 1 int64, ascending from 0 to n_drafted; a request may have drafted nothing.  (What lies outside
+ *                is taken as the nearest that does not.)
+ *   uniforms     fp32 in [0, 1), one for each row of target
+ *   tokens       n_drafted + requests: what stays, the sample, then -1 up to the request's last row
+ *   accepted     int32 for each request: how many stay
+ *   workspace    rose_draft_verify_workspace_bytes, 256-byte aligned: never fewer for more requests or columns; contents before the
+ *                call do not matter; calls that share one must be ordered on one stream
+ * Products, differences and sums are formed in 64 bits.  Rows of zeros, or with a NaN, give some token in range.
+ * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a workspace that is too small;
+ * ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, or requests with 2^24 or more stretches of 4096 columns together.
+ */
+rose_status rose_draft_verify_workspace_bytes(int64_t requests, int64_t cols, size_t *bytes);
+rose_status rose_draft_verify(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride, int32_t dtype,
+                              int64_t cols, const void *drafted, int32_t token_bytes, int64_t n_drafted, const int64_t *offsets,
+                              int64_t requests, const float *uniforms, void *tokens, int32_t *accepted, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * Low-rank adapters of many requests beside a product that they share:  out[i] += scales[a] * up[a] (down[a] x[i]),  a = chosen[i]
+ *   x            m x k, bf16
+ *   down, up     [adapters][rank][k] and [adapters][n][rank], bf16, without gaps
+ *   scales       fp32 for each adapter, or NULL: 1
+ *   chosen       int32 or int64 (chosen_bytes 4 or 8) for each row; outside 0 .. adapters - 1: none, the row of out is left as it is
+ *   out          m x n, bf16 or fp32: what the shared product left there, read and written once
+ *   workspace    rose_adapter_linear_workspace_bytes, 256-byte aligned: never fewer where a size grows; contents before the call do not
+ *                matter; calls that share one must be ordered on one stream
+ * Products are exact, sums and what lies between the two products fp32; one rounding, of the sum with out.  How a sum is divided depends
+ * on the sizes.
+ * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too small;
+ * ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, more than ROSE_MOST_ADAPTERS adapters or a rank above ROSE_MOST_RANK.
+ */
+#define ROSE_MOST_ADAPTERS 65536
+#define ROSE_MOST_RANK 1024
+rose_status rose_adapter_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank, size_t *bytes);
+rose_status rose_adapter_linear(const void *x, int64_t m, int64_t k, int64_t x_stride, const void *down, const void *up,
+                                const float *scales, int64_t adapters, int64_t rank, const void *chosen, int32_t chosen_bytes,
+                                void *out, int32_t out_dtype, int64_t n, int64_t out_stride, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
 const char *rose_status_str(rose_status s);
 
 #ifdef __cplusplus

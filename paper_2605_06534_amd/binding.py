@@ -20,6 +20,7 @@ LAYER_FIRST, LAYER_LAST = -1, -2
 TILE_ORDER_AUTO, TILE_ORDER_SPREAD, TILE_ORDER_NEIGHBOURS, TILE_ORDER_TIMED = 0, 1, 2, 3
 STATIC_SCRATCH_BYTES = 48 << 20
 GRAD_WORKSPACE_BYTES = 32768
+DISTILL_MOST_TOP, MOST_ADAPTERS, MOST_RANK = 1024, 65536, 1024
 MX4_BLOCK = 32
 
 _LIB_PATH = os.environ.get("ROSE_DELTA_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)),
@@ -93,6 +94,18 @@ _SIGS = {
     "rose_mx4_matmul": (_i32, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i32, _i64, _vp]),
     "rose_mx4_linear_workspace_bytes": (_i32, [_i64, _i64, _i64, _P(_size)]),
     "rose_mx4_linear": (_i32, [_vp, _i32, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i32, _i64, _vp, _size, _vp]),
+    "rose_layer_norm": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _i32, _f32, _i32, _vp, _i32, _i64, _vp, _vp, _vp]),
+    "rose_layer_norm_grad_workspace_bytes": (_i32, [_i64, _i64, _P(_size)]),
+    "rose_layer_norm_grad": (_i32, [_vp, _i32, _i64, _vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _vp, _vp, _i64, _vp, _vp, _i32, _vp,
+                                    _size, _vp]),
+    "rose_distill_workspace_bytes": (_i32, [_i64, _i64, _P(_size)]),
+    "rose_distill_loss": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _i64, ctypes.c_double, _vp, _vp, _vp, _size, _vp]),
+    "rose_distill_grad": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _i64, ctypes.c_double, _vp, _vp, _vp, _i64, _vp]),
+    "rose_distill_loss_grad": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _i64, ctypes.c_double, _vp, _vp, _vp, _vp, _i64, _vp, _size, _vp]),
+    "rose_draft_verify_workspace_bytes": (_i32, [_i64, _i64, _P(_size)]),
+    "rose_draft_verify": (_i32, [_vp, _i64, _vp, _i64, _i32, _i64, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _size, _vp]),
+    "rose_adapter_linear_workspace_bytes": (_i32, [_i64, _i64, _i64, _i64, _i64, _P(_size)]),
+    "rose_adapter_linear": (_i32, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _i64, _vp, _i32, _vp, _i32, _i64, _i64, _vp, _size, _vp]),
     "rose_status_str": (ctypes.c_char_p, [_i32]),
 }
 
@@ -556,3 +569,170 @@ def mx4_linear(x, w, out, ws, stream=None):
     _on_gpu("mx4_linear", w.codes, w.scales, ws)
     _check(_lib.rose_mx4_linear(xp, xt, m, xs, w.codes.data_ptr(), w.scales.data_ptr(), n, k, op, ot, os_, ws.data_ptr(),
                                 ws.numel() * ws.element_size(), _stream(stream)), "mx4_linear")
+
+
+# ---------------------------------------------------------------------------------------------------
+# operators between hidden states and tokens
+# ---------------------------------------------------------------------------------------------------
+def _list(t, n, dtypes, what):
+    """The address of n contiguous elements on the GPU, None for None."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.is_contiguous()) or t.numel() != n or t.dtype not in dtypes:
+        raise RoseError(ERR_SHAPE, "%s: %d contiguous elements of %s on the GPU are wanted"
+                        % (what, n, " or ".join(str(d)[6:] for d in dtypes)))
+    return t.data_ptr()
+
+
+_F32 = (torch.float32,)
+
+
+def _bytes(name, what, *sizes, device="cuda"):
+    v = _size()
+    _check(getattr(_lib, name)(*sizes, ctypes.byref(v)), what)
+    return torch.empty(v.value, dtype=torch.uint8, device=device)
+
+
+def _one_device(what, stream, *tensors):
+    """Everything on one GPU, the current one unless a stream says otherwise."""
+    here = tensors[0].get_device() if stream is not None else torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise RoseError(ERR_SHAPE, "%s: all tensors on the GPU that the call runs on are wanted" % what)
+
+
+def layer_norm(x, weight, out, bias=None, mean=None, rstd=None, eps=1e-5, center=True, stream=None):
+    """out = (x - mean) * rstd * weight + bias, row by row; center=False: the root mean square norm.  mean and rstd (float32, one a row)
+    get what the gradient needs; out may be x."""
+    xp, xt, rows, cols, xs = _matrix(x, "layer_norm")
+    op, ot, o_rows, o_cols, os_ = _matrix(out, "layer_norm")
+    _same(o_rows == rows and o_cols == cols and (bias is None or bias.dtype == weight.dtype), "layer_norm")
+    _one_device("layer_norm", stream, x, out, weight, bias, mean, rstd)
+    _check(_lib.rose_layer_norm(xp, xt, rows, cols, xs, _list(weight, cols, _DTYPES, "layer_norm"), _list(bias, cols, _DTYPES, "layer_norm"),
+                                _DTYPES[weight.dtype], eps, 1 if center else 0, op, ot, os_, _list(mean, rows, _F32, "layer_norm"),
+                                _list(rstd, rows, _F32, "layer_norm"), _stream(stream)), "layer_norm")
+
+
+def layer_norm_grad_workspace(rows, cols, device="cuda"):
+    return _bytes("rose_layer_norm_grad_workspace_bytes", "layer_norm_grad_workspace", rows, cols, device=device)
+
+
+def layer_norm_grad(dy, x, weight, rstd, dx, dweight, ws, mean=None, dbias=None, accumulate=False, stream=None):
+    """The gradients of layer_norm for x (into dx, of x's type) and for weight and bias (float32, None: not wanted; accumulate: added to what
+    is there).  mean=None: of the root mean square norm.  dx may be x or dy."""
+    dp, dt, d_rows, d_cols, ds = _matrix(dy, "layer_norm_grad")
+    xp, xt, rows, cols, xs = _matrix(x, "layer_norm_grad")
+    gp, gt, g_rows, g_cols, gs = _matrix(dx, "layer_norm_grad")
+    _same(d_rows == g_rows == rows and d_cols == g_cols == cols and gt == xt, "layer_norm_grad")
+    _on_gpu("layer_norm_grad", ws)
+    _one_device("layer_norm_grad", stream, x, dy, weight, rstd, dx, dweight, ws, mean, dbias)
+    _check(_lib.rose_layer_norm_grad(dp, dt, ds, xp, xt, xs, rows, cols, _list(weight, cols, _DTYPES, "layer_norm_grad"),
+                                     _DTYPES[weight.dtype], _list(mean, rows, _F32, "layer_norm_grad"), _list(rstd, rows, _F32, "layer_norm_grad"),
+                                     gp, gs, _list(dweight, cols, _F32, "layer_norm_grad"), _list(dbias, cols, _F32, "layer_norm_grad"),
+                                     1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "layer_norm_grad")
+
+
+def _entries(logits, ids, teacher, what):
+    """-> (the arguments that the forms of the distillation share, rows, columns, type)"""
+    zp, zt, rows, cols, zs = _matrix(logits, what)
+    size = _ID_BYTES.get(ids.dtype)
+    if (size is None or teacher.dtype != torch.float32 or ids.dim() != 2 or ids.shape != teacher.shape or len(ids) != rows or
+            not (ids.is_cuda and teacher.is_cuda and ids.is_contiguous() and teacher.is_contiguous())):
+        raise RoseError(ERR_SHAPE, "%s: contiguous ids (int32 or int64) and logits (float32) of the teacher, as many for each row, are wanted" % what)
+    return (zp, zt, rows, cols, zs, ids.data_ptr(), size, teacher.data_ptr(), ids.shape[1]), rows, cols, zt
+
+
+def _gradient_like(d_logits, rows, cols, dtype, what):
+    gp, gt, g_rows, g_cols, gs = _matrix(d_logits, what)
+    _same((g_rows, g_cols, gt) == (rows, cols, dtype), what)
+    return gp, gs
+
+
+def distill_workspace(rows, cols, device="cuda"):
+    return _bytes("rose_distill_workspace_bytes", "distill_workspace", rows, cols, device=device)
+
+
+def distill_loss(logits, ids, teacher, loss, lse, ws, temperature=1.0, stream=None):
+    """loss (one a row): the divergence of softmax(logits / T) from the softmax of a teacher's top logits (ids, teacher: as many for each row;
+    ids outside the columns: no entry; rows without any: 0).  lse gets what distill_grad needs."""
+    entries, rows, _, _ = _entries(logits, ids, teacher, "distill_loss")
+    _on_gpu("distill_loss", ws)
+    _one_device("distill_loss", stream, logits, ids, teacher, loss, lse, ws)
+    _check(_lib.rose_distill_loss(*entries, temperature, _list(loss, rows, _F32, "distill_loss"), _list(lse, rows, _F32, "distill_loss"),
+                                  ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "distill_loss")
+
+
+def distill_grad(logits, ids, teacher, lse, d_loss, d_logits, temperature=1.0, stream=None):
+    """d_logits = d_loss * (softmax(logits / T) - the teacher's) / T, from the lse of distill_loss; d_logits may be logits."""
+    entries, rows, cols, dtype = _entries(logits, ids, teacher, "distill_grad")
+    gp, gs = _gradient_like(d_logits, rows, cols, dtype, "distill_grad")
+    _one_device("distill_grad", stream, logits, ids, teacher, lse, d_loss, d_logits)
+    _check(_lib.rose_distill_grad(*entries, temperature, _list(lse, rows, _F32, "distill_grad"), _list(d_loss, rows, _F32, "distill_grad"),
+                                  gp, gs, _stream(stream)), "distill_grad")
+
+
+def distill_loss_grad(logits, ids, teacher, d_loss, loss, lse, d_logits, ws, temperature=1.0, stream=None):
+    """distill_loss and distill_grad in one call, for a d_loss that is known beforehand."""
+    entries, rows, cols, dtype = _entries(logits, ids, teacher, "distill_loss_grad")
+    gp, gs = _gradient_like(d_logits, rows, cols, dtype, "distill_loss_grad")
+    _on_gpu("distill_loss_grad", ws)
+    _one_device("distill_loss_grad", stream, logits, ids, teacher, d_loss, loss, lse, d_logits, ws)
+    _check(_lib.rose_distill_loss_grad(*entries, temperature, _list(d_loss, rows, _F32, "distill_loss_grad"),
+                                       _list(loss, rows, _F32, "distill_loss_grad"), _list(lse, rows, _F32, "distill_loss_grad"), gp, gs,
+                                       ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "distill_loss_grad")
+
+
+def draft_verify_workspace(requests, cols, device="cuda"):
+    return _bytes("rose_draft_verify_workspace_bytes", "draft_verify_workspace", requests, cols, device=device)
+
+
+def draft_verify(target, draft, drafted, offsets, uniforms, tokens, accepted, ws, stream=None):
+    """Which drafted tokens stay, and the token behind them.  target, uniforms, tokens: a row for each drafted token and one more for each
+    request (request r's begin at offsets[r] + r); draft: the drafts' probabilities, or None where they have none; accepted: int32 for each
+    request.  The sample uses the number of the request's last row; tokens behind it become -1."""
+    tp, tt, rows, cols, ts = _matrix(target, "draft_verify")
+    ip, ib, n = _tokens(drafted, "draft_verify")
+    requests = offsets.numel() - 1
+    qp, qs = None, 0
+    if draft is not None:
+        qp, qt, q_rows, q_cols, qs = _matrix(draft, "draft_verify")
+        _same((qt, q_rows, q_cols) == (tt, n, cols), "draft_verify")
+        qp = qp if n else None
+    _same(requests >= 0 and rows == n + requests, "draft_verify")
+    _on_gpu("draft_verify", ws)
+    _one_device("draft_verify", stream, target, draft, drafted, offsets, uniforms, tokens, accepted, ws)
+    _check(_lib.rose_draft_verify(tp, ts, qp, qs, tt, cols, ip, ib, n, _list(offsets, requests + 1, (torch.int64,), "draft_verify"), requests,
+                                  _list(uniforms, rows, _F32, "draft_verify"), _list(tokens, rows, (drafted.dtype,), "draft_verify"),
+                                  _list(accepted, requests, (torch.int32,), "draft_verify"), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                  _stream(stream)), "draft_verify")
+
+
+class Adapters:
+    """Low-rank adapters side by side: down [adapters, rank, k] and up [adapters, n, rank] in bf16, scales (float32, one each) or None: 1."""
+
+    def __init__(self, down, up, scales=None):
+        self.down, self.up, self.scales = down, up, scales
+        _same(down.dim() == 3 and up.dim() == 3 and down.dtype == up.dtype == torch.bfloat16 and down.is_contiguous() and up.is_contiguous() and
+              down.shape[0] == up.shape[0] and down.shape[1] == up.shape[2], "Adapters")
+        self.adapters, self.rank, self.k = down.shape
+        self.n = up.shape[1]
+        _same(scales is None or (scales.dtype == torch.float32 and scales.is_contiguous() and scales.numel() == self.adapters), "Adapters")
+
+
+def adapter_linear_workspace(m, adapters, device=None):
+    return _bytes("rose_adapter_linear_workspace_bytes", "adapter_linear_workspace", m, adapters.n, adapters.k, adapters.adapters, adapters.rank,
+                  device=adapters.down.device if device is None else device)
+
+
+def adapter_linear(x, adapters, chosen, out, ws, stream=None):
+    """out[i] += scale * up (down x[i]) with the adapter chosen[i] of each row; rows without one (a number outside) are left as they are."""
+    xp, xt, m, k, xs = _matrix(x, "adapter_linear")
+    cp, cb, n_chosen = _tokens(chosen, "adapter_linear")
+    op, ot, m_out, n, os_ = _matrix(out, "adapter_linear")
+    _same(xt == DTYPE_BF16 and m_out == n_chosen == m and adapters.k == k and adapters.n == n, "adapter_linear")
+    down, up, scales = adapters.down, adapters.up, adapters.scales
+    _on_gpu("adapter_linear", ws, down, up, scales)
+    _one_device("adapter_linear", stream, x, down, up, scales, chosen, out, ws)
+    _check(_lib.rose_adapter_linear(xp, m, k, xs, down.data_ptr(), up.data_ptr(), scales.data_ptr() if scales is not None else None,
+                                    adapters.adapters, adapters.rank, cp, cb, op, ot, n, os_, ws.data_ptr(), ws.numel() * ws.element_size(),
+                                    _stream(stream)), "adapter_linear")

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librose_delta.so")
-SOURCES = ["plan.cpp", "api.cpp", "ops_api.cpp", "kernels.hip", "embedding.hip", "grad.hip", "mx4.hip"]
+SOURCES = ["plan.cpp", "api.cpp", "ops_api.cpp", "kernels.hip", "embedding.hip", "grad.hip", "mx4.hip", "norm.hip", "distill.hip", "verify.hip", "adapter.hip"]
 
 
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",

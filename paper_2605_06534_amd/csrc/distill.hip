@@ -1,0 +1,353 @@
+// The divergence of a student's distribution q = softmax(z / T) over all columns from p = softmax(t / T) of a teacher's top logits,
+//   loss = sum_j p_j (log p_j - log q_j),   lse = log sum_i exp(z_i / T),   dz = d_loss (q - p) / T,
+// and its gradient.  A row is read for its largest logit and sum, which go along together, and read again for the gradient; what a
+// row's few entries change is written over the row behind it.
+#include "ops_device.h"
+
+namespace rose {
+
+namespace {
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr int kMostTop = ROSE_DISTILL_MOST_TOP;
+constexpr float kLog2E = 1.44269504088896340736f;
+
+// elements of 16 bytes
+template <class T> constexpr int kPer = 16 / (int)sizeof(T);
+
+// (results below 2^-126 come out as zero, which nothing here tells from what they are)
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// sum of exp((z - most) / T) over some columns.  The reference is never an infinity: with it a stretch of masked columns would
+// give inf - inf.
+struct Sum {
+    float most, sum;
+    __device__ __forceinline__ void join(const Sum &o, float c) {
+        const float m = fmaxf(most, o.most);
+        sum = sum * exp2_of((most - m) * c) + o.sum * exp2_of((o.most - m) * c);
+        most = m;
+    }
+};
+
+// ... over the columns first .. first + n of a row, by THREADS threads; c = log2(e) / T
+template <class T, int THREADS>
+__device__ __forceinline__ Sum sum_of(const T *z, int64_t n, float c) {
+    constexpr int W = kPer<T>, AHEAD = 4;
+    const int64_t vectors = n / W;
+    Sum s = {kLowest, 0.f};
+    for (int64_t i = threadIdx.x; i < vectors; i += AHEAD * THREADS) {
+        Raw<T, W> raw[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            // (a vector that is not there: the first one again, which changes no maximum, and adds nothing below)
+            const int64_t at = i + u * THREADS < vectors ? i + u * THREADS : i;
+            load(z + at * W, raw[u]);
+        }
+        float f[AHEAD][W], most = s.most;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            widen(raw[u], f[u]);
+#pragma unroll
+            for (int e = 0; e < W; ++e) most = fmaxf(most, f[u][e]);
+        }
+        s.sum *= exp2_of((s.most - most) * c);
+        s.most = most;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            float t = 0.f;
+#pragma unroll
+            for (int e = 0; e < W; ++e) t += exp2_of((f[u][e] - most) * c);
+            s.sum += i + u * THREADS < vectors ? t : 0.f;
+        }
+    }
+    if (threadIdx.x < n - vectors * W) {
+        const float f = to_f32(z[vectors * W + threadIdx.x]), most = fmaxf(s.most, f);
+        s.sum = s.sum * exp2_of((s.most - most) * c) + exp2_of((f - most) * c);
+        s.most = most;
+    }
+    return s;
+}
+
+// over the workgroup, the same in every thread
+template <int THREADS>
+__device__ __forceinline__ Sum join_all(Sum s, float c, Sum *shared) {
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) s.join(Sum{__shfl_xor(s.most, d), __shfl_xor(s.sum, d)}, c);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = shared[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) s.join(shared[w], c);
+    return s;
+}
+
+__device__ __forceinline__ double lse_of(const Sum &s, const DistillArgs &a) { return (double)s.most / a.temperature + log((double)s.sum); }
+
+// A row's entries as wave 0 leaves them: which columns, their probabilities and logits.
+struct Entries {
+    int32_t id[kMostTop];
+    float p[kMostTop], z[kMostTop];
+    int32_t any;
+};
+__device__ __forceinline__ int64_t id_at(const DistillArgs &a, int64_t i) {
+    return a.wide ? static_cast<const int64_t *>(a.ids)[i] : static_cast<const int32_t *>(a.ids)[i];
+}
+
+// By wave 0: the entries of the row; returns sum of p (log p - z / T), what the loss is but for lse.
+template <class T>
+__device__ __forceinline__ double read_entries(const DistillArgs &a, int64_t row, Entries &s) {
+    const int lane = threadIdx.x;
+    const T *z = static_cast<const T *>(a.logits) + row * a.stride;
+    float most = -INFINITY;
+    bool any = false, odd = false;
+    for (int j = lane; j < a.top; j += 64) {
+        const int64_t id = id_at(a, row * a.top + j);
+        const float t = a.teacher[row * a.top + j];
+        const bool here = id >= 0 && id < a.cols && t != -INFINITY;
+        s.id[j] = here ? (int32_t)id : -1;
+        s.p[j] = t;
+        s.z[j] = here ? to_f32(z[id]) : 0.f;
+        any |= here;
+        odd |= here && t != t;
+        if (here) most = fmaxf(most, t);
+    }
+    any = __any(any);
+    if (lane == 0) s.any = any;
+    if (!any) return 0.;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if (__any(odd)) most = NAN;
+    double size = 0.;
+    for (int j = lane; j < a.top; j += 64)
+        if (s.id[j] >= 0) size += exp(((double)s.p[j] - (double)most) / a.temperature);
+    size = wave_sum(size);
+    const double log_size = log(size);
+    double loss = 0.;
+    for (int j = lane; j < a.top; j += 64) {
+        if (s.id[j] < 0) continue;
+        const double log_p = ((double)s.p[j] - (double)most) / a.temperature - log_size, p = exp(log_p);
+        s.p[j] = (float)p;
+        if (p > 0. || p != p) loss += p * (log_p - (double)s.z[j] / a.temperature);
+    }
+    return wave_sum(loss);
+}
+
+// What a logit's probability is a function of.  FROM_LSE: exp(z / T - lse), where 1 / T comes in two parts if the result has 24 bits; else
+// exp((z - most) / T) / sum.
+template <class T, bool FROM_LSE>
+struct Q {
+    float c, high, low, ref, factor;        // factor: d_loss / T (/ sum)
+    __device__ __forceinline__ float operator()(float z) const {
+        if constexpr (!FROM_LSE) return exp2_of((z - ref) * c) * factor;
+        if constexpr (sizeof(T) == 2) return exp2_of(fmaf(z, high, -ref) * kLog2E) * factor;
+        z = fmaxf(z, kLowest);              // (times a low part of zero)
+        return exp2_of(fmaf(z, low, fmaf(z, high, -ref)) * kLog2E) * factor;
+    }
+};
+template <class T, bool FROM_LSE>
+__device__ __forceinline__ Q<T, FROM_LSE> q_of(const DistillArgs &a, float ref, double sum, float d_loss) {
+    const double inverse = 1. / a.temperature;
+    const float high = (float)inverse;
+    // (an lse of minus infinity: a row of nothing but that)
+    const float factor = FROM_LSE && ref == -INFINITY ? NAN : (float)(d_loss * inverse / sum);
+    return {(float)(inverse * 1.44269504088896340736), high, (float)(inverse - high), ref, factor};
+}
+
+// The gradient of columns `from` .. `from + n` of a row whose entries are known.
+template <class T, int THREADS, bool FROM_LSE>
+__device__ __forceinline__ void write_gradient(const DistillArgs &a, int64_t row, int64_t from, int64_t n, const Entries &s, const Q<T, FROM_LSE> &q, float d) {
+    constexpr int W = kPer<T>, AHEAD = 4;
+    const T *z = static_cast<const T *>(a.logits) + row * a.stride + from;
+    T *out = static_cast<T *>(a.d_logits) + row * a.d_stride + from;
+    const int64_t vectors = n / W;
+    if (!s.any) {                                           // nothing is learnt here, whatever the logits are
+        const float none[W] = {};
+        for (int64_t i = threadIdx.x; i < vectors; i += THREADS) store(out + i * W, none);
+        if (threadIdx.x < n - vectors * W) out[vectors * W + threadIdx.x] = from_f32<T>(0.f);
+        return;
+    }
+    for (int64_t i = threadIdx.x; i < vectors; i += AHEAD * THREADS) {
+        Raw<T, W> raw[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (i + u * THREADS < vectors) load(z + (i + u * THREADS) * W, raw[u]);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (i + u * THREADS >= vectors) break;
+            float f[W];
+            widen(raw[u], f);
+#pragma unroll
+            for (int e = 0; e < W; ++e) f[e] = q(f[e]);
+            store(out + (i + u * THREADS) * W, f);
+        }
+    }
+    if (threadIdx.x < n - vectors * W) {
+        const int64_t i = vectors * W + threadIdx.x;
+        out[i] = from_f32<T>(q(to_f32(z[i])));
+    }
+    // the entries' columns once more, behind what was written above (a column that is named twice has both its probabilities)
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.top; j += THREADS) {
+        const int64_t at = (int64_t)s.id[j] - from;
+        if (s.id[j] < 0 || at < 0 || at >= n) continue;
+        float p = 0.f;
+        for (int i = 0; i < a.top; ++i) p += s.id[i] == s.id[j] ? s.p[i] : 0.f;
+        out[at] = from_f32<T>(q(s.z[j]) - p * d);
+    }
+}
+
+// ---- a workgroup a row ----
+template <class T, int THREADS, bool GRADIENT>
+__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a) {
+    __shared__ Entries entries;
+    __shared__ Sum shared[THREADS / 64];
+    const int64_t row = blockIdx.x;
+    const float c = (float)(1.44269504088896340736 / a.temperature);
+    double loss = 0.;
+    if (threadIdx.x < 64) loss = read_entries<T>(a, row, entries);
+    const Sum s = join_all<THREADS>(sum_of<T, THREADS>(static_cast<const T *>(a.logits) + row * a.stride, a.cols, c), c, shared);
+    if (threadIdx.x == 0) {
+        const double lse = lse_of(s, a);
+        a.lse[row] = (float)lse;
+        a.loss[row] = entries.any ? (float)(loss + lse) : 0.f;
+    }
+    if constexpr (GRADIENT) {
+        const float d_loss = a.d_loss[row];
+        write_gradient<T, THREADS>(a, row, 0, a.cols, entries, q_of<T, false>(a, s.most, s.sum, d_loss), (float)(d_loss / a.temperature));
+    }
+}
+
+// ---- several workgroups a row ----
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a) {
+    __shared__ Entries entries;
+    __shared__ Sum shared[THREADS / 64];
+    const int64_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    const int64_t from = part * a.piece, n = from + a.piece < a.cols ? a.piece : a.cols - from;
+    const float c = (float)(1.44269504088896340736 / a.temperature);
+    if (part == 0 && threadIdx.x < 64) {
+        const double loss = read_entries<T>(a, row, entries);
+        if (threadIdx.x == 0) a.losses[row] = entries.any ? loss : NAN;
+    }
+    const Sum s = join_all<THREADS>(sum_of<T, THREADS>(static_cast<const T *>(a.logits) + row * a.stride + from, n, c), c, shared);
+    if (threadIdx.x == 0) a.partials[blockIdx.x] = {s.most, s.sum};
+}
+
+__device__ __forceinline__ Sum joined(const DistillArgs &a, int64_t row, float c) {
+    const int lane = threadIdx.x & 63;
+    Sum s = {kLowest, 0.f};
+    if (lane < a.parts) {
+        const DistillArgs::Part v = a.partials[row * a.parts + lane];
+        s = {v.most, v.sum};
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) s.join(Sum{__shfl_xor(s.most, d), __shfl_xor(s.sum, d)}, c);
+    return s;
+}
+
+__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Sum &s, bool any) {
+    const double lse = lse_of(s, a);
+    a.lse[row] = (float)lse;
+    a.loss[row] = any ? (float)(a.losses[row] + lse) : 0.f;
+}
+
+// whether a row has entries, by a wave
+__device__ __forceinline__ bool any_entry(const DistillArgs &a, int64_t row) {
+    bool any = false;
+    for (int j = threadIdx.x & 63; j < a.top; j += 64) {
+        const int64_t id = id_at(a, row * a.top + j);
+        any |= id >= 0 && id < a.cols && a.teacher[row * a.top + j] != -INFINITY;
+    }
+    return __any(any);
+}
+
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
+    const int64_t row = blockIdx.x;
+    const Sum s = joined(a, row, (float)(1.44269504088896340736 / a.temperature));
+    const bool any = any_entry(a, row);
+    if (threadIdx.x == 0) write_loss(a, row, s, any);
+}
+
+// FROM_LSE: lse is given; else from the parts' sums
+template <class T, int THREADS, bool FROM_LSE>
+__global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillArgs a) {
+    __shared__ Entries entries;
+    const int64_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    const int64_t from = part * a.piece, n = from + a.piece < a.cols ? a.piece : a.cols - from;
+    // (the entries' logits are read in front of the first write of this workgroup; those of other parts are of no use here)
+    if (threadIdx.x < 64) {
+        DistillArgs own = a;
+        read_entries<T>(own, row, entries);
+    }
+    const float d_loss = a.d_loss[row];
+    __syncthreads();
+    const float d = (float)(d_loss / a.temperature);
+    if constexpr (FROM_LSE) {
+        write_gradient<T, THREADS>(a, row, from, n, entries, q_of<T, true>(a, a.lse[row], 1., d_loss), d);
+    } else {
+        const Sum s = joined(a, row, (float)(1.44269504088896340736 / a.temperature));
+        if (part == 0 && threadIdx.x == 0) write_loss(a, row, s, entries.any);
+        write_gradient<T, THREADS>(a, row, from, n, entries, q_of<T, false>(a, s.most, s.sum, d_loss), d);
+    }
+}
+
+// Parts of a row: where rows alone do not fill the chip, as many as make four workgroups a CU, of 2048 columns at least.
+constexpr int64_t kWanted = 1024, kLeast = 2048;
+constexpr size_t kWorkspace = kWanted * 16;           // a loss for each row and a sum for each part
+
+void divide(DistillArgs &a) {
+    int64_t parts = a.rows > 0 ? kWanted / a.rows : 1;
+    const int64_t most = (a.cols + kLeast - 1) / kLeast;
+    parts = parts < most ? parts : most;
+    parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
+    a.piece = ((a.cols + parts - 1) / parts + 63) / 64 * 64;
+    a.parts = (int32_t)((a.cols + a.piece - 1) / a.piece);
+    a.losses = reinterpret_cast<double *>(a.workspace);
+    a.partials = reinterpret_cast<DistillArgs::Part *>(a.workspace + kWanted * 8);
+}
+
+template <class T>
+int loss(DistillArgs &a, bool gradient, hipStream_t st) {
+    constexpr int MANY = 1024, FEW = 256;
+    divide(a);
+    if (a.parts > 1) {
+        hipLaunchKernelGGL((distill_part_kernel<T, FEW>), dim3((unsigned)(a.rows * a.parts)), dim3(FEW), 0, st, a);
+        if (int e = (int)hipGetLastError()) return e;
+        if (gradient) hipLaunchKernelGGL((distill_grad_kernel<T, FEW, false>), dim3((unsigned)(a.rows * a.parts)), dim3(FEW), 0, st, a);
+        else hipLaunchKernelGGL(distill_join_kernel, dim3((unsigned)a.rows), dim3(64), 0, st, a);
+    } else if (gradient) {
+        if (a.cols > 16384) hipLaunchKernelGGL((distill_row_kernel<T, MANY, true>), dim3((unsigned)a.rows), dim3(MANY), 0, st, a);
+        else hipLaunchKernelGGL((distill_row_kernel<T, FEW, true>), dim3((unsigned)a.rows), dim3(FEW), 0, st, a);
+    } else {
+        if (a.cols > 16384) hipLaunchKernelGGL((distill_row_kernel<T, MANY, false>), dim3((unsigned)a.rows), dim3(MANY), 0, st, a);
+        else hipLaunchKernelGGL((distill_row_kernel<T, FEW, false>), dim3((unsigned)a.rows), dim3(FEW), 0, st, a);
+    }
+    return (int)hipGetLastError();
+}
+
+template <class T>
+int grad(DistillArgs &a, hipStream_t st) {
+    divide(a);
+    hipLaunchKernelGGL((distill_grad_kernel<T, 256, true>), dim3((unsigned)(a.rows * a.parts)), dim3(256), 0, st, a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+size_t distill_workspace(int64_t, int64_t) { return kWorkspace; }
+
+int launch_distill_loss(const DistillArgs &args, bool f32, bool gradient, void *stream) {
+    DistillArgs a = args;
+    if (a.rows == 0) return 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return f32 ? loss<float>(a, gradient, st) : loss<bf16_t>(a, gradient, st);
+}
+
+int launch_distill_grad(const DistillArgs &args, bool f32, void *stream) {
+    DistillArgs a = args;
+    if (a.rows == 0) return 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return f32 ? grad<float>(a, st) : grad<bf16_t>(a, st);
+}
+
+}  // namespace rose

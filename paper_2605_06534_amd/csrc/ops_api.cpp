@@ -1,4 +1,4 @@
-// C ABI of the operators at the two ends of a synchronisation: argument checks and hand-off to the launchers.
+// C ABI of the operators at the two ends of a synchronisation and between hidden states and tokens: argument checks and hand-off to the launchers.
 #include "ops_internal.h"
 
 namespace {
@@ -182,4 +182,160 @@ extern "C" rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m
         a.a_scales = scales;
     }
     return status_of(rose::launch_mx4_product(a, out_dtype == ROSE_DTYPE_F32, stream));
+}
+
+extern "C" rose_status rose_layer_norm(const void *x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t x_stride, const void *weight,
+                                       const void *bias, int32_t weight_dtype, float eps, int32_t center, void *out, int32_t out_dtype,
+                                       int64_t out_stride, float *mean, float *rstd, void *stream) {
+    ROSE_CHECK(check_matrix(x, x_dtype, rows, cols, x_stride));
+    ROSE_CHECK(check_matrix(out, out_dtype, rows, cols, out_stride));
+    ROSE_CHECK(check_matrix(weight, weight_dtype, 1, cols, cols));
+    if (cols == 0 || !(eps >= 0.f) || (bias && !center)) return ROSE_ERR_ARG;
+    if (!aligned(bias, size_of(weight_dtype)) || !aligned(mean, 4) || !aligned(rstd, 4)) return ROSE_ERR_ALIGN;
+    rose::NormArgs a = {x, weight, bias, out, rows, cols, x_stride, out_stride, mean, rstd, eps, center != 0, weight_dtype == ROSE_DTYPE_F32};
+    return status_of(rose::launch_layer_norm(a, x_dtype == ROSE_DTYPE_F32, out_dtype == ROSE_DTYPE_F32, stream));
+}
+
+extern "C" rose_status rose_layer_norm_grad_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes) {
+    if (!bytes || rows < 0 || cols < 0) return ROSE_ERR_ARG;
+    if (rows >= kMost || cols >= kMost) return ROSE_ERR_UNSUPPORTED;
+    *bytes = rose::layer_norm_grad_workspace(rows, cols);
+    return ROSE_OK;
+}
+
+extern "C" rose_status rose_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_stride, const void *x, int32_t x_dtype,
+                                            int64_t x_stride, int64_t rows, int64_t cols, const void *weight, int32_t weight_dtype,
+                                            const float *mean, const float *rstd, void *dx, int64_t dx_stride, float *dweight,
+                                            float *dbias, int32_t accumulate, void *workspace, size_t workspace_bytes, void *stream) {
+    ROSE_CHECK(check_matrix(dy, dy_dtype, rows, cols, dy_stride));
+    ROSE_CHECK(check_matrix(x, x_dtype, rows, cols, x_stride));
+    ROSE_CHECK(check_matrix(dx, x_dtype, rows, cols, dx_stride));
+    ROSE_CHECK(check_matrix(weight, weight_dtype, 1, cols, cols));
+    if (cols == 0 || (rows > 0 && !rstd)) return ROSE_ERR_ARG;
+    if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4)) return ROSE_ERR_ALIGN;
+    ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::layer_norm_grad_workspace(rows, cols)));
+    rose::NormGradArgs a = {dy, x, weight, dx, rows, cols, dy_stride, x_stride, dx_stride, mean, rstd, dweight, dbias,
+                            accumulate != 0, weight_dtype == ROSE_DTYPE_F32, static_cast<char *>(workspace)};
+    return status_of(rose::launch_layer_norm_grad(a, dy_dtype == ROSE_DTYPE_F32, x_dtype == ROSE_DTYPE_F32, stream));
+}
+
+namespace {
+
+// What the three forms of the distillation have in common.
+rose_status check_distill(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids, int32_t id_bytes,
+                          const float *teacher, int64_t top, double temperature) {
+    const rose_status s = check_matrix(logits, dtype, rows, cols, stride);
+    if (s != ROSE_OK) return s;
+    if ((id_bytes != 4 && id_bytes != 8) || top < 0 || cols == 0 || !(temperature > 0.) || !(1. / temperature > 0.)) return ROSE_ERR_ARG;
+    if (rows >= (1 << 22) || top > ROSE_DISTILL_MOST_TOP) return ROSE_ERR_UNSUPPORTED;
+    if (rows > 0 && top > 0 && (!ids || !teacher)) return ROSE_ERR_ARG;
+    return aligned(ids, (size_t)id_bytes) && aligned(teacher, 4) ? ROSE_OK : ROSE_ERR_ALIGN;
+}
+
+// A list of fp32 numbers that the call touches if it has any rows.
+rose_status check_rows(const float *p, int64_t rows) { return rows > 0 && !p ? ROSE_ERR_ARG : aligned(p, 4) ? ROSE_OK : ROSE_ERR_ALIGN; }
+
+}  // namespace
+
+extern "C" rose_status rose_distill_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes) {
+    if (!bytes || rows < 0 || cols < 0) return ROSE_ERR_ARG;
+    if (rows >= kMost || cols >= kMost) return ROSE_ERR_UNSUPPORTED;
+    *bytes = rose::distill_workspace(rows, cols);
+    return ROSE_OK;
+}
+
+extern "C" rose_status rose_distill_loss(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids,
+                                         int32_t id_bytes, const float *teacher, int64_t top, double temperature, float *loss, float *lse,
+                                         void *workspace, size_t workspace_bytes, void *stream) {
+    ROSE_CHECK(check_distill(logits, dtype, rows, cols, stride, ids, id_bytes, teacher, top, temperature));
+    ROSE_CHECK(check_rows(loss, rows));
+    ROSE_CHECK(check_rows(lse, rows));
+    ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::distill_workspace(rows, cols)));
+    rose::DistillArgs a = {logits, rows, cols, stride, ids, id_bytes == 8, teacher, top, temperature, nullptr, loss, lse, nullptr, 0,
+                           static_cast<char *>(workspace), 0, 0, nullptr, nullptr};
+    return status_of(rose::launch_distill_loss(a, dtype == ROSE_DTYPE_F32, false, stream));
+}
+
+extern "C" rose_status rose_distill_loss_grad(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids,
+                                              int32_t id_bytes, const float *teacher, int64_t top, double temperature, const float *d_loss,
+                                              float *loss, float *lse, void *d_logits, int64_t d_stride, void *workspace,
+                                              size_t workspace_bytes, void *stream) {
+    ROSE_CHECK(check_distill(logits, dtype, rows, cols, stride, ids, id_bytes, teacher, top, temperature));
+    ROSE_CHECK(check_matrix(d_logits, dtype, rows, cols, d_stride));
+    ROSE_CHECK(check_rows(d_loss, rows));
+    ROSE_CHECK(check_rows(loss, rows));
+    ROSE_CHECK(check_rows(lse, rows));
+    ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::distill_workspace(rows, cols)));
+    rose::DistillArgs a = {logits, rows, cols, stride, ids, id_bytes == 8, teacher, top, temperature, d_loss, loss, lse, d_logits, d_stride,
+                           static_cast<char *>(workspace), 0, 0, nullptr, nullptr};
+    return status_of(rose::launch_distill_loss(a, dtype == ROSE_DTYPE_F32, true, stream));
+}
+
+extern "C" rose_status rose_distill_grad(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids,
+                                         int32_t id_bytes, const float *teacher, int64_t top, double temperature, const float *lse,
+                                         const float *d_loss, void *d_logits, int64_t d_stride, void *stream) {
+    ROSE_CHECK(check_distill(logits, dtype, rows, cols, stride, ids, id_bytes, teacher, top, temperature));
+    ROSE_CHECK(check_matrix(d_logits, dtype, rows, cols, d_stride));
+    ROSE_CHECK(check_rows(lse, rows));
+    ROSE_CHECK(check_rows(d_loss, rows));
+    rose::DistillArgs a = {logits, rows, cols, stride, ids, id_bytes == 8, teacher, top, temperature, d_loss, nullptr,
+                           const_cast<float *>(lse), d_logits, d_stride, nullptr, 0, 0, nullptr, nullptr};
+    return status_of(rose::launch_distill_grad(a, dtype == ROSE_DTYPE_F32, stream));
+}
+
+extern "C" rose_status rose_draft_verify_workspace_bytes(int64_t requests, int64_t cols, size_t *bytes) {
+    if (!bytes || requests < 0 || cols < 0) return ROSE_ERR_ARG;
+    if (requests >= kMost || cols >= kMost) return ROSE_ERR_UNSUPPORTED;
+    *bytes = rose::draft_verify_workspace(requests, cols);
+    return ROSE_OK;
+}
+
+extern "C" rose_status rose_draft_verify(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride, int32_t dtype,
+                                         int64_t cols, const void *drafted, int32_t token_bytes, int64_t n_drafted, const int64_t *offsets,
+                                         int64_t requests, const float *uniforms, void *tokens, int32_t *accepted, void *workspace,
+                                         size_t workspace_bytes, void *stream) {
+    if (n_drafted < 0 || requests < 0 || cols <= 0) return ROSE_ERR_ARG;
+    if (n_drafted >= kMost || requests >= kMost || n_drafted + requests >= kMost) return ROSE_ERR_UNSUPPORTED;
+    ROSE_CHECK(check_matrix(target, dtype, requests ? n_drafted + requests : 0, cols, target_stride));
+    if (draft) ROSE_CHECK(check_matrix(draft, dtype, n_drafted, cols, draft_stride));
+    ROSE_CHECK(check_tokens(drafted, token_bytes, n_drafted, 0));
+    if (requests > 0 && (!offsets || !uniforms || !tokens || !accepted)) return ROSE_ERR_ARG;
+    if (!aligned(offsets, 8) || !aligned(uniforms, 4) || !aligned(tokens, (size_t)token_bytes) || !aligned(accepted, 4)) return ROSE_ERR_ALIGN;
+    ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::draft_verify_workspace(requests, cols)));
+    if (!rose::draft_verify_fits(requests, cols)) return ROSE_ERR_UNSUPPORTED;
+    rose::VerifyArgs a = {target, draft, cols, target_stride, draft_stride, drafted, token_bytes == 8, n_drafted, offsets, requests, uniforms,
+                          tokens, accepted, workspace, 0};
+    return status_of(rose::launch_draft_verify(a, dtype == ROSE_DTYPE_F32, stream));
+}
+
+namespace {
+
+rose_status check_adapters(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank) {
+    if (m < 0 || n < 0 || k < 0 || adapters < 0 || rank < 0) return ROSE_ERR_ARG;
+    return m < kMost && n < kMost && k < kMost && adapters <= ROSE_MOST_ADAPTERS && rank <= ROSE_MOST_RANK ? ROSE_OK : ROSE_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+extern "C" rose_status rose_adapter_linear_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank, size_t *bytes) {
+    if (!bytes) return ROSE_ERR_ARG;
+    ROSE_CHECK(check_adapters(m, n, k, adapters, rank));
+    *bytes = rose::adapter_linear_workspace(m, n, k, adapters, rank);
+    return ROSE_OK;
+}
+
+extern "C" rose_status rose_adapter_linear(const void *x, int64_t m, int64_t k, int64_t x_stride, const void *down, const void *up,
+                                           const float *scales, int64_t adapters, int64_t rank, const void *chosen, int32_t chosen_bytes,
+                                           void *out, int32_t out_dtype, int64_t n, int64_t out_stride, void *workspace,
+                                           size_t workspace_bytes, void *stream) {
+    ROSE_CHECK(check_adapters(m, n, k, adapters, rank));
+    ROSE_CHECK(check_matrix(x, ROSE_DTYPE_BF16, m, k, x_stride));
+    ROSE_CHECK(check_matrix(out, out_dtype, m, n, out_stride));
+    ROSE_CHECK(check_tokens(chosen, chosen_bytes, m, 0));
+    if (adapters > 0 && rank > 0 && ((k > 0 && !down) || (n > 0 && !up))) return ROSE_ERR_ARG;
+    if (!aligned(down, 2) || !aligned(up, 2) || !aligned(scales, 4)) return ROSE_ERR_ALIGN;
+    ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::adapter_linear_workspace(m, n, k, adapters, rank)));
+    rose::AdapterArgs a = {x, down, up, scales, chosen, chosen_bytes == 8, out, m, n, k, rank, adapters, x_stride, out_stride,
+                           static_cast<char *>(workspace), nullptr};
+    return status_of(rose::launch_adapter_linear(a, out_dtype == ROSE_DTYPE_F32, stream));
 }

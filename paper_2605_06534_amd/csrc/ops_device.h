@@ -122,6 +122,34 @@ __device__ __forceinline__ void store(T *p, int n, const float (&f)[W]) {
         if (i < n) p[i] = from_f32<T>(f[i]);
 }
 
+// sum over the lanes of a wave, the same in each
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+// sums over a workgroup of WAVES waves, the same in every thread; `shared` may be used again at once
+template <int WAVES, class T, int N>
+__device__ __forceinline__ void block_sum(T (&v)[N], T (&shared)[N * WAVES]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) shared[i * WAVES + (threadIdx.x >> 6)] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = shared[i * WAVES];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[i] += shared[i * WAVES + w];
+        }
+        __syncthreads();
+    }
+}
+
 // The vectors of a matrix, so many elements each, row after row, in groups of PER neighbouring ones, a group a workgroup: so that no lane is
 // idle whatever the columns are.  (A workgroup a group, not workgroups that walk: stores count as loads do among what a wave waits
 // for, and one that goes on waits for its stores.  Quantising 151936 x 4096 249 us, 357 with 2048 workgroups that ask ahead.)

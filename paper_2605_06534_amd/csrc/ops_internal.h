@@ -1,4 +1,5 @@
-// Launchers of the operators at the two ends of a synchronisation (embedding.hip, grad.hip, mx4.hip); ops_api.cpp
+// Launchers of the operators at the two ends of a synchronisation and between hidden states and tokens (embedding.hip, grad.hip,
+// mx4.hip, norm.hip, distill.hip, verify.hip, adapter.hip); ops_api.cpp
 // checks arguments and calls them.  All return a hipError_t as int.
 #pragma once
 
@@ -73,5 +74,83 @@ struct Mx4ProductArgs {
 bool mx4_product_takes_bf16(int64_t m, int64_t n, int64_t k);
 bool mx4_product_fits(int64_t m, int64_t n, int64_t k);        // into launches
 int launch_mx4_product(const Mx4ProductArgs &a, bool out_f32, void *stream);
+
+struct NormArgs {
+    const void *x, *weight, *bias;      // bias may be null
+    void *out;
+    int64_t rows, cols, x_stride, out_stride;
+    float *mean, *rstd;                 // either may be null
+    float eps;
+    bool center, w_f32;
+};
+int launch_layer_norm(const NormArgs &a, bool x_f32, bool out_f32, void *stream);
+
+struct NormGradArgs {
+    const void *dy, *x, *weight;
+    void *dx;                           // of x's type
+    int64_t rows, cols, dy_stride, x_stride, dx_stride;
+    const float *mean, *rstd;           // mean null: not centred
+    float *dweight, *dbias;             // either may be null
+    bool accumulate, w_f32;
+    char *workspace;
+};
+size_t layer_norm_grad_workspace(int64_t rows, int64_t cols);
+int launch_layer_norm_grad(const NormGradArgs &a, bool dy_f32, bool x_f32, void *stream);
+
+struct DistillArgs {
+    const void *logits;
+    int64_t rows, cols, stride;
+    const void *ids;
+    int32_t wide;                       // 64-bit ids
+    const float *teacher;
+    int64_t top;
+    double temperature;
+    const float *d_loss;
+    float *loss, *lse;
+    void *d_logits;                     // of the logits' type
+    int64_t d_stride;
+    char *workspace;
+    // the launchers': parts of a row, their columns and sums
+    int32_t parts;
+    int64_t piece;
+    double *losses;
+    struct Part {
+        float most, sum;
+    } *partials;
+};
+size_t distill_workspace(int64_t rows, int64_t cols);
+int launch_distill_loss(const DistillArgs &a, bool f32, bool gradient, void *stream);
+int launch_distill_grad(const DistillArgs &a, bool f32, void *stream);      // from lse
+
+struct VerifyArgs {
+    const void *target, *draft;         // draft may be null
+    int64_t cols, target_stride, draft_stride;
+    const void *drafted;
+    int32_t wide;                       // 64-bit tokens
+    int64_t n_drafted;
+    const int64_t *offsets;
+    int64_t requests;
+    const float *uniforms;
+    void *tokens;
+    int32_t *accepted;
+    void *sums;
+    int64_t parts;                      // the launcher's
+};
+bool draft_verify_fits(int64_t requests, int64_t cols);        // into launches
+size_t draft_verify_workspace(int64_t requests, int64_t cols);
+int launch_draft_verify(const VerifyArgs &a, bool f32, void *stream);
+
+struct AdapterArgs {
+    const void *x, *down, *up;
+    const float *scales;                // may be null
+    const void *chosen;
+    int32_t wide;                       // 64-bit numbers of adapters
+    void *out;
+    int64_t m, n, k, rank, adapters, x_stride, out_stride;
+    char *workspace;
+    float *h;                           // the launcher's
+};
+size_t adapter_linear_workspace(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank);
+int launch_adapter_linear(const AdapterArgs &a, bool out_f32, void *stream);
 
 }  // namespace rose
