@@ -312,7 +312,9 @@ namespace {
 
 rose_status check_adapters(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank) {
     if (m < 0 || n < 0 || k < 0 || adapters < 0 || rank < 0) return ROSE_ERR_ARG;
-    return m < kMost && n < kMost && k < kMost && adapters <= ROSE_MOST_ADAPTERS && rank <= ROSE_MOST_RANK ? ROSE_OK : ROSE_ERR_UNSUPPORTED;
+    // (groups of rows times blocks of ranks are workgroups)
+    if (m < (1 << 29) && adapters <= ROSE_MOST_ADAPTERS && rank <= ROSE_MOST_RANK && (m / 64 + adapters) * ((rank + 63) / 64) >= (1 << 24)) return ROSE_ERR_UNSUPPORTED;
+    return m < (1 << 29) && n < kMost && k < kMost && adapters <= ROSE_MOST_ADAPTERS && rank <= ROSE_MOST_RANK ? ROSE_OK : ROSE_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -335,7 +337,9 @@ extern "C" rose_status rose_adapter_linear(const void *x, int64_t m, int64_t k, 
     if (adapters > 0 && rank > 0 && ((k > 0 && !down) || (n > 0 && !up))) return ROSE_ERR_ARG;
     if (!aligned(down, 2) || !aligned(up, 2) || !aligned(scales, 4)) return ROSE_ERR_ALIGN;
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::adapter_linear_workspace(m, n, k, adapters, rank)));
-    rose::AdapterArgs a = {x, down, up, scales, chosen, chosen_bytes == 8, out, m, n, k, rank, adapters, x_stride, out_stride,
-                           static_cast<char *>(workspace), nullptr};
+    rose::AdapterArgs a = {};
+    a.x = x, a.down = down, a.up = up, a.scales = scales, a.chosen = chosen, a.wide = chosen_bytes == 8, a.out = out;
+    a.m = m, a.n = n, a.k = k, a.rank = rank, a.adapters = adapters, a.x_stride = x_stride, a.out_stride = out_stride;
+    a.workspace = static_cast<char *>(workspace);
     return status_of(rose::launch_adapter_linear(a, out_dtype == ROSE_DTYPE_F32, stream));
 }

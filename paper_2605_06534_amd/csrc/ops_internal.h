@@ -148,7 +148,15 @@ struct AdapterArgs {
     void *out;
     int64_t m, n, k, rank, adapters, x_stride, out_stride;
     char *workspace;
-    float *h;                           // the launcher's
+    // the launcher's: what lies between the products, [splits][m][ranks]; rows in order of their adapters, and groups of them
+    float *h;
+    int64_t ranks, splits, share;       // ranks in whole tiles; parts of k, and elements of one
+    int64_t columns;                    // of a workgroup
+    int64_t units, group;               // groups, or adapters to look for; rows of a group, at most
+    int32_t *order;
+    struct Group {
+        int32_t adapter, first, n;
+    } *groups;
 };
 size_t adapter_linear_workspace(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank);
 int launch_adapter_linear(const AdapterArgs &a, bool out_f32, void *stream);
