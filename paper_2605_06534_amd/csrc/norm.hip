@@ -15,6 +15,129 @@ __device__ __forceinline__ float element(const void *p, bool f32, int64_t i) {
     return f32 ? static_cast<const float *>(p)[i] : to_f32(static_cast<const bf16_t *>(p)[i]);
 }
 
+// Elements that a lane reads or writes at a time: 16 bytes of the wider type
+template <class A, class B>
+constexpr int kPer = sizeof(A) == 4 || sizeof(B) == 4 ? 4 : 8;
+
+template <int W>
+__device__ __forceinline__ void read_weight(const void *p, bool f32, int64_t i, float (&f)[W]) {
+    if (f32) {
+        Raw<float, W> raw;
+        load(static_cast<const float *>(p) + i, raw);
+        widen(raw, f);
+    } else {
+        Raw<bf16_t, W> raw;
+        load(static_cast<const bf16_t *>(p) + i, raw);
+        widen(raw, f);
+    }
+}
+
+// ---- rows that stay in registers: read once, LANES lanes a row, V vectors a lane; what is behind the last whole vector an element a lane ----
+template <class X, class Y, int LANES, int V>
+__global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows_kernel(NormArgs a) {
+    constexpr int W = kPer<X, Y>, THREADS = LANES < kThreads ? kThreads : LANES;
+    __shared__ float shared[4][LANES > 64 ? LANES / 64 : 1];
+    const int lane = threadIdx.x % LANES;
+    const int64_t wanted = (int64_t)blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
+    const bool there = wanted < a.rows;
+    const int64_t row = there ? wanted : a.rows - 1;
+    const X *x = static_cast<const X *>(a.x) + row * a.x_stride;
+    const int32_t vectors = (int32_t)(a.cols / W), rest = (int32_t)(a.cols - (int64_t)vectors * W);
+    Raw<X, W> raw[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        zero(raw[v]);
+        if (v * LANES + lane < vectors) load(x + (v * LANES + lane) * W, raw[v]);
+    }
+    const float tail = lane < rest ? to_f32(x[vectors * W + lane]) : 0.f;
+    // Each 16 lanes, or each wave of a longer row, find their own mean and the squares of the deviations from it; waves then join theirs in one
+    // exchange:  sum (x - mean)^2 = sum over the waves of squares + n (mean - the wave's)^2.
+    auto total = [](float v) { return LANES == 16 ? sum16(v) : wave_sum(v); };
+    const int wave = LANES > 64 ? (int)threadIdx.x >> 6 : 0;
+    float n = (float)a.cols;
+    if constexpr (LANES > 64) {
+        int32_t mine = wave == 0 ? rest : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int32_t left = vectors - v * LANES - wave * 64;
+            mine += W * (left < 0 ? 0 : left < 64 ? left : 64);
+        }
+        n = (float)mine;
+    }
+    float sum = 0.f, mean = 0.f;
+    if (a.center) {
+        float s = tail;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float f[W];
+            widen(raw[v], f);
+#pragma unroll
+            for (int e = 0; e < W; ++e) s += f[e];
+        }
+        sum = total(s);
+        mean = n > 0.f ? sum / n : 0.f;
+    }
+    float s = lane < rest ? (tail - mean) * (tail - mean) : 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float f[W], t = 0.f;
+        widen(raw[v], f);
+#pragma unroll
+        for (int e = 0; e < W; ++e) t = fmaf(f[e] - mean, f[e] - mean, t);
+        s += v * LANES + lane < vectors ? t : 0.f;
+    }
+    float squares = total(s);
+    if constexpr (LANES > 64) {
+        constexpr int WAVES = LANES / 64;
+        if ((threadIdx.x & 63) == 0) shared[0][wave] = squares, shared[1][wave] = sum, shared[2][wave] = mean, shared[3][wave] = n;
+        __syncthreads();
+        if (a.center) {
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) sum += shared[1][w];
+            mean = sum / (float)a.cols;
+        }
+        squares = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float d = a.center ? shared[2][w] - mean : 0.f;
+            squares += fmaf(d * shared[3][w], d, shared[0][w]);
+        }
+    }
+    const float rstd = 1.f / sqrtf(squares / (float)a.cols + a.eps);
+    if (!there) return;
+    if (lane == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    Y *out = static_cast<Y *>(a.out) + row * a.out_stride;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int32_t col = (v * LANES + lane) * W;
+        if (v * LANES + lane >= vectors) continue;
+        float f[W], w[W];
+        widen(raw[v], f);
+        read_weight(a.weight, a.w_f32, col, w);
+#pragma unroll
+        for (int e = 0; e < W; ++e) f[e] = (f[e] - mean) * rstd * w[e];
+        if (a.bias) {
+            read_weight(a.bias, a.w_f32, col, w);
+#pragma unroll
+            for (int e = 0; e < W; ++e) f[e] += w[e];
+        }
+        if constexpr (W * sizeof(Y) == 8) {
+            u32x2_any *q = reinterpret_cast<u32x2_any *>(out + col);
+            *q = u32x2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
+        } else {
+            store(out + col, f);
+        }
+    }
+    if (lane < rest) {
+        const int64_t col = vectors * W + lane;
+        out[col] = from_f32<Y>(fmaf((tail - mean) * rstd, element(a.weight, a.w_f32, col), a.bias ? element(a.bias, a.w_f32, col) : 0.f));
+    }
+}
+
 // ---- rows of any length: a workgroup a row, element by element, each element always the same thread's ----
 template <class X, class Y>
 __global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
@@ -112,8 +235,30 @@ unsigned row_groups(int64_t rows) {
     return (unsigned)(rows < most ? rows : most);
 }
 
+template <class X, class Y, int LANES, int V>
+int norm_rows(const NormArgs &a, hipStream_t st) {
+    constexpr int THREADS = LANES < kThreads ? kThreads : LANES, PER = THREADS / LANES;
+    hipLaunchKernelGGL((norm_rows_kernel<X, Y, LANES, V>), dim3((unsigned)((a.rows + PER - 1) / PER)), dim3(THREADS), 0, st, a);
+    return (int)hipGetLastError();
+}
+
 template <class X, class Y>
 int norm(const NormArgs &a, hipStream_t st) {
+    // (rows that one launch can have; and vectors)
+    constexpr int64_t W = kPer<X, Y>;
+    const int64_t n = a.cols / W;
+    if (a.rows < kMostThreads / 1024 && n > 0) {
+        if (n <= 16) return norm_rows<X, Y, 16, 1>(a, st);
+        if (n <= 32) return norm_rows<X, Y, 16, 2>(a, st);
+        if (n <= 64) return norm_rows<X, Y, 64, 1>(a, st);
+        if (n <= 128) return norm_rows<X, Y, 64, 2>(a, st);
+        if (n <= 256) return norm_rows<X, Y, 256, 1>(a, st);
+        if (n <= 512) return norm_rows<X, Y, 256, 2>(a, st);
+        if (n <= 768) return norm_rows<X, Y, 256, 3>(a, st);
+        if (n <= 1024) return norm_rows<X, Y, 256, 4>(a, st);
+        if (n <= 2048) return norm_rows<X, Y, 256, 8>(a, st);
+        if (n <= 8192) return norm_rows<X, Y, 1024, 8>(a, st);
+    }
     hipLaunchKernelGGL((layer_norm_kernel<X, Y>), dim3(row_groups(a.rows)), dim3(kThreads), 0, st, a);
     return (int)hipGetLastError();
 }
