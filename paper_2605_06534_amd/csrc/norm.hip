@@ -32,6 +32,13 @@ __device__ __forceinline__ void read_weight(const void *p, bool f32, int64_t i, 
     }
 }
 
+// (half a vector of bf16 where the other side is fp32)
+template <class T, int W>
+__device__ __forceinline__ void write(T *p, const float (&f)[W]) {
+    if constexpr (W * sizeof(T) == 8) *reinterpret_cast<u32x2_any *>(p) = u32x2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
+    else store(p, f);
+}
+
 // ---- rows that stay in registers: read once, LANES lanes a row, V vectors a lane; what is behind the last whole vector an element a lane ----
 template <class X, class Y, int LANES, int V>
 __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows_kernel(NormArgs a) {
@@ -125,12 +132,7 @@ __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows
 #pragma unroll
             for (int e = 0; e < W; ++e) f[e] += w[e];
         }
-        if constexpr (W * sizeof(Y) == 8) {
-            u32x2_any *q = reinterpret_cast<u32x2_any *>(out + col);
-            *q = u32x2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
-        } else {
-            store(out + col, f);
-        }
+        write(out + col, f);
     }
     if (lane < rest) {
         const int64_t col = vectors * W + lane;
@@ -215,16 +217,193 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(NormGradArgs a, 
     partials[(2 * part + 1) * a.cols + col] = db;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_join_kernel(NormGradArgs a, const float *partials, int64_t parts) {
-    const int64_t col = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (col >= a.cols) return;
-    float dw = 0.f, db = 0.f;
-    for (int64_t p = 0; p < parts; ++p) {
-        dw += partials[2 * p * a.cols + col];
-        db += partials[(2 * p + 1) * a.cols + col];
+// ---- gradients in one pass: a workgroup keeps kColumns columns a lane of dw and db in registers while rows go by, ROWS at a time, the next
+// ones on their way; TEAM threads have a row, in whole waves (TEAM = 0: as many as the workgroup has), or 16 lanes.  The two means of a row
+// are the only thing that goes from wave to wave.
+// 256 workgroups: each leaves sums of all columns behind, 8 bytes a column (16384 x 5120 in bf16: 110 us, with 512 of them 116, with 768 128).
+// x and dy are read for the last time, so that the caches need not keep them: 99 us, 5.1 TB/s.  (Columns a lane 8: the same; two rows at
+// a time instead of one: 89 us against 96 of 16384 x 4096, four spill.) ----
+constexpr int kColumns = 16;
+
+template <class D, class X, int TEAM, int ROWS, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a, float *partials, int64_t piece) {
+    constexpr int W = kPer<D, X>, V = kColumns / W;
+    constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1;            // of a row's (TEAM = 0: blockDim.x / 64)
+    constexpr bool ONE = TEAM == 0;
+    __shared__ float exchange[2][THREADS / 64][2 * ROWS];
+    __shared__ float joined[ONE ? 1 : THREADS * kColumns];
+    const int team = ONE ? (int)blockDim.x : TEAM, lane = ONE ? (int)threadIdx.x : (int)threadIdx.x % TEAM;
+    const int group = ONE ? 0 : (int)threadIdx.x / TEAM, groups = ONE ? 1 : THREADS / TEAM;
+    const int wave = (int)threadIdx.x >> 6, first_wave = ONE ? 0 : TEAM >= 64 ? group * WAVES : wave, waves = ONE ? (int)blockDim.x >> 6 : WAVES;
+    const int32_t vectors = (int32_t)(a.cols / W), rest = (int32_t)(a.cols - (int64_t)vectors * W);
+    const bool in_rest = lane < rest;
+    const int64_t tail = (int64_t)vectors * W + lane;
+    // `piece` rows a workgroup, its groups take ROWS of them in turn
+    const int64_t first = blockIdx.x * piece, end = first + piece < a.rows ? first + piece : a.rows;
+    float w[V][W], dw[V][W], db[V][W], w_tail = 0.f, dw_tail = 0.f, db_tail = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) w[v][e] = dw[v][e] = db[v][e] = 0.f;
+        if (v * team + lane < vectors) read_weight(a.weight, a.w_f32, (v * team + lane) * W, w[v]);
     }
-    if (a.dweight) a.dweight[col] = a.accumulate ? a.dweight[col] + dw : dw;
-    if (a.dbias) a.dbias[col] = a.accumulate ? a.dbias[col] + db : db;
+    if (in_rest) w_tail = element(a.weight, a.w_f32, tail);
+    Raw<X, W> x_raw[ROWS][V];
+    Raw<D, W> d_raw[ROWS][V];
+    float x_tail[ROWS], d_tail[ROWS], means[ROWS], rstds[ROWS];
+    auto ask = [&](int64_t at) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t row = at + r < end ? at + r : end - 1;
+            const X *x = static_cast<const X *>(a.x) + row * a.x_stride;
+            const D *dy = static_cast<const D *>(a.dy) + row * a.dy_stride;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v * team + lane < vectors) {
+                    load<true>(x + (v * team + lane) * W, x_raw[r][v]);
+                    load<true>(dy + (v * team + lane) * W, d_raw[r][v]);
+                } else {
+                    zero(x_raw[r][v]);
+                    zero(d_raw[r][v]);
+                }
+            x_tail[r] = in_rest ? to_f32(x[tail]) : 0.f;
+            d_tail[r] = in_rest ? to_f32(dy[tail]) : 0.f;
+            means[r] = a.mean ? a.mean[row] : 0.f;
+            rstds[r] = a.rstd[row];
+        }
+    };
+    const int64_t stride = (int64_t)groups * ROWS, steps = (piece + stride - 1) / stride;
+    const float inverse = 1.f / (float)a.cols;
+    int64_t row = first + (int64_t)group * ROWS;
+    ask(row);
+    for (int64_t step = 0; step < steps; ++step, row += stride) {
+        float xhat[ROWS][V][W], g[ROWS][V][W], xh_tail[ROWS], g_tail[ROWS], sums[2 * ROWS], rstd[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const float here = row + r < end ? 1.f : 0.f;           // (the last row again adds nothing)
+            float s = 0.f, t = 0.f;
+            rstd[r] = rstds[r];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float d[W];
+                widen(x_raw[r][v], xhat[r][v]);
+                widen(d_raw[r][v], d);
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    xhat[r][v][e] = (xhat[r][v][e] - means[r]) * rstd[r];
+                    g[r][v][e] = d[e] * w[v][e];
+                    s += g[r][v][e];
+                    t = fmaf(g[r][v][e], xhat[r][v][e], t);
+                }
+                if (row + r < end) {
+#pragma unroll
+                    for (int e = 0; e < W; ++e) {
+                        dw[v][e] = fmaf(d[e], xhat[r][v][e], dw[v][e]);
+                        db[v][e] += d[e];
+                    }
+                }
+            }
+            xh_tail[r] = (x_tail[r] - means[r]) * rstd[r];
+            g_tail[r] = d_tail[r] * w_tail;
+            s += g_tail[r];
+            t = fmaf(g_tail[r], xh_tail[r], t);
+            if (here != 0.f && in_rest) {
+                dw_tail = fmaf(d_tail[r], xh_tail[r], dw_tail);
+                db_tail += d_tail[r];
+            }
+            sums[2 * r] = s;
+            sums[2 * r + 1] = t;
+        }
+        if (step + 1 < steps) ask(row + stride);
+#pragma unroll
+        for (int i = 0; i < 2 * ROWS; ++i) sums[i] = TEAM == 16 ? sum16(sums[i]) : wave_sum(sums[i]);
+        if constexpr (TEAM == 0 || TEAM > 64) {
+            float(&shared)[THREADS / 64][2 * ROWS] = exchange[step & 1];
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int i = 0; i < 2 * ROWS; ++i) shared[wave][i] = sums[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2 * ROWS; ++i) sums[i] = 0.f;
+            for (int k = 0; k < waves; ++k)
+#pragma unroll
+                for (int i = 0; i < 2 * ROWS; ++i) sums[i] += shared[first_wave + k][i];
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (row + r >= end) continue;
+            const float c1 = a.mean ? -sums[2 * r] * inverse * rstd[r] : 0.f, c2 = -sums[2 * r + 1] * inverse * rstd[r];
+            X *dx = static_cast<X *>(a.dx) + (row + r) * a.dx_stride;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (v * team + lane >= vectors) continue;
+                float f[W];
+#pragma unroll
+                for (int e = 0; e < W; ++e) f[e] = fmaf(g[r][v][e], rstd[r], fmaf(xhat[r][v][e], c2, c1));
+                write(dx + (v * team + lane) * W, f);
+            }
+            if (in_rest) dx[tail] = from_f32<X>(fmaf(g_tail[r], rstd[r], fmaf(xh_tail[r], c2, c1)));
+        }
+    }
+    // the groups' sums, in order
+    if (!a.dweight && !a.dbias) return;
+    float *out = partials + 2 * (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float(&sum)[V][W] = which ? db : dw;
+        float &sum_tail = which ? db_tail : dw_tail;
+        if constexpr (!ONE) {
+            // (the elements behind the last whole vector go into the place of a vector that is not there, or along with lane 0's)
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < W; ++e) joined[(v * W + e) * THREADS + threadIdx.x] = sum[v][e];
+            __syncthreads();
+            if (group == 0)
+                for (int k = 1; k < groups; ++k)
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+#pragma unroll
+                        for (int e = 0; e < W; ++e) sum[v][e] += joined[(v * W + e) * THREADS + k * team + lane];
+            __syncthreads();
+            joined[threadIdx.x] = sum_tail;
+            __syncthreads();
+            if (group == 0)
+                for (int k = 1; k < groups; ++k) sum_tail += joined[k * team + lane];
+        }
+        if (group == 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v * team + lane < vectors) {
+                    store(out + which * a.cols + (v * team + lane) * W, sum[v]);
+                }
+            if (in_rest) out[which * a.cols + tail] = sum_tail;
+        }
+    }
+}
+
+// the parts' sums, in order: kJoinColumns columns a workgroup, each by kJoinLanes threads
+constexpr int kJoinColumns = 32, kJoinLanes = 32;
+__global__ __launch_bounds__(kJoinColumns * kJoinLanes) void norm_join_kernel(NormGradArgs a, const float *partials, int64_t parts) {
+    __shared__ float shared[2][kJoinLanes][kJoinColumns];
+    const int c = threadIdx.x % kJoinColumns, lane = threadIdx.x / kJoinColumns;
+    const int64_t col = (int64_t)blockIdx.x * kJoinColumns + c;
+    float dw = 0.f, db = 0.f;
+    if (col < a.cols)
+#pragma unroll 8
+        for (int64_t p = lane; p < parts; p += kJoinLanes) {
+            dw += partials[2 * p * a.cols + col];
+            db += partials[(2 * p + 1) * a.cols + col];
+        }
+    shared[0][lane][c] = dw;
+    shared[1][lane][c] = db;
+    __syncthreads();
+    if (lane > 1 || col >= a.cols) return;
+    float s = 0.f;
+    for (int k = 0; k < kJoinLanes; ++k) s += shared[lane][k][c];
+    float *out = lane ? a.dbias : a.dweight;
+    if (out) out[col] = a.accumulate ? out[col] + s : s;
 }
 
 constexpr int64_t kMostParts = 256;
@@ -265,22 +444,45 @@ int norm(const NormArgs &a, hipStream_t st) {
 
 size_t means_bytes(int64_t rows) { return ((size_t)rows * sizeof(RowMeans) + 255) / 256 * 256; }
 
+int join(const NormGradArgs &a, const float *partials, int64_t parts, hipStream_t st) {
+    if (!a.dweight && !a.dbias) return 0;
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((a.cols + kJoinColumns - 1) / kJoinColumns)), dim3(kJoinColumns * kJoinLanes), 0, st, a, partials, parts);
+    return (int)hipGetLastError();
+}
+
+template <class D, class X, int TEAM, int ROWS, int THREADS>
+int norm_grad_rows(const NormGradArgs &a, float *partials, int threads, hipStream_t st) {
+    const int64_t groups = TEAM ? THREADS / TEAM : 1, least = groups * ROWS;
+    int64_t piece = (a.rows + kMostParts - 1) / kMostParts;
+    piece = (piece + least - 1) / least * least;
+    const int64_t parts = (a.rows + piece - 1) / piece;
+    hipLaunchKernelGGL((norm_grad_kernel<D, X, TEAM, ROWS, THREADS>), dim3((unsigned)parts), dim3(threads), 0, st, a, partials, piece);
+    if (int e = (int)hipGetLastError()) return e;
+    return join(a, partials, parts, st);
+}
+
 template <class D, class X>
 int norm_grad(const NormGradArgs &a, hipStream_t st) {
     RowMeans *means = reinterpret_cast<RowMeans *>(a.workspace);
     float *partials = reinterpret_cast<float *>(a.workspace + means_bytes(a.rows));
+    if (a.rows == 0) return join(a, partials, 0, st);
+    constexpr int64_t W = kPer<D, X>;
+    const int64_t n = a.cols / W, lanes = (n * W + kColumns - 1) / kColumns, threads = (lanes + 63) / 64 * 64;
+    if (n > 0) {
+        if (lanes <= 16) return norm_grad_rows<D, X, 16, 1, 256>(a, partials, 256, st);
+        if (lanes <= 64) return norm_grad_rows<D, X, 64, 2, 256>(a, partials, 256, st);
+        if (lanes <= 128) return norm_grad_rows<D, X, 128, 2, 256>(a, partials, 256, st);
+        if (lanes <= 512) return norm_grad_rows<D, X, 0, 2, 512>(a, partials, (int)threads, st);
+        if (lanes <= 1024) return norm_grad_rows<D, X, 0, 1, 1024>(a, partials, (int)threads, st);
+    }
     const int64_t tiles = (a.cols + kThreads - 1) / kThreads, most = kMostThreads / kThreads / tiles;
     const int64_t wanted = most < kMostParts ? most : kMostParts;
-    const int64_t piece = (a.rows + wanted - 1) / wanted, parts = piece ? (a.rows + piece - 1) / piece : 0;
-    if (a.rows > 0) {
-        hipLaunchKernelGGL((norm_means_kernel<D, X>), dim3(row_groups(a.rows)), dim3(kThreads), 0, st, a, means);
-        if (int e = (int)hipGetLastError()) return e;
-        hipLaunchKernelGGL((norm_columns_kernel<D, X>), dim3((unsigned)(tiles * parts)), dim3(kThreads), 0, st, a, means, partials, piece, tiles);
-        if (int e = (int)hipGetLastError()) return e;
-    }
-    if (!a.dweight && !a.dbias) return 0;
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)tiles), dim3(kThreads), 0, st, a, partials, parts);
-    return (int)hipGetLastError();
+    const int64_t piece = (a.rows + wanted - 1) / wanted, parts = (a.rows + piece - 1) / piece;
+    hipLaunchKernelGGL((norm_means_kernel<D, X>), dim3(row_groups(a.rows)), dim3(kThreads), 0, st, a, means);
+    if (int e = (int)hipGetLastError()) return e;
+    hipLaunchKernelGGL((norm_columns_kernel<D, X>), dim3((unsigned)(tiles * parts)), dim3(kThreads), 0, st, a, means, partials, piece, tiles);
+    if (int e = (int)hipGetLastError()) return e;
+    return join(a, partials, parts, st);
 }
 
 }  // namespace
