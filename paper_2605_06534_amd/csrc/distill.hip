@@ -2,6 +2,8 @@
 //   loss = sum_j p_j (log p_j - log q_j),   lse = log sum_i exp(z_i / T),   dz = d_loss (q - p) / T,
 // and its gradient.  A row is read for its largest logit and sum, which go along together, and read again for the gradient; what a
 // row's few entries change is written over the row behind it.
+#include <type_traits>
+
 #include "ops_device.h"
 
 namespace rose {
@@ -11,6 +13,9 @@ namespace {
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kMostTop = ROSE_DISTILL_MOST_TOP;
 constexpr float kLog2E = 1.44269504088896340736f;
+
+constexpr int kAhead = 4;                           // vectors that a thread has under way
+constexpr int kChunkThreads = 256;
 
 // elements of 16 bytes
 template <class T> constexpr int kPer = 16 / (int)sizeof(T);
@@ -32,7 +37,7 @@ struct Sum {
 // ... over the columns first .. first + n of a row, by THREADS threads; c = log2(e) / T
 template <class T, int THREADS>
 __device__ __forceinline__ Sum sum_of(const T *z, int64_t n, float c) {
-    constexpr int W = kPer<T>, AHEAD = 4;
+    constexpr int W = kPer<T>, AHEAD = kAhead;
     const int64_t vectors = n / W;
     Sum s = {kLowest, 0.f};
     for (int64_t i = threadIdx.x; i < vectors; i += AHEAD * THREADS) {
@@ -93,8 +98,15 @@ __device__ __forceinline__ int64_t id_at(const DistillArgs &a, int64_t i) {
     return a.wide ? static_cast<const int64_t *>(a.ids)[i] : static_cast<const int32_t *>(a.ids)[i];
 }
 
-// By wave 0: the entries of the row; returns sum of p (log p - z / T), what the loss is but for lse.
-template <class T>
+// exp of a number in 64 bits, to 24 of them: the exponent of 2 in two parts, of which the hardware takes the first
+__device__ __forceinline__ float exp_of(double x) {
+    const double y = x * 1.44269504088896340736;
+    const float high = (float)y, low = (float)(y - (double)high);
+    return exp2_of(high) * fmaf(high > -INFINITY ? low : 0.f, 0.693147180559945309f, 1.f);
+}
+
+// By wave 0: the entries of the row; returns sum of p (log p - z / T), what the loss is but for lse.  LOSS: wanted; else p to 24 bits is enough.
+template <class T, bool LOSS = true>
 __device__ __forceinline__ double read_entries(const DistillArgs &a, int64_t row, Entries &s) {
     const int lane = threadIdx.x;
     const T *z = static_cast<const T *>(a.logits) + row * a.stride;
@@ -117,6 +129,19 @@ __device__ __forceinline__ double read_entries(const DistillArgs &a, int64_t row
 #pragma unroll
     for (int d = 32; d > 0; d /= 2) most = fmaxf(most, __shfl_xor(most, d));
     if (__any(odd)) most = NAN;
+    if constexpr (!LOSS) {
+        const double inverse = 1. / a.temperature;
+        double size = 0.;
+        for (int j = lane; j < a.top; j += 64) {
+            if (s.id[j] < 0) continue;
+            s.p[j] = exp_of(((double)s.p[j] - (double)most) * inverse);
+            size += (double)s.p[j];
+        }
+        size = 1. / wave_sum(size);
+        for (int j = lane; j < a.top; j += 64)
+            if (s.id[j] >= 0) s.p[j] = (float)((double)s.p[j] * size);
+        return 0.;
+    }
     double size = 0.;
     for (int j = lane; j < a.top; j += 64)
         if (s.id[j] >= 0) size += exp(((double)s.p[j] - (double)most) / a.temperature);
@@ -153,10 +178,23 @@ __device__ __forceinline__ Q<T, FROM_LSE> q_of(const DistillArgs &a, float ref, 
     return {(float)(inverse * 1.44269504088896340736), high, (float)(inverse - high), ref, factor};
 }
 
+// The columns of a row's entries once more, behind what all threads wrote (one that is named twice has both its probabilities).
+template <class T, int THREADS, bool FROM_LSE>
+__device__ __forceinline__ void write_entries(const DistillArgs &a, T *out, int64_t from, int64_t n, const Entries &s, const Q<T, FROM_LSE> &q, float d) {
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.top; j += THREADS) {
+        const int64_t at = (int64_t)s.id[j] - from;
+        if (s.id[j] < 0 || at < 0 || at >= n) continue;
+        float p = 0.f;
+        for (int i = 0; i < a.top; ++i) p += s.id[i] == s.id[j] ? s.p[i] : 0.f;
+        out[at] = from_f32<T>(q(s.z[j]) - p * d);
+    }
+}
+
 // The gradient of columns `from` .. `from + n` of a row whose entries are known.
 template <class T, int THREADS, bool FROM_LSE>
 __device__ __forceinline__ void write_gradient(const DistillArgs &a, int64_t row, int64_t from, int64_t n, const Entries &s, const Q<T, FROM_LSE> &q, float d) {
-    constexpr int W = kPer<T>, AHEAD = 4;
+    constexpr int W = kPer<T>, AHEAD = kAhead;
     const T *z = static_cast<const T *>(a.logits) + row * a.stride + from;
     T *out = static_cast<T *>(a.d_logits) + row * a.d_stride + from;
     const int64_t vectors = n / W;
@@ -170,7 +208,7 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &a, int64_t row
         Raw<T, W> raw[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
-            if (i + u * THREADS < vectors) load(z + (i + u * THREADS) * W, raw[u]);
+            if (i + u * THREADS < vectors) load<true>(z + (i + u * THREADS) * W, raw[u]);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             if (i + u * THREADS >= vectors) break;
@@ -178,22 +216,14 @@ __device__ __forceinline__ void write_gradient(const DistillArgs &a, int64_t row
             widen(raw[u], f);
 #pragma unroll
             for (int e = 0; e < W; ++e) f[e] = q(f[e]);
-            store(out + (i + u * THREADS) * W, f);
+            store<true>(out + (i + u * THREADS) * W, f);
         }
     }
     if (threadIdx.x < n - vectors * W) {
         const int64_t i = vectors * W + threadIdx.x;
         out[i] = from_f32<T>(q(to_f32(z[i])));
     }
-    // the entries' columns once more, behind what was written above (a column that is named twice has both its probabilities)
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.top; j += THREADS) {
-        const int64_t at = (int64_t)s.id[j] - from;
-        if (s.id[j] < 0 || at < 0 || at >= n) continue;
-        float p = 0.f;
-        for (int i = 0; i < a.top; ++i) p += s.id[i] == s.id[j] ? s.p[i] : 0.f;
-        out[at] = from_f32<T>(q(s.z[j]) - p * d);
-    }
+    write_entries<T, THREADS>(a, out, from, n, s, q, d);
 }
 
 // ---- a workgroup a row ----
@@ -210,10 +240,174 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a) {
         const double lse = lse_of(s, a);
         a.lse[row] = (float)lse;
         a.loss[row] = entries.any ? (float)(loss + lse) : 0.f;
+        if (!GRADIENT) a.partials[row] = {s.most, s.sum};
     }
     if constexpr (GRADIENT) {
         const float d_loss = a.d_loss[row];
         write_gradient<T, THREADS>(a, row, 0, a.cols, entries, q_of<T, false>(a, s.most, s.sum, d_loss), (float)(d_loss / a.temperature));
+    }
+}
+
+// ---- rows that stay in registers between sum and gradient: a workgroup goes from row to row, V vectors a thread.  As a vector's gradient is
+// written the next row's is asked for in its place, so that reading, writing and the sums of what has come go on together.  Thread j has
+// the row's entry j. ----
+template <class T>
+__device__ __forceinline__ void nothing(Raw<T, kPer<T>> &r) {           // columns of minus infinity
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.d[i] = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+}
+
+// (all threads' address and a thread's own 32 bits of bytes behind it: no address registers for each vector)
+template <class T>
+__device__ __forceinline__ T *vector_of(T *row, int64_t bytes, uint32_t own) {
+    typedef typename std::conditional<std::is_const<T>::value, const char, char>::type B;
+    return reinterpret_cast<T *>(reinterpret_cast<B *>(row) + bytes + own);
+}
+
+// What is widened again later is not kept wide, which would take the registers of more than one row.
+template <class T, int W>
+__device__ __forceinline__ void keep_narrow(Raw<T, W> &r) {
+#pragma unroll
+    for (int i = 0; i < Raw<T, W>::kWords; ++i) asm volatile("" : "+v"(r.d[i]));
+}
+
+// One thread's sum of what it has of the row's end
+__device__ __forceinline__ Sum begin(float z, float c) {
+    const float most = fmaxf(z, kLowest);
+    return {most, exp2_of((z - most) * c)};
+}
+template <class T, int THREADS, int V>
+__global__ __launch_bounds__(THREADS) void distill_rows_kernel(DistillArgs a) {
+    constexpr int W = kPer<T>, WAVES = THREADS / 64, AT_ONCE = 2;
+    static_assert(V % AT_ONCE == 0, "whole steps");
+    __shared__ Sum sums[WAVES];
+    __shared__ float tops[WAVES], probabilities[THREADS];
+    __shared__ double sizes[WAVES], losses[WAVES];
+    __shared__ int32_t columns[THREADS];
+    const int thread = (int)threadIdx.x, wave = thread >> 6;
+    const uint32_t lane = threadIdx.x * 16;             // bytes
+    const int32_t vectors = (int32_t)(a.cols / W), rest = (int32_t)(a.cols - (int64_t)vectors * W), top = (int32_t)a.top;
+    const float c = (float)(1.44269504088896340736 / a.temperature);
+    const double inverse = 1. / a.temperature;
+    Raw<T, W> raw[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) nothing(raw[v]);
+    float tail = -INFINITY;
+    int32_t id = -1;
+    float teacher = -INFINITY, z_entry = 0.f;
+    auto ask = [&](int64_t row, int32_t &id_, float &teacher_) {
+        if (thread < top) {
+            const int64_t i = id_at(a, row * top + thread);
+            teacher_ = a.teacher[row * top + thread];
+            id_ = i >= 0 && i < a.cols && teacher_ != -INFINITY ? (int32_t)i : -1;
+        }
+    };
+    int64_t row = blockIdx.x;
+    const T *z = static_cast<const T *>(a.logits) + row * a.stride;
+    ask(row, id, teacher);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v * THREADS + thread < vectors) load<true>(vector_of(z, v * THREADS * 16, lane), raw[v]);
+    if (thread < rest) tail = to_f32(z[vectors * W + thread]);
+    if (id >= 0) z_entry = to_f32(z[id]);
+    for (; row < a.rows; row += gridDim.x) {
+        const int64_t next = row + gridDim.x;
+        const bool more = next < a.rows;
+        const T *z_next = static_cast<const T *>(a.logits) + next * a.stride;
+        const float d_loss = a.d_loss[row];
+        int32_t id_next = -1;
+        float teacher_next = -INFINITY;
+        if (more) ask(next, id_next, teacher_next);
+        Sum s = begin(tail, c);
+#pragma unroll
+        for (int v = 0; v < V; v += AT_ONCE) {
+            float f[AT_ONCE][W], most = s.most;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                widen(raw[v + u], f[u]);
+#pragma unroll
+                for (int e = 0; e < W; ++e) most = fmaxf(most, f[u][e]);
+            }
+            s.sum *= exp2_of((s.most - most) * c);
+            s.most = most;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                float t = 0.f;
+#pragma unroll
+                for (int e = 0; e < W; ++e) t += exp2_of((f[u][e] - most) * c);
+                s.sum += t;
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) keep_narrow(raw[v]);
+        // (a teacher's logit that is no number makes all of them none)
+        float high = id < 0 ? -INFINITY : teacher != teacher ? INFINITY : teacher;
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) {
+            s.join(Sum{__shfl_xor(s.most, d), __shfl_xor(s.sum, d)}, c);
+            high = fmaxf(high, __shfl_xor(high, d));
+        }
+        if ((thread & 63) == 0) sums[wave] = s, tops[wave] = high;
+        __syncthreads();
+        s = sums[0];
+        high = tops[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            s.join(sums[w], c);
+            high = fmaxf(high, tops[w]);
+        }
+        const bool any = high > -INFINITY;
+        double p = 0.;
+        if (any && wave * 64 < top) {
+            double loss = 0.;
+            if (id >= 0) {
+                const double t = ((double)teacher - (double)high) * inverse;
+                p = exp(t);
+                if (p > 0. || p != p) loss = p * (t - (double)z_entry * inverse);
+            }
+            const double size = wave_sum(p);
+            loss = wave_sum(loss);
+            if ((thread & 63) == 0) sizes[wave] = size, losses[wave] = loss;
+        }
+        const Q<T, false> q = q_of<T, false>(a, s.most, s.sum, d_loss);
+        float z_entry_next = 0.f;
+        if (id_next >= 0) z_entry_next = to_f32(z_next[id_next]);
+        T *out = static_cast<T *>(a.d_logits) + row * a.d_stride;
+        const float tail_now = tail;
+        if (more && thread < rest) tail = to_f32(z_next[vectors * W + thread]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (v * THREADS + thread >= vectors) continue;
+            float f[W];
+            widen(raw[v], f);
+#pragma unroll
+            for (int e = 0; e < W; ++e) f[e] = any ? q(f[e]) : 0.f;
+            store<true>(vector_of(out, v * THREADS * 16, lane), f);
+            if (more) load<true>(vector_of(z_next, v * THREADS * 16, lane), raw[v]);
+        }
+        if (thread < rest) out[vectors * W + thread] = from_f32<T>(any ? q(tail_now) : 0.f);
+        __syncthreads();
+        double size = 0., loss = 0.;
+        for (int w = 0; w * 64 < top && w < WAVES; ++w) size += sizes[w], loss += losses[w];
+        if (thread == 0) {
+            const double lse = lse_of(s, a);
+            a.lse[row] = (float)lse;
+            a.loss[row] = any ? (float)(loss / size - log(size) + lse) : 0.f;
+        }
+        if (any) {
+            columns[thread] = id;
+            probabilities[thread] = (float)(p / size);
+            __syncthreads();
+            if (id >= 0) {
+                float sum = 0.f;
+                for (int i = 0; i < top; ++i) sum += columns[i] == id ? probabilities[i] : 0.f;
+                out[id] = from_f32<T>(q(z_entry) - sum * (float)(d_loss * inverse));
+            }
+        }
+        z = z_next;
+        id = id_next;
+        teacher = teacher_next;
+        z_entry = z_entry_next;
     }
 }
 
@@ -268,32 +462,29 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs a) {
     if (threadIdx.x == 0) write_loss(a, row, s, any);
 }
 
-// FROM_LSE: lse is given; else from the parts' sums
-template <class T, int THREADS, bool FROM_LSE>
-__global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillArgs a) {
+// A chunk of a row a workgroup, one step for each thread: one that goes on waits for its stores (4096 x 151936 in bf16 448 us, 498 with two
+// steps, 533 with a workgroup a row).  FROM_LSE: lse is given; else from the parts' sums.
+template <class T, bool FROM_LSE>
+__global__ __launch_bounds__(kChunkThreads) void distill_grad_kernel(DistillArgs a) {
     __shared__ Entries entries;
-    const int64_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-    const int64_t from = part * a.piece, n = from + a.piece < a.cols ? a.piece : a.cols - from;
-    // (the entries' logits are read in front of the first write of this workgroup; those of other parts are of no use here)
-    if (threadIdx.x < 64) {
-        DistillArgs own = a;
-        read_entries<T>(own, row, entries);
-    }
+    const int64_t row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+    const int64_t from = chunk * a.chunk, n = from + a.chunk < a.cols ? a.chunk : a.cols - from;
+    // (the entries' logits are read in front of the first write of this workgroup; those in other chunks are of no use here)
+    if (threadIdx.x < 64) read_entries<T, false>(a, row, entries);
     const float d_loss = a.d_loss[row];
     __syncthreads();
     const float d = (float)(d_loss / a.temperature);
     if constexpr (FROM_LSE) {
-        write_gradient<T, THREADS>(a, row, from, n, entries, q_of<T, true>(a, a.lse[row], 1., d_loss), d);
+        write_gradient<T, kChunkThreads>(a, row, from, n, entries, q_of<T, true>(a, a.lse[row], 1., d_loss), d);
     } else {
         const Sum s = joined(a, row, (float)(1.44269504088896340736 / a.temperature));
-        if (part == 0 && threadIdx.x == 0) write_loss(a, row, s, entries.any);
-        write_gradient<T, THREADS>(a, row, from, n, entries, q_of<T, false>(a, s.most, s.sum, d_loss), d);
+        if (a.parts > 1 && chunk == 0 && threadIdx.x == 0) write_loss(a, row, s, entries.any);
+        write_gradient<T, kChunkThreads>(a, row, from, n, entries, q_of<T, false>(a, s.most, s.sum, d_loss), d);
     }
 }
 
 // Parts of a row: where rows alone do not fill the chip, as many as make four workgroups a CU, of 2048 columns at least.
 constexpr int64_t kWanted = 1024, kLeast = 2048;
-constexpr size_t kWorkspace = kWanted * 16;           // a loss for each row and a sum for each part
 
 void divide(DistillArgs &a) {
     int64_t parts = a.rows > 0 ? kWanted / a.rows : 1;
@@ -302,39 +493,57 @@ void divide(DistillArgs &a) {
     parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
     a.piece = ((a.cols + parts - 1) / parts + 63) / 64 * 64;
     a.parts = (int32_t)((a.cols + a.piece - 1) / a.piece);
-    a.losses = reinterpret_cast<double *>(a.workspace);
-    a.partials = reinterpret_cast<DistillArgs::Part *>(a.workspace + kWanted * 8);
+    a.losses = reinterpret_cast<double *>(a.workspace);                                 // of each row where there are parts ...
+    a.partials = reinterpret_cast<DistillArgs::Part *>(a.workspace + kWanted * 8);      // ... and the sums of all parts, or of all rows
+}
+
+template <class T, bool FROM_LSE>
+int gradient_of(DistillArgs &a, hipStream_t st) {
+    a.chunk = kChunkThreads * kAhead * kPer<T>;
+    while (a.rows * ((a.cols + a.chunk - 1) / a.chunk) > kMostThreads / kChunkThreads) a.chunk *= 2;
+    a.chunks = (a.cols + a.chunk - 1) / a.chunk;
+    hipLaunchKernelGGL((distill_grad_kernel<T, FROM_LSE>), dim3((unsigned)(a.rows * a.chunks)), dim3(kChunkThreads), 0, st, a);
+    return (int)hipGetLastError();
+}
+
+template <class T, int THREADS, int V>
+int in_rows(const DistillArgs &a, hipStream_t st) {
+    const int64_t most = THREADS == 256 ? 768 : V <= 20 ? 512 : 256;
+    hipLaunchKernelGGL((distill_rows_kernel<T, THREADS, V>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(THREADS), 0, st, a);
+    return (int)hipGetLastError();
 }
 
 template <class T>
 int loss(DistillArgs &a, bool gradient, hipStream_t st) {
     constexpr int MANY = 1024, FEW = 256;
     divide(a);
+    const int64_t n = a.cols / kPer<T>;
+    const dim3 rows((unsigned)a.rows);
     if (a.parts > 1) {
         hipLaunchKernelGGL((distill_part_kernel<T, FEW>), dim3((unsigned)(a.rows * a.parts)), dim3(FEW), 0, st, a);
         if (int e = (int)hipGetLastError()) return e;
-        if (gradient) hipLaunchKernelGGL((distill_grad_kernel<T, FEW, false>), dim3((unsigned)(a.rows * a.parts)), dim3(FEW), 0, st, a);
-        else hipLaunchKernelGGL(distill_join_kernel, dim3((unsigned)a.rows), dim3(64), 0, st, a);
-    } else if (gradient) {
-        if (a.cols > 16384) hipLaunchKernelGGL((distill_row_kernel<T, MANY, true>), dim3((unsigned)a.rows), dim3(MANY), 0, st, a);
-        else hipLaunchKernelGGL((distill_row_kernel<T, FEW, true>), dim3((unsigned)a.rows), dim3(FEW), 0, st, a);
-    } else {
-        if (a.cols > 16384) hipLaunchKernelGGL((distill_row_kernel<T, MANY, false>), dim3((unsigned)a.rows), dim3(MANY), 0, st, a);
-        else hipLaunchKernelGGL((distill_row_kernel<T, FEW, false>), dim3((unsigned)a.rows), dim3(FEW), 0, st, a);
+        if (gradient) return gradient_of<T, false>(a, st);
+        hipLaunchKernelGGL(distill_join_kernel, rows, dim3(64), 0, st, a);
+        return (int)hipGetLastError();
     }
-    return (int)hipGetLastError();
-}
-
-template <class T>
-int grad(DistillArgs &a, hipStream_t st) {
-    divide(a);
-    hipLaunchKernelGGL((distill_grad_kernel<T, 256, true>), dim3((unsigned)(a.rows * a.parts)), dim3(256), 0, st, a);
-    return (int)hipGetLastError();
+    if (gradient) {
+        if (n <= 256 * 8) {
+            hipLaunchKernelGGL((distill_row_kernel<T, FEW, true>), rows, dim3(FEW), 0, st, a);
+            return (int)hipGetLastError();
+        }
+        if (n <= 256 * 16 && a.top <= 256) return in_rows<T, 256, 16>(a, st);
+        if (n <= 512 * 20 && a.top <= 512) return in_rows<T, 512, 20>(a, st);
+        if (n <= 512 * 38 && a.top <= 512) return in_rows<T, 512, 38>(a, st);
+    }
+    if (n > 4096) hipLaunchKernelGGL((distill_row_kernel<T, MANY, false>), rows, dim3(MANY), 0, st, a);
+    else hipLaunchKernelGGL((distill_row_kernel<T, FEW, false>), rows, dim3(FEW), 0, st, a);
+    if (int e = (int)hipGetLastError()) return e;
+    return gradient ? gradient_of<T, false>(a, st) : 0;
 }
 
 }  // namespace
 
-size_t distill_workspace(int64_t, int64_t) { return kWorkspace; }
+size_t distill_workspace(int64_t rows, int64_t) { return (size_t)(kWanted * 8) + sizeof(DistillArgs::Part) * (size_t)(rows > kWanted ? rows : kWanted); }
 
 int launch_distill_loss(const DistillArgs &args, bool f32, bool gradient, void *stream) {
     DistillArgs a = args;
@@ -347,7 +556,7 @@ int launch_distill_grad(const DistillArgs &args, bool f32, void *stream) {
     DistillArgs a = args;
     if (a.rows == 0) return 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return f32 ? grad<float>(a, st) : grad<bf16_t>(a, st);
+    return f32 ? gradient_of<float, true>(a, st) : gradient_of<bf16_t, true>(a, st);
 }
 
 }  // namespace rose

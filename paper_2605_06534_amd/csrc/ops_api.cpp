@@ -252,7 +252,7 @@ extern "C" rose_status rose_distill_loss(const void *logits, int32_t dtype, int6
     ROSE_CHECK(check_rows(lse, rows));
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::distill_workspace(rows, cols)));
     rose::DistillArgs a = {logits, rows, cols, stride, ids, id_bytes == 8, teacher, top, temperature, nullptr, loss, lse, nullptr, 0,
-                           static_cast<char *>(workspace), 0, 0, nullptr, nullptr};
+                           static_cast<char *>(workspace), 0, 0, 0, 0, nullptr, nullptr};
     return status_of(rose::launch_distill_loss(a, dtype == ROSE_DTYPE_F32, false, stream));
 }
 
@@ -267,7 +267,7 @@ extern "C" rose_status rose_distill_loss_grad(const void *logits, int32_t dtype,
     ROSE_CHECK(check_rows(lse, rows));
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::distill_workspace(rows, cols)));
     rose::DistillArgs a = {logits, rows, cols, stride, ids, id_bytes == 8, teacher, top, temperature, d_loss, loss, lse, d_logits, d_stride,
-                           static_cast<char *>(workspace), 0, 0, nullptr, nullptr};
+                           static_cast<char *>(workspace), 0, 0, 0, 0, nullptr, nullptr};
     return status_of(rose::launch_distill_loss(a, dtype == ROSE_DTYPE_F32, true, stream));
 }
 
@@ -279,7 +279,7 @@ extern "C" rose_status rose_distill_grad(const void *logits, int32_t dtype, int6
     ROSE_CHECK(check_rows(lse, rows));
     ROSE_CHECK(check_rows(d_loss, rows));
     rose::DistillArgs a = {logits, rows, cols, stride, ids, id_bytes == 8, teacher, top, temperature, d_loss, nullptr,
-                           const_cast<float *>(lse), d_logits, d_stride, nullptr, 0, 0, nullptr, nullptr};
+                           const_cast<float *>(lse), d_logits, d_stride, nullptr, 0, 0, 0, 0, nullptr, nullptr};
     return status_of(rose::launch_distill_grad(a, dtype == ROSE_DTYPE_F32, stream));
 }
 

@@ -110,9 +110,9 @@ struct DistillArgs {
     void *d_logits;                     // of the logits' type
     int64_t d_stride;
     char *workspace;
-    // the launchers': parts of a row, their columns and sums
+    // the launchers': parts of a row that are summed, their columns and sums; chunks of a row whose gradient is written, their columns
     int32_t parts;
-    int64_t piece;
+    int64_t piece, chunks, chunk;
     double *losses;
     struct Part {
         float most, sum;
