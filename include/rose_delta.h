@@ -681,7 +681,7 @@ rose_status rose_distill_loss_grad(const void *logits, int32_t dtype, int64_t ro
  *                call do not matter; calls that share one must be ordered on one stream
  * Products, differences and sums are formed in 64 bits.  Rows of zeros, or with a NaN, give some token in range.
  * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a workspace that is too small;
- * ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, or requests with 2^24 or more stretches of 4096 columns together.
+ * ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^31 or more rows or columns, or 2^18 or more requests.
  */
 rose_status rose_draft_verify_workspace_bytes(int64_t requests, int64_t cols, size_t *bytes);
 rose_status rose_draft_verify(const void *target, int64_t target_stride, const void *draft, int64_t draft_stride, int32_t dtype,

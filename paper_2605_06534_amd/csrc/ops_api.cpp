@@ -304,7 +304,7 @@ extern "C" rose_status rose_draft_verify(const void *target, int64_t target_stri
     ROSE_CHECK(check_workspace(workspace, workspace_bytes, rose::draft_verify_workspace(requests, cols)));
     if (!rose::draft_verify_fits(requests, cols)) return ROSE_ERR_UNSUPPORTED;
     rose::VerifyArgs a = {target, draft, cols, target_stride, draft_stride, drafted, token_bytes == 8, n_drafted, offsets, requests, uniforms,
-                          tokens, accepted, workspace, 0};
+                          tokens, accepted, static_cast<double *>(workspace), 0, 0};
     return status_of(rose::launch_draft_verify(a, dtype == ROSE_DTYPE_F32, stream));
 }
 

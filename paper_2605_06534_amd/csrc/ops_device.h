@@ -141,10 +141,30 @@ __device__ __forceinline__ float wave_sum(float v) {
     v = sum16(v);
     return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
 }
+template <int CONTROL>
+__device__ __forceinline__ double moved(double v) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CONTROL, 0xF, 0xF, true),
+                            __builtin_amdgcn_update_dpp(0, __double2loint(v), CONTROL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ double of_lane(double v, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
-    return v;
+    v += moved<0xB1>(v);
+    v += moved<0x4E>(v);
+    v += moved<0x141>(v);
+    v += moved<0x140>(v);
+    return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
+}
+// running sum over the lanes of a wave, each lane's own value with it: rows of 16 (what is shifted in from outside is zero), then rows in turn
+__device__ __forceinline__ double wave_running(double v) {
+    v += moved<0x111>(v);
+    v += moved<0x112>(v);
+    v += moved<0x114>(v);
+    v += moved<0x118>(v);
+    const int row = (threadIdx.x & 63) >> 4;
+    const double a = of_lane(v, 15), b = a + of_lane(v, 31), c = b + of_lane(v, 47);
+    return v + (row == 0 ? 0. : row == 1 ? a : row == 2 ? b : c);
 }
 
 // sums over a workgroup of WAVES waves, the same in every thread; `shared` may be used again at once

@@ -133,8 +133,8 @@ struct VerifyArgs {
     const float *uniforms;
     void *tokens;
     int32_t *accepted;
-    void *sums;
-    int64_t parts;                      // the launcher's
+    double *sums;                       // of each part
+    int64_t parts, part;                // the launcher's: parts of a row, and their columns
 };
 bool draft_verify_fits(int64_t requests, int64_t cols);        // into launches
 size_t draft_verify_workspace(int64_t requests, int64_t cols);

@@ -3,7 +3,11 @@
 // behind the last one of all a sample of p, by the inverse of the running sum.  A row's sum goes over all its columns, in 64 bits:
 // differences and sums of fp32 numbers are then exact but for the last of 53 bits.
 //
-// A row is cut into parts: one launch sums each part, a second one finds the part that the sample falls into and looks through that one.
+// A row is cut into up to 64 parts: one launch sums each part, a second one finds the part that the sample falls into (a lane a part) and looks
+// through that one.  Three trips to memory, one behind the other, say which row that is: offsets, tokens, their probabilities; each workgroup
+// makes them by itself (64 requests of 151936 columns in fp32: 13 us, 78 MB at 6 TB/s; 200 of 152064 in bf16 without drafts' probabilities
+// 17 us; a launch in front that makes them for all takes 3.3 us and saves 1.3).  What runs in sequence in the second launch, 6.5 us, are
+// its trips: sums, the part, the token.
 #include "ops_device.h"
 
 namespace rose {
@@ -12,11 +16,8 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kEach = 16;                           // neighbouring columns of a thread
-constexpr int64_t kPart = kThreads * kEach;
-
-struct Sums {
-    double over, whole;                             // of max(p - q, 0), and of p
-};
+constexpr int64_t kStep = kThreads * kEach;         // columns that a workgroup looks at together
+constexpr int kMostParts = 64;
 
 __device__ __forceinline__ int64_t id_at(const VerifyArgs &a, int64_t i) {
     return a.wide ? static_cast<const int64_t *>(a.drafted)[i] : static_cast<const int32_t *>(a.drafted)[i];
@@ -29,12 +30,16 @@ struct Request {
 };
 
 // (offsets that make no sense are brought within the tokens that there are)
-template <class T>
-__device__ __forceinline__ Request request_of(const VerifyArgs &a, int64_t r) {
+__device__ __forceinline__ Request within(const VerifyArgs &a, int64_t r) {
     int64_t first = a.offsets[r], end = a.offsets[r + 1];
     first = first < 0 ? 0 : first > a.n_drafted ? a.n_drafted : first;
     end = end < first ? first : end > a.n_drafted ? a.n_drafted : end;
-    Request q = {first, end - first, end - first};
+    return {first, end - first, end - first};
+}
+template <class T>
+__device__ __forceinline__ Request request_of(const VerifyArgs &a, int64_t r) {
+    Request q = within(a, r);
+    const int64_t first = q.first;
     const int lane = threadIdx.x & 63;
     for (int64_t i = 0; i < q.length; i += 64) {
         bool stays = true;
@@ -56,23 +61,26 @@ __device__ __forceinline__ Request request_of(const VerifyArgs &a, int64_t r) {
     return q;
 }
 
-// Weights of the columns that a thread has of a part: p, and what of it the draft left.
+// Weights of the columns that a thread has of a part: what the draft left of p; p itself where nothing was refused, or nothing is left.
 template <class T>
 struct Weights {
     float p[kEach], q[kEach];
     int64_t at;
     int n;
-    __device__ __forceinline__ Weights(const VerifyArgs &a, int64_t r, const Request &request, int64_t from) {
+    bool less;                                      // a draft's probabilities come off
+    __device__ __forceinline__ Weights(const VerifyArgs &a, int64_t r, const Request &request, int64_t from, bool left = true) {
         at = from + threadIdx.x * kEach;
         n = at >= a.cols ? 0 : a.cols - at < kEach ? (int)(a.cols - at) : kEach;
-        const T *target = static_cast<const T *>(a.target) + (request.row() + r) * a.target_stride + at;
-        read(target, p);
-        if (a.draft && request.refused()) {
+        less = left && a.draft && request.refused();
+        read(static_cast<const T *>(a.target) + (request.row() + r) * a.target_stride + at, p);
+        if (less) {
             read(static_cast<const T *>(a.draft) + request.row() * a.draft_stride + at, q);
-        } else {
-            const int64_t id = request.refused() ? id_at(a, request.row()) - at : -1;       // (no draft: all of the refused token is gone)
+        } else if (left && request.refused()) {
+            // (no draft: all of the refused token is gone)
+            const int64_t gone = id_at(a, request.row()) - at;
+            if (gone >= 0 && gone < kEach)
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) q[e] = e == id ? p[e] : 0.f;
+                for (int e = 0; e < kEach; ++e) p[e] = e == (int)gone ? 0.f : p[e];
         }
     }
     __device__ __forceinline__ void read(const T *from, float (&f)[kEach]) const {
@@ -81,121 +89,134 @@ struct Weights {
         else load(from, n, raw);
         widen(raw, f);
     }
-    __device__ __forceinline__ double over(int e) const { return fmax((double)p[e] - (double)q[e], 0.); }
+    // calls f(element, weight) for each
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+        if (less) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) f(e, (double)p[e] - (double)fminf(p[e], q[e]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) f(e, (double)p[e]);
+        }
+    }
 };
+
+// Sum of a part's weights, in thread 0.
+template <class T>
+__device__ __forceinline__ double part_sum(const VerifyArgs &a, int64_t r, const Request &request, int64_t part, bool left, double (&shared)[kWaves]) {
+    double s = 0.;
+    for (int64_t step = 0; step < a.part; step += kStep) {
+        const Weights<T> w(a, r, request, part * a.part + step, left);
+        w.each([&](int, double v) { s += v; });
+    }
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = shared[0];
+#pragma unroll
+    for (int v = 1; v < kWaves; ++v) s += shared[v];
+    return s;
+}
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void verify_sum_kernel(VerifyArgs a) {
-    __shared__ double shared[2 * kWaves];
+    __shared__ double shared[kWaves];
     const int64_t r = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const Request request = request_of<T>(a, r);
-    const Weights<T> w(a, r, request, part * kPart);
-    double s[2] = {0., 0.};
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        s[0] += w.over(e);
-        s[1] += (double)w.p[e];
-    }
-    block_sum<kWaves>(s, shared);
+    const double s = part_sum<T>(a, r, request, part, true, shared);
     if (threadIdx.x == 0) {
-        static_cast<Sums *>(a.sums)[blockIdx.x] = Sums{s[0], s[1]};
+        a.sums[blockIdx.x] = s;
         if (part == 0) a.accepted[r] = (int32_t)request.kept;
     }
 }
 
-// Running sums over the threads: up to this one's value, with it, and of all.  (One thread's end is the next one's start to the last bit.)
-struct Running {
-    double start, end, all;
-};
-__device__ __forceinline__ Running running(double v, double (&shared)[kWaves]) {
-    double s = v;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(s, d);
-        if ((int)(threadIdx.x & 63) >= d) s += o;
-    }
-    if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = s;
-    __syncthreads();
-    double front = 0., all = 0.;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < (int)(threadIdx.x >> 6)) front += shared[w];
-        all += shared[w];
-    }
-    __syncthreads();
-    const double up = __shfl_up(s, 1);
-    return {front + ((threadIdx.x & 63) ? up : 0.), front + s, all};
+// (one that ends where the next begins, to the last bit, so that no goal lies between them)
+__device__ __forceinline__ double start_of(double end) {
+    const double up = __shfl_up(end, 1);
+    return (threadIdx.x & 63) ? up : 0.;
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
-    __shared__ double shared[kWaves];
-    __shared__ double front_of;
-    __shared__ int64_t chosen;
-    __shared__ unsigned long long first, last;
+    __shared__ double ends[kWaves];
+    __shared__ int64_t chosen, last;
     const int64_t r = blockIdx.x;
-    const Request request = request_of<T>(a, r);
-    const Sums *sums = static_cast<const Sums *>(a.sums) + r * a.parts;
-    // all of the row, and which weights count
-    double over = 0., whole = 0.;
-    for (int64_t i = threadIdx.x; i < a.parts; i += kThreads) {
-        over += sums[i].over;
-        whole += sums[i].whole;
-    }
-    over = running(over, shared).all;
-    whole = running(whole, shared).all;
-    const bool left = over > 0.;
-    const double goal = (double)a.uniforms[request.first + request.length + r] * (left ? over : whole);
-    // the part that the sample falls into; none, by rounding or a number of 1: the last that has anything
-    if (threadIdx.x == 0) chosen = -1, last = 0, first = ~0ull;
-    __syncthreads();
-    double base = 0.;
-    for (int64_t i = 0; i < a.parts; i += kThreads) {
-        const double v = i + threadIdx.x < a.parts ? (left ? sums[i + threadIdx.x].over : sums[i + threadIdx.x].whole) : 0.;
-        const Running b = running(v, shared);
-        if (base + b.start <= goal && goal < base + b.end) {
-            chosen = i + threadIdx.x;
-            front_of = base + b.start;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double value = lane < a.parts ? a.sums[r * a.parts + lane] : 0.;
+    Request request = within(a, r);
+    request.kept = a.accepted[r];
+    const double u = a.uniforms[request.first + request.length + r];
+    if (threadIdx.x == 0) chosen = -1, last = -1;
+    auto put = [&](int64_t i, int64_t token) {
+        const int64_t at = request.first + r + i;
+        if (a.wide) static_cast<int64_t *>(a.tokens)[at] = token;
+        else static_cast<int32_t *>(a.tokens)[at] = (int32_t)token;
+    };
+    // the row's sum; where the draft leaves nothing the weights are the target's, which nobody has summed yet
+    double all = wave_sum(value);
+    const bool left = !request.refused() || all > 0.;
+    if (!left) {
+        for (int part = 0; part < a.parts; ++part) {
+            const double s = part_sum<T>(a, r, request, part, false, ends);
+            if (lane == part) value = s;
+            __syncthreads();
         }
-        if (v > 0.) atomicMax(&last, (unsigned long long)(i + threadIdx.x));
+        all = wave_sum(value);
+    }
+    // the part that the goal falls into, or by rounding, or with a number of 1, the last that has anything
+    const double goal = u * all, end = wave_running(value);
+    const uint64_t hit = __ballot(start_of(end) <= goal && goal < end), some = __ballot(value > 0.);
+    const int part = hit ? __builtin_ctzll(hit) : some ? 63 - __builtin_clzll(some) : 0;
+    double front = of_lane(start_of(end), part);
+    for (int64_t i = threadIdx.x; i <= request.length; i += kThreads)
+        if (i != request.kept) put(i, i < request.kept ? id_at(a, request.first + i) : -1);
+    // the column, a step of the part at a time
+    for (int64_t step = 0; step < a.part; step += kStep) {
+        const Weights<T> w(a, r, request, part * a.part + step, left);
+        double s = 0.;
+        int64_t end_of = -1;
+        w.each([&](int e, double v) {
+            s += v;
+            if (v > 0.) end_of = w.at + e;
+        });
+        const double within_wave = wave_running(s);
+        if (lane == 63) ends[wave] = within_wave;
+        __syncthreads();
+        double base = front, behind = front;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) {
+            if (v < wave) base += ends[v];
+            behind += ends[v];
+        }
+        const double to = base + within_wave, from = base + start_of(within_wave);
+        if (from <= goal && goal < to) {
+            // (the walk may end a bit short of where the sums do: then at the last column that has anything)
+            int64_t token = -1;
+            double run = from;
+            w.each([&](int e, double v) {
+                run += v;
+                if (token < 0 && v > 0. && goal < run) token = w.at + e;
+            });
+            if (token < 0) token = end_of;
+            chosen = token;
+        }
+        if (end_of >= 0) atomicMax(reinterpret_cast<long long *>(&last), (long long)end_of);
         __syncthreads();
         if (chosen >= 0) break;
-        base += b.all;
+        front = behind;
     }
-    const int64_t found = chosen >= 0 ? chosen : (int64_t)last;
-    const double found_front = chosen >= 0 ? front_of : base;
-    __syncthreads();
-    if (threadIdx.x == 0) last = 0;
-    // the column
-    const Weights<T> w(a, r, request, found * kPart);
-    double s = 0.;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) s += left ? w.over(e) : (double)w.p[e];
-    int64_t token = -1, end = -1;
-    double run = found_front + running(s, shared).start;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        const double v = left ? w.over(e) : (double)w.p[e];
-        run += v;
-        if (v > 0.) end = w.at + e;
-        if (v > 0. && token < 0 && goal < run) token = w.at + e;
-    }
-    // the first of them; none: the part's last column that has anything; nothing at all: the row's last column
-    if (token >= 0) atomicMin(&first, (unsigned long long)token);
-    if (end >= 0) atomicMax(&last, (unsigned long long)end + 1);
-    __syncthreads();
-    const int64_t sample = first != ~0ull ? (int64_t)first : last > 0 ? (int64_t)last - 1 : a.cols - 1;
-    for (int64_t i = threadIdx.x; i <= request.length; i += kThreads) {
-        const int64_t out = i < request.kept ? id_at(a, request.first + i) : i == request.kept ? sample : -1;
-        const int64_t at = request.first + r + i;
-        if (a.wide) static_cast<int64_t *>(a.tokens)[at] = out;
-        else static_cast<int32_t *>(a.tokens)[at] = (int32_t)out;
-    }
+    if (threadIdx.x == 0) put(request.kept, chosen >= 0 ? chosen : last >= 0 ? last : a.cols - 1);
 }
+
+// Parts of a row, of whole steps: 64 at most, so that a lane has each.
+int64_t part_of(int64_t cols) { return ((cols + kStep * kMostParts - 1) / (kStep * kMostParts)) * kStep; }
+int64_t parts_of(int64_t cols) { return (cols + part_of(cols) - 1) / part_of(cols); }
 
 template <class T>
 int verify(VerifyArgs &a, hipStream_t st) {
-    a.parts = (a.cols + kPart - 1) / kPart;
+    a.part = part_of(a.cols);
+    a.parts = parts_of(a.cols);
     hipLaunchKernelGGL(verify_sum_kernel<T>, dim3((unsigned)(a.requests * a.parts)), dim3(kThreads), 0, st, a);
     if (int e = (int)hipGetLastError()) return e;
     hipLaunchKernelGGL(verify_pick_kernel<T>, dim3((unsigned)a.requests), dim3(kThreads), 0, st, a);
@@ -204,9 +225,12 @@ int verify(VerifyArgs &a, hipStream_t st) {
 
 }  // namespace
 
-bool draft_verify_fits(int64_t requests, int64_t cols) { return requests * ((cols + kPart - 1) / kPart) <= kMostThreads / kThreads; }
+bool draft_verify_fits(int64_t requests, int64_t) { return requests < (1 << 18); }        // (64 parts of each are 2^24 workgroups)
 
-size_t draft_verify_workspace(int64_t requests, int64_t cols) { return (size_t)requests * ((cols + kPart - 1) / kPart) * sizeof(Sums); }
+size_t draft_verify_workspace(int64_t requests, int64_t cols) {
+    const int64_t steps = (cols + kStep - 1) / kStep;
+    return (size_t)requests * (steps < kMostParts ? steps : kMostParts) * sizeof(double);
+}
 
 int launch_draft_verify(const VerifyArgs &args, bool f32, void *stream) {
     VerifyArgs a = args;
