@@ -20,6 +20,7 @@ constexpr int kFew = 512;                           // rows that a workgroup loo
 constexpr int kMostSplit = 16;                      // parts of the sums over k
 constexpr int64_t kSplitRows = 32768;               // rows of partial sums, where there are parts
 constexpr int kSortThreads = 1024;
+constexpr int64_t kLarge = 32;                      // rows of each adapter on average from which on 64 go together
 
 __device__ __forceinline__ int64_t adapter_of(const AdapterArgs &a, int64_t row) {
     const int64_t id = a.wide ? static_cast<const int64_t *>(a.chosen)[row] : static_cast<const int32_t *>(a.chosen)[row];
@@ -103,11 +104,11 @@ struct Rows16 {
     __device__ __forceinline__ int64_t row(int64_t i) const { return list[i < n ? i : n - 1]; }
 };
 
-// ---- h = down x: a workgroup has RANKS tiles of ranks and a part of k; its waves share k (TILES = 1), or have a tile of rows each (4) ----
-template <int RANKS, int TILES, bool SORTED>
+// ---- h = down x: a workgroup has RANKS tiles of ranks and a part of k that its waves share ----
+template <int RANKS, bool SORTED>
 __global__ __launch_bounds__(kThreads) void adapter_down_kernel(AdapterArgs a) {
     __shared__ int32_t found[SORTED ? 1 : kFew];
-    __shared__ f32x4 sums[TILES == 1 ? (kWaves - 1) * RANKS * 64 : 1];
+    __shared__ f32x4 sums[(kWaves - 1) * RANKS * 64];
     const int64_t unit = blockIdx.x % a.units, rest = blockIdx.x / a.units;
     const int64_t split = rest % a.splits, rank0 = rest / a.splits * (RANKS * kTile);
     const Rows16<SORTED> rows(a, unit, found);
@@ -120,14 +121,14 @@ __global__ __launch_bounds__(kThreads) void adapter_down_kernel(AdapterArgs a) {
         const int64_t r = rank0 + t * kTile + in_tile;
         down[t] = static_cast<const bf16_t *>(a.down) + (rows.id * a.rank + (r < a.rank ? r : a.rank - 1)) * a.k + part * 8;
     }
-    for (int32_t tile = TILES == 1 ? 0 : wave * kTile; tile < rows.n; tile += TILES * kTile) {
+    for (int32_t tile = 0; tile < rows.n; tile += kTile) {
         const int64_t row = rows.row(tile + in_tile);
         const bf16_t *x = static_cast<const bf16_t *>(a.x) + row * a.x_stride + part * 8;
         f32x4 c[RANKS];
 #pragma unroll
         for (int t = 0; t < RANKS; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        constexpr int STEP = 64, STRIDE = TILES == 1 ? kWaves * STEP : STEP;
-        for (int64_t k = from + (TILES == 1 ? wave * STEP : 0); k < to; k += STRIDE) {
+        constexpr int STEP = 64;
+        for (int64_t k = from + wave * STEP; k < to; k += kWaves * STEP) {
             Raw8<bf16_t> xv[2], dv[2][RANKS];
             if (k + STEP <= a.k) {
 #pragma unroll
@@ -151,18 +152,16 @@ __global__ __launch_bounds__(kThreads) void adapter_down_kernel(AdapterArgs a) {
 #pragma unroll
                 for (int t = 0; t < RANKS; ++t) c[t] = multiply(dv[h][t], xv[h], c[t]);
         }
-        if constexpr (TILES == 1) {
-            __syncthreads();
-            if (wave > 0)
+        __syncthreads();
+        if (wave > 0)
 #pragma unroll
-                for (int t = 0; t < RANKS; ++t) sums[((wave - 1) * RANKS + t) * 64 + lane] = c[t];
-            __syncthreads();
-            if (wave > 0) continue;
+            for (int t = 0; t < RANKS; ++t) sums[((wave - 1) * RANKS + t) * 64 + lane] = c[t];
+        __syncthreads();
+        if (wave > 0) continue;
 #pragma unroll
-            for (int w = 0; w < kWaves - 1; ++w)
+        for (int w = 0; w < kWaves - 1; ++w)
 #pragma unroll
-                for (int t = 0; t < RANKS; ++t) c[t] += sums[(w * RANKS + t) * 64 + lane];
-        }
+            for (int t = 0; t < RANKS; ++t) c[t] += sums[(w * RANKS + t) * 64 + lane];
         if (tile + in_tile < rows.n) {
             float *h = a.h + (split * a.m + row) * a.ranks + rank0 + part * 4;
 #pragma unroll
@@ -247,7 +246,7 @@ struct Piece<bf16_t> {
     static __device__ __forceinline__ int column(int t, int i) { return t / 2 * 32 + i / 4 * 8 + (t & 1) * 4 + (i & 3); }
 };
 
-template <class O, int STEPS, int TILES, bool SORTED, bool ODD>
+template <class O, int STEPS, bool SORTED, bool ODD>
 __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
     typedef Piece<O> P;
     __shared__ int32_t found[SORTED ? 1 : kFew];
@@ -258,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
     const float scale = a.scales ? a.scales[rows.id] : 1.f;
     const bf16_t *up = static_cast<const bf16_t *>(a.up);
     const int64_t from = chunk * a.columns, to = from + a.columns < a.n ? from + a.columns : a.n;
-    for (int32_t tile = TILES == 1 ? 0 : wave * kTile; tile < rows.n; tile += TILES * kTile) {
+    for (int32_t tile = 0; tile < rows.n; tile += kTile) {
         const int64_t row = rows.row(tile + in_tile);
         const bool here = tile + in_tile < rows.n;
         Raw8<bf16_t> h[STEPS ? STEPS : 1][3];
@@ -266,8 +265,8 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) inner(a, row, s * 32 + part * 8, scale, h[s]);
         O *out = static_cast<O *>(a.out) + row * a.out_stride;
-        constexpr int STRIDE = TILES == 1 ? kWaves * P::kColumns : P::kColumns;
-        for (int64_t n = from + (TILES == 1 ? wave * P::kColumns : 0); n < to; n += STRIDE) {
+        constexpr int STRIDE = kWaves * P::kColumns;
+        for (int64_t n = from + wave * P::kColumns; n < to; n += STRIDE) {
             const bool whole = n + P::kColumns <= a.n;
             Raw<O, P::kPer> old[P::kVectors];
             if (whole && here)
@@ -329,6 +328,191 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
     }
 }
 
+// ---- many rows of each adapter: tiles of 64 rows whose operands go through LDS.  What a lane of a matrix instruction needs lies in 16 rows
+// of memory next to each other's lanes, and such a load takes 64 cycles for its 16 lines a quarter; so rows are read along their length into
+// LDS, and results are laid out so that lanes next to each other have columns next to each other (8192 rows of 300 each, rank 64: the first
+// product 74 us without LDS, DOWN_US so; the second 164 and UP_US). ----
+constexpr int kRows = 64;                           // of a group
+constexpr int kDepth = 64;                          // elements of k at a time: 8 vectors
+constexpr int kUpColumns = 128;                     // of out, a workgroup
+
+// Place of a row's vector c in LDS: rows one behind the other, vectors moved about by a number of the row so that lanes' rows fall on other banks
+__device__ __forceinline__ int place(int row, int c, int vectors, int by) { return (row * vectors + (c ^ (by & (vectors - 1)))) * 8; }
+
+template <int RANKS>
+__global__ __launch_bounds__(kThreads) void adapter_down_tiles_kernel(AdapterArgs a) {
+    constexpr int VECTORS = kDepth / 8, XS = kRows * VECTORS / kThreads, DS = RANKS * kTile * VECTORS, D_EACH = (DS + kThreads - 1) / kThreads;
+    __shared__ __align__(16) bf16_t x_tile[2][kRows * kDepth], d_tile[2][RANKS * kTile * kDepth];
+    const int64_t unit = blockIdx.x % a.units, rest = blockIdx.x / a.units;
+    const int64_t split = rest % a.splits, rank0 = rest / a.splits * (RANKS * kTile);
+    const AdapterArgs::Group g = a.groups[unit];
+    if (g.n == 0) return;
+    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, in_tile = lane & 15, part = lane >> 4;
+    const int64_t from = split * a.share, to = from + a.share < a.k ? from + a.share : a.k;
+    const bf16_t *x[XS], *down[D_EACH];
+#pragma unroll
+    for (int i = 0; i < XS; ++i) {
+        const int row = (thread + i * kThreads) / VECTORS;
+        x[i] = static_cast<const bf16_t *>(a.x) + a.order[g.first + (row < g.n ? row : g.n - 1)] * a.x_stride + thread % VECTORS * 8;
+    }
+#pragma unroll
+    for (int i = 0; i < D_EACH; ++i) {
+        const int64_t r = rank0 + (thread + i * kThreads) / VECTORS;
+        down[i] = static_cast<const bf16_t *>(a.down) + (g.adapter * a.rank + (r < a.rank ? r : a.rank - 1)) * a.k + thread % VECTORS * 8;
+    }
+    Raw8<bf16_t> xv[XS], dv[D_EACH];
+    auto ask = [&](int64_t k) {
+        const int64_t left = a.k - k - thread % VECTORS * 8;
+        const int n = left < 0 ? 0 : left < 8 ? (int)left : 8;
+#pragma unroll
+        for (int i = 0; i < XS; ++i)
+            if (n == 8) load(x[i] + k, xv[i]);
+            else load(x[i] + k, n, xv[i]);
+#pragma unroll
+        for (int i = 0; i < D_EACH; ++i)
+            if (n == 8) load(down[i] + k, dv[i]);
+            else load(down[i] + k, n, dv[i]);
+    };
+    auto put = [&](bf16_t *tile, int q, const Raw8<bf16_t> &v) {
+        const int row = q / VECTORS;
+        *reinterpret_cast<u32x4 *>(tile + place(row, q % VECTORS, VECTORS, row)) = u32x4{v.d[0], v.d[1], v.d[2], v.d[3]};
+    };
+    auto get = [&](const bf16_t *tile, int row, int c) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + place(row, c, VECTORS, row));
+        return Raw8<bf16_t>{{v[0], v[1], v[2], v[3]}};
+    };
+    f32x4 c[RANKS];
+#pragma unroll
+    for (int t = 0; t < RANKS; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (from < to) ask(from);
+    int buffer = 0;
+    for (int64_t k = from; k < to; k += kDepth, buffer ^= 1) {
+#pragma unroll
+        for (int i = 0; i < XS; ++i) put(x_tile[buffer], thread + i * kThreads, xv[i]);
+#pragma unroll
+        for (int i = 0; i < D_EACH; ++i)
+            if (DS % kThreads == 0 || thread + i * kThreads < DS) put(d_tile[buffer], thread + i * kThreads, dv[i]);
+        // (one barrier a step: the buffer that the next step fills was last read in front of this one)
+        __syncthreads();
+        if (k + kDepth < to) ask(k + kDepth);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const Raw8<bf16_t> xf = get(x_tile[buffer], wave * kTile + in_tile, h * 4 + part);
+#pragma unroll
+            for (int t = 0; t < RANKS; ++t) c[t] = multiply(get(d_tile[buffer], t * kTile + in_tile, h * 4 + part), xf, c[t]);
+        }
+    }
+    if (wave * kTile + in_tile >= g.n) return;
+    float *h = a.h + (split * a.m + g.first + wave * kTile + in_tile) * a.ranks + rank0 + part * 4;
+#pragma unroll
+    for (int t = 0; t < RANKS; ++t)
+        if (rank0 + t * kTile < a.ranks) *reinterpret_cast<f32x4 *>(h + t * kTile) = c[t];
+}
+
+// scale * h, its parts added in order, in three numbers of 8 bits, as the lanes of the second product hold them: a wave a tile and 32 ranks
+__global__ __launch_bounds__(kThreads) void adapter_cut_kernel(AdapterArgs a) {
+    const int64_t at = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6), steps = (a.rank + 31) / 32;
+    const int lane = threadIdx.x & 63, in_tile = lane & 15, part = lane >> 4;
+    if (at >= a.units * (kRows / kTile) * steps) return;
+    const int64_t step = at % steps, tile = at / steps, unit = tile / (kRows / kTile);
+    const AdapterArgs::Group g = a.groups[unit];
+    const int row = (int)(tile % (kRows / kTile)) * kTile + in_tile;
+    if (g.n <= row - in_tile) return;
+    Raw8<bf16_t> out[3];
+    inner(a, g.first + (row < g.n ? row : g.n - 1), step * 32 + part * 8, a.scales ? a.scales[g.adapter] : 1.f, out);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        *reinterpret_cast<u32x4 *>(a.cut + ((at * 3 + i) * 64 + lane) * 8) = u32x4{out[i].d[0], out[i].d[1], out[i].d[2], out[i].d[3]};
+}
+
+// STEPS: of 32 ranks that are in LDS at a time.  Rows of out are the rows of the results here, columns their columns: a lane has 16 bytes of
+// each of four rows.
+template <class O, int STEPS, bool ODD>
+__global__ __launch_bounds__(kThreads) void adapter_up_tiles_kernel(AdapterArgs a) {
+    constexpr int VECTORS = STEPS * 4, EACH = kUpColumns * VECTORS / kThreads, PER = 16 / (int)sizeof(O), WIDTH = 16 * PER, PASSES = kUpColumns / WIDTH;
+    __shared__ __align__(16) bf16_t up_tile[kUpColumns * STEPS * 32];
+    const int64_t unit = blockIdx.x % a.units, n0 = blockIdx.x / a.units * kUpColumns;
+    const AdapterArgs::Group g = a.groups[unit];
+    if (g.n == 0) return;
+    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, in_tile = lane & 15, part = lane >> 4;
+    const bool busy = wave * kTile < g.n;
+    const bf16_t *up = static_cast<const bf16_t *>(a.up);
+    // the lane's four rows of out, and what is there
+    O *out[4];
+    bool here[4];
+    Raw<O, PER> old[PASSES][4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const int row = wave * kTile + part * 4 + v;
+        here[v] = row < g.n;
+        out[v] = static_cast<O *>(a.out) + a.order[g.first + (here[v] ? row : g.n - 1)] * a.out_stride + n0 + in_tile * PER;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p)
+            if (here[v] && n0 + p * WIDTH + in_tile * PER + PER <= a.n) load(out[v] + p * WIDTH, old[p][v]);
+    }
+    f32x4 c[PASSES][PER];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int t = 0; t < PER; ++t) c[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t steps = (a.rank + 31) / 32;
+    const bf16_t *cut = a.cut + ((unit * (kRows / kTile) + wave) * steps * 3 * 64 + lane) * 8;
+    for (int64_t first = 0; first < steps; first += STEPS) {
+        Raw8<bf16_t> h[STEPS][3];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (busy && first + s < steps) {
+#pragma unroll
+                for (int i = 0; i < 3; ++i) load(cut + ((first + s) * 3 + i) * 64 * 8, h[s][i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i) zero(h[s][i]);
+            }
+        if (first > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int q = thread + i * kThreads, row = q / VECTORS, vector = q % VECTORS;
+            const int64_t column = n0 + row < a.n ? n0 + row : a.n - 1;
+            Raw8<bf16_t> v;
+            read_up<ODD>(a, up, (g.adapter * a.n + column) * a.rank, first * 32 + vector * 8, v);
+            *reinterpret_cast<u32x4 *>(up_tile + place(row, vector, VECTORS, row / PER)) = u32x4{v.d[0], v.d[1], v.d[2], v.d[3]};
+        }
+        __syncthreads();
+        if (!busy) continue;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+                for (int t = 0; t < PER; ++t) {
+                    const int row = p * WIDTH + in_tile * PER + t;
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(up_tile + place(row, s * 4 + part, VECTORS, row / PER));
+                    const Raw8<bf16_t> uv = {{v[0], v[1], v[2], v[3]}};
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) c[p][t] = multiply(h[s][i], uv, c[p][t]);
+                }
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (!here[v]) continue;
+            const int64_t column = n0 + p * WIDTH + in_tile * PER;
+            O *q = out[v] + p * WIDTH;
+            if (column + PER <= a.n) {
+                float f[PER];
+                widen(old[p][v], f);
+#pragma unroll
+                for (int t = 0; t < PER; ++t) f[t] += c[p][t][v];
+                store(q, f);
+            } else {
+#pragma unroll
+                for (int t = 0; t < PER; ++t)
+                    if (column + t < a.n) q[t] = from_f32<O>(to_f32(q[t]) + c[p][t][v]);
+            }
+        }
+}
+
 int64_t padded(int64_t rank) { return (rank + kTile - 1) / kTile * kTile; }
 
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -337,47 +521,80 @@ int64_t split_rows(int64_t m) { return m * kMostSplit < kSplitRows ? m * kMostSp
 
 int64_t clamp(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 
-template <int RANKS, int TILES, bool SORTED>
+template <int RANKS, bool SORTED>
 int down(const AdapterArgs &a, hipStream_t st) {
     const int64_t blocks = (a.rank + RANKS * kTile - 1) / (RANKS * kTile);
-    hipLaunchKernelGGL((adapter_down_kernel<RANKS, TILES, SORTED>), dim3((unsigned)(a.units * a.splits * blocks)), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((adapter_down_kernel<RANKS, SORTED>), dim3((unsigned)(a.units * a.splits * blocks)), dim3(kThreads), 0, st, a);
     return (int)hipGetLastError();
 }
-template <int TILES, bool SORTED>
+template <bool SORTED>
 int down(const AdapterArgs &a, hipStream_t st) {
-    return a.rank <= 16 ? down<1, TILES, SORTED>(a, st) : a.rank <= 32 ? down<2, TILES, SORTED>(a, st) : down<4, TILES, SORTED>(a, st);
+    return a.rank <= 16 ? down<1, SORTED>(a, st) : a.rank <= 32 ? down<2, SORTED>(a, st) : down<4, SORTED>(a, st);
 }
 
-template <class O, int TILES, bool SORTED, bool ODD>
+template <class O, bool SORTED, bool ODD>
 int up(const AdapterArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(a.units * ((a.n + a.columns - 1) / a.columns))), block(kThreads);
-    if (a.rank <= 32) hipLaunchKernelGGL((adapter_up_kernel<O, 1, TILES, SORTED, ODD>), grid, block, 0, st, a);
-    else if (a.rank <= 64) hipLaunchKernelGGL((adapter_up_kernel<O, 2, TILES, SORTED, ODD>), grid, block, 0, st, a);
-    else if (a.rank <= 128) hipLaunchKernelGGL((adapter_up_kernel<O, 4, TILES, SORTED, ODD>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((adapter_up_kernel<O, 0, TILES, SORTED, ODD>), grid, block, 0, st, a);
+    if (a.rank <= 32) hipLaunchKernelGGL((adapter_up_kernel<O, 1, SORTED, ODD>), grid, block, 0, st, a);
+    else if (a.rank <= 64) hipLaunchKernelGGL((adapter_up_kernel<O, 2, SORTED, ODD>), grid, block, 0, st, a);
+    else if (a.rank <= 128) hipLaunchKernelGGL((adapter_up_kernel<O, 4, SORTED, ODD>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((adapter_up_kernel<O, 0, SORTED, ODD>), grid, block, 0, st, a);
     return (int)hipGetLastError();
 }
 
-template <int TILES, bool SORTED>
-int both(AdapterArgs &a, bool out_f32, hipStream_t st) {
-    // Parts of k: as many as make four workgroups a CU, of 256 elements at least.  Parts of n: eight a CU, of 256 columns at least.
+// Parts of k: as many as make four workgroups a CU, of 256 elements at least.
+void divide(AdapterArgs &a) {
     const int64_t blocks = a.rank <= 64 ? 1 : (a.rank + 63) / 64;
     a.splits = clamp(1024 / (a.units * blocks), 1, clamp(split_rows(a.m) / a.m, 1, kMostSplit));
     a.splits = clamp(a.splits, 1, a.k > 256 ? (a.k + 255) / 256 : 1);
     a.share = ((a.k + a.splits - 1) / a.splits + 255) / 256 * 256;
     if (a.k > 0) a.splits = (a.k + a.share - 1) / a.share;
+}
+
+template <int RANKS>
+int down_tiles(const AdapterArgs &a, hipStream_t st) {
+    const int64_t blocks = (a.rank + RANKS * kTile - 1) / (RANKS * kTile);
+    hipLaunchKernelGGL((adapter_down_tiles_kernel<RANKS>), dim3((unsigned)(a.units * a.splits * blocks)), dim3(kThreads), 0, st, a);
+    return (int)hipGetLastError();
+}
+
+template <class O, bool ODD>
+int up_tiles(const AdapterArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)(a.units * ((a.n + kUpColumns - 1) / kUpColumns))), block(kThreads);
+    if (a.rank <= 32) hipLaunchKernelGGL((adapter_up_tiles_kernel<O, 1, ODD>), grid, block, 0, st, a);
+    else if (a.rank <= 64) hipLaunchKernelGGL((adapter_up_tiles_kernel<O, 2, ODD>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((adapter_up_tiles_kernel<O, 4, ODD>), grid, block, 0, st, a);
+    return (int)hipGetLastError();
+}
+
+int in_tiles(AdapterArgs &a, bool out_f32, hipStream_t st) {
+    divide(a);
+    if (int e = a.rank <= 16 ? down_tiles<1>(a, st) : a.rank <= 32 ? down_tiles<2>(a, st) : down_tiles<4>(a, st)) return e;
+    const int64_t waves = a.units * (kRows / kTile) * ((a.rank + 31) / 32);
+    hipLaunchKernelGGL(adapter_cut_kernel, dim3((unsigned)((waves + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a);
+    if (int e = (int)hipGetLastError()) return e;
+    if (a.rank % 8) return out_f32 ? up_tiles<float, true>(a, st) : up_tiles<bf16_t, true>(a, st);
+    return out_f32 ? up_tiles<float, false>(a, st) : up_tiles<bf16_t, false>(a, st);
+}
+
+// Parts of n: eight workgroups a CU, of 256 columns at least.
+template <bool SORTED>
+int both(AdapterArgs &a, bool out_f32, hipStream_t st) {
+    divide(a);
     const int64_t chunks = clamp(2048 / a.units, 1, (a.n + 255) / 256);
     a.columns = ((a.n + chunks - 1) / chunks + 255) / 256 * 256;
-    if (int e = down<TILES, SORTED>(a, st)) return e;
-    if (a.rank % 8) return out_f32 ? up<float, TILES, SORTED, true>(a, st) : up<bf16_t, TILES, SORTED, true>(a, st);
-    return out_f32 ? up<float, TILES, SORTED, false>(a, st) : up<bf16_t, TILES, SORTED, false>(a, st);
+    if (int e = down<SORTED>(a, st)) return e;
+    if (a.rank % 8) return out_f32 ? up<float, SORTED, true>(a, st) : up<bf16_t, SORTED, true>(a, st);
+    return out_f32 ? up<float, SORTED, false>(a, st) : up<bf16_t, SORTED, false>(a, st);
 }
 
 }  // namespace
 
 size_t adapter_linear_workspace(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank) {
     (void)n, (void)k;
-    return whole((size_t)split_rows(m) * padded(rank) * 4) + whole((size_t)m * 4) + (size_t)(m / kTile + adapters) * sizeof(AdapterArgs::Group);
+    const int64_t tiled = m / kRows + (adapters < m / kLarge ? adapters : m / kLarge);
+    return whole((size_t)split_rows(m) * padded(rank) * 4) + whole((size_t)m * 4) + whole((size_t)(m / kTile + adapters) * sizeof(AdapterArgs::Group)) +
+           (size_t)tiled * kRows * ((rank + 31) / 32 * 32) * 6;
 }
 
 int launch_adapter_linear(const AdapterArgs &args, bool out_f32, void *stream) {
@@ -389,17 +606,18 @@ int launch_adapter_linear(const AdapterArgs &args, bool out_f32, void *stream) {
     // Few rows, and few of each adapter: no launch that sorts.
     if (a.m <= 64 || (a.m <= kFew && a.m <= 8 * a.adapters)) {
         a.units = a.adapters <= a.m ? a.adapters : a.m;
-        return both<1, false>(a, out_f32, st);
+        return both<false>(a, out_f32, st);
     }
     char *at = a.workspace + whole((size_t)split_rows(a.m) * a.ranks * 4);
     a.order = reinterpret_cast<int32_t *>(at);
     a.groups = reinterpret_cast<AdapterArgs::Group *>(at + whole((size_t)a.m * 4));
-    const bool large = a.m >= 32 * a.adapters;
-    a.group = large ? 4 * kTile : kTile;
+    a.cut = reinterpret_cast<bf16_t *>(at + whole((size_t)a.m * 4) + whole((size_t)(a.m / kTile + a.adapters) * sizeof(AdapterArgs::Group)));
+    const bool large = a.m >= kLarge * a.adapters;
+    a.group = large ? kRows : kTile;
     a.units = a.m / a.group + a.adapters;
     hipLaunchKernelGGL(adapter_sort_kernel, dim3((unsigned)a.adapters), dim3(kSortThreads), 0, st, a);
     if (int e = (int)hipGetLastError()) return e;
-    return large ? both<4, true>(a, out_f32, st) : both<1, true>(a, out_f32, st);
+    return large ? in_tiles(a, out_f32, st) : both<true>(a, out_f32, st);
 }
 
 }  // namespace rose

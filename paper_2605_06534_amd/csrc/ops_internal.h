@@ -140,6 +140,7 @@ bool draft_verify_fits(int64_t requests, int64_t cols);        // into launches
 size_t draft_verify_workspace(int64_t requests, int64_t cols);
 int launch_draft_verify(const VerifyArgs &a, bool f32, void *stream);
 
+struct bf16_t;
 struct AdapterArgs {
     const void *x, *down, *up;
     const float *scales;                // may be null
@@ -153,6 +154,7 @@ struct AdapterArgs {
     int64_t ranks, splits, share;       // ranks in whole tiles; parts of k, and elements of one
     int64_t columns;                    // of a workgroup
     int64_t units, group;               // groups, or adapters to look for; rows of a group, at most
+    bf16_t *cut;                        // scale * h in three numbers of 8 bits
     int32_t *order;
     struct Group {
         int32_t adapter, first, n;
