@@ -39,35 +39,46 @@ __device__ __forceinline__ f32x4 multiply(const Raw8<bf16_t> &p, const Raw8<bf16
 // less / group + a on: the next adapter's begin behind them, since floor(x / g) + 1 >= ceil(y / g) + floor((x - y) / g).
 __global__ __launch_bounds__(kSortThreads) void adapter_sort_kernel(AdapterArgs a) {
     constexpr int WAVES = kSortThreads / 64;
-    __shared__ int64_t less_of[WAVES], mine_of[WAVES];
-    const int64_t id = blockIdx.x;
+    __shared__ int32_t less_of[WAVES], mine_of[WAVES];
+    const int32_t id = (int32_t)blockIdx.x, m = (int32_t)a.m, group = (int32_t)a.group;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t share = ((a.m + WAVES - 1) / WAVES + 63) / 64 * 64, from = wave * share, to = from + share < a.m ? from + share : a.m;
-    int64_t less = 0, mine = 0;
-    for (int64_t i = from; i < to; i += 64) {
-        const int64_t c = i + lane < to ? adapter_of(a, i + lane) : -1;
-        less += __popcll(__ballot(c >= 0 && c < id));
-        mine += __popcll(__ballot(c == id));
+    const int32_t share = ((m + WAVES - 1) / WAVES + 63) / 64 * 64, from = wave * share < m ? wave * share : m, to = from + share < m ? from + share : m;
+    constexpr int AHEAD = 8;                        // (rows that are asked for together)
+    int32_t less = 0, mine = 0;
+    for (int32_t i = from; i < to; i += 64 * AHEAD) {
+        int32_t c[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) c[u] = i + 64 * u + lane < to ? (int32_t)adapter_of(a, i + 64 * u + lane) : -1;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            less += __popcll(__ballot(c[u] >= 0 && c[u] < id));
+            mine += __popcll(__ballot(c[u] == id));
+        }
     }
     if (lane == 0) less_of[wave] = less, mine_of[wave] = mine;
     __syncthreads();
-    int64_t all_less = 0, all_mine = 0, front = 0;
+    int32_t all_less = 0, all_mine = 0, front = 0;
     for (int w = 0; w < WAVES; ++w) {
         all_less += less_of[w];
         if (w < wave) front += mine_of[w];
         all_mine += mine_of[w];
     }
-    for (int64_t i = from; i < to; i += 64) {
-        const bool here = i + lane < to && adapter_of(a, i + lane) == id;
-        const uint64_t rows = __ballot(here);
-        if (here) a.order[all_less + front + __popcll(rows & ((1ull << lane) - 1))] = (int32_t)(i + lane);
-        front += __popcll(rows);
+    for (int32_t i = from; mine > 0 && i < to; i += 64 * AHEAD) {
+        int32_t c[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) c[u] = i + 64 * u + lane < to ? (int32_t)adapter_of(a, i + 64 * u + lane) : -1;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const uint64_t rows = __ballot(c[u] == id);
+            if (c[u] == id) a.order[all_less + front + __popcll(rows & ((1ull << lane) - 1))] = i + 64 * u + lane;
+            front += __popcll(rows);
+        }
     }
-    const int64_t first = all_less / a.group + id;
-    const int64_t end = id + 1 == a.adapters ? a.units : (all_less + all_mine) / a.group + id + 1;
-    for (int64_t s = first + threadIdx.x; s < end; s += kSortThreads) {
-        const int64_t left = all_mine - (s - first) * a.group;
-        a.groups[s] = {(int32_t)id, (int32_t)(all_less + (s - first) * a.group), (int32_t)(left < 0 ? 0 : left < a.group ? left : a.group)};
+    const int32_t first = all_less / group + id;
+    const int32_t end = id + 1 == a.adapters ? (int32_t)a.units : (all_less + all_mine) / group + id + 1;
+    for (int32_t s = first + (int32_t)threadIdx.x; s < end; s += kSortThreads) {
+        const int32_t left = all_mine - (s - first) * group;
+        a.groups[s] = {id, all_less + (s - first) * group, left < 0 ? 0 : left < group ? left : group};
     }
 }
 
@@ -428,28 +439,17 @@ __global__ __launch_bounds__(kThreads) void adapter_cut_kernel(AdapterArgs a) {
 // STEPS: of 32 ranks that are in LDS at a time.  Rows of out are the rows of the results here, columns their columns: a lane has 16 bytes of
 // each of four rows.
 template <class O, int STEPS, bool ODD>
-__global__ __launch_bounds__(kThreads) void adapter_up_tiles_kernel(AdapterArgs a) {
+__global__ __launch_bounds__(kThreads, STEPS == 1 ? 4 : 1) void adapter_up_tiles_kernel(AdapterArgs a) {
     constexpr int VECTORS = STEPS * 4, EACH = kUpColumns * VECTORS / kThreads, PER = 16 / (int)sizeof(O), WIDTH = 16 * PER, PASSES = kUpColumns / WIDTH;
     __shared__ __align__(16) bf16_t up_tile[kUpColumns * STEPS * 32];
-    const int64_t unit = blockIdx.x % a.units, n0 = blockIdx.x / a.units * kUpColumns;
+    // neighbouring groups, which have the same adapter, on the same of 8 dies (workgroups go to them in turn)
+    const int64_t each = (a.units + 7) / 8, slot = blockIdx.x % (each * 8), unit = slot % 8 * each + slot / 8, n0 = blockIdx.x / (each * 8) * kUpColumns;
+    if (unit >= a.units) return;
     const AdapterArgs::Group g = a.groups[unit];
     if (g.n == 0) return;
     const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, in_tile = lane & 15, part = lane >> 4;
     const bool busy = wave * kTile < g.n;
     const bf16_t *up = static_cast<const bf16_t *>(a.up);
-    // the lane's four rows of out, and what is there
-    O *out[4];
-    bool here[4];
-    Raw<O, PER> old[PASSES][4];
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const int row = wave * kTile + part * 4 + v;
-        here[v] = row < g.n;
-        out[v] = static_cast<O *>(a.out) + a.order[g.first + (here[v] ? row : g.n - 1)] * a.out_stride + n0 + in_tile * PER;
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p)
-            if (here[v] && n0 + p * WIDTH + in_tile * PER + PER <= a.n) load(out[v] + p * WIDTH, old[p][v]);
-    }
     f32x4 c[PASSES][PER];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p)
@@ -457,8 +457,18 @@ __global__ __launch_bounds__(kThreads) void adapter_up_tiles_kernel(AdapterArgs 
         for (int t = 0; t < PER; ++t) c[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int64_t steps = (a.rank + 31) / 32;
     const bf16_t *cut = a.cut + ((unit * (kRows / kTile) + wave) * steps * 3 * 64 + lane) * 8;
+    O *out[4];
+    bool here[4];
+    Raw<O, PER> old[PASSES][4];
     for (int64_t first = 0; first < steps; first += STEPS) {
-        Raw8<bf16_t> h[STEPS][3];
+        // (in the order in which they are wanted: a wait for one is a wait for all that were asked for before)
+        Raw8<bf16_t> uv[EACH], h[STEPS][3];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int q = thread + i * kThreads, row = q / VECTORS, vector = q % VECTORS;
+            const int64_t column = n0 + row < a.n ? n0 + row : a.n - 1;
+            read_up<ODD>(a, up, (g.adapter * a.n + column) * a.rank, first * 32 + vector * 8, uv[i]);
+        }
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
             if (busy && first + s < steps) {
@@ -468,29 +478,43 @@ __global__ __launch_bounds__(kThreads) void adapter_up_tiles_kernel(AdapterArgs 
 #pragma unroll
                 for (int i = 0; i < 3; ++i) zero(h[s][i]);
             }
-        if (first > 0) __syncthreads();
+        if (first == 0) {
+            // the lane's four rows of out, and what is there
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int row = wave * kTile + part * 4 + v;
+                here[v] = row < g.n;
+                out[v] = static_cast<O *>(a.out) + a.order[g.first + (here[v] ? row : g.n - 1)] * a.out_stride + n0 + in_tile * PER;
+#pragma unroll
+                for (int p = 0; p < PASSES; ++p)
+                    if (here[v] && n0 + p * WIDTH + in_tile * PER + PER <= a.n) load(out[v] + p * WIDTH, old[p][v]);
+            }
+        } else {
+            __syncthreads();
+        }
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int q = thread + i * kThreads, row = q / VECTORS, vector = q % VECTORS;
-            const int64_t column = n0 + row < a.n ? n0 + row : a.n - 1;
-            Raw8<bf16_t> v;
-            read_up<ODD>(a, up, (g.adapter * a.n + column) * a.rank, first * 32 + vector * 8, v);
-            *reinterpret_cast<u32x4 *>(up_tile + place(row, vector, VECTORS, row / PER)) = u32x4{v.d[0], v.d[1], v.d[2], v.d[3]};
+            const int q = thread + i * kThreads, row = q / VECTORS;
+            *reinterpret_cast<u32x4 *>(up_tile + place(row, q % VECTORS, VECTORS, row / PER)) = u32x4{uv[i].d[0], uv[i].d[1], uv[i].d[2], uv[i].d[3]};
         }
         __syncthreads();
         if (!busy) continue;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p)
+            for (int p = 0; p < PASSES; ++p) {
+                Raw8<bf16_t> f[PER];
 #pragma unroll
                 for (int t = 0; t < PER; ++t) {
                     const int row = p * WIDTH + in_tile * PER + t;
                     const u32x4 v = *reinterpret_cast<const u32x4 *>(up_tile + place(row, s * 4 + part, VECTORS, row / PER));
-                    const Raw8<bf16_t> uv = {{v[0], v[1], v[2], v[3]}};
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) c[p][t] = multiply(h[s][i], uv, c[p][t]);
+                    f[t] = Raw8<bf16_t>{{v[0], v[1], v[2], v[3]}};
                 }
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+#pragma unroll
+                    for (int t = 0; t < PER; ++t) c[p][t] = multiply(h[s][i], f[t], c[p][t]);
+            }
     }
 #pragma unroll
     for (int p = 0; p < PASSES; ++p)
@@ -560,7 +584,7 @@ int down_tiles(const AdapterArgs &a, hipStream_t st) {
 
 template <class O, bool ODD>
 int up_tiles(const AdapterArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.units * ((a.n + kUpColumns - 1) / kUpColumns))), block(kThreads);
+    const dim3 grid((unsigned)(((a.units + 7) / 8 * 8) * ((a.n + kUpColumns - 1) / kUpColumns))), block(kThreads);
     if (a.rank <= 32) hipLaunchKernelGGL((adapter_up_tiles_kernel<O, 1, ODD>), grid, block, 0, st, a);
     else if (a.rank <= 64) hipLaunchKernelGGL((adapter_up_tiles_kernel<O, 2, ODD>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((adapter_up_tiles_kernel<O, 4, ODD>), grid, block, 0, st, a);
