@@ -101,12 +101,18 @@ struct Rows16 {
             n = 0;
             list = shared;
             if (id < 0) return;
-            for (int32_t i = 0; i < a.m; i += 64) {
-                const bool here = i + lane < a.m && adapter_of(a, i + lane) == id;
-                const uint64_t rows = __ballot(here);
-                // (every wave writes the same)
-                if (here) shared[n + __popcll(rows & ((1ull << lane) - 1))] = i + lane;
-                n += __popcll(rows);
+            constexpr int AHEAD = 2;
+            for (int32_t i = 0; i < a.m; i += 64 * AHEAD) {
+                bool here[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) here[u] = i + 64 * u + lane < a.m && adapter_of(a, i + 64 * u + lane) == id;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const uint64_t rows = __ballot(here[u]);
+                    // (every wave writes the same)
+                    if (here[u]) shared[n + __popcll(rows & ((1ull << lane) - 1))] = i + 64 * u + lane;
+                    n += __popcll(rows);
+                }
             }
             __syncthreads();
             if (a.adapters > a.m && n > 0 && shared[0] != unit) n = 0;
@@ -209,9 +215,10 @@ __device__ __forceinline__ void inner(const AdapterArgs &a, int64_t row, int64_t
     float f[8] = {};
     if (r < a.ranks) {
         const float *h = a.h + row * a.ranks + r;
-        for (int64_t s = 0; s < a.splits; ++s, h += a.m * a.ranks) {
+#pragma unroll 4
+        for (int s = 0; s < (int)a.splits; ++s) {
             Raw8<float> raw;
-            load(h, raw);
+            load(h + s * a.m * a.ranks, raw);
             float g[8];
             widen(raw, g);
 #pragma unroll
@@ -261,6 +268,7 @@ template <class O, int STEPS, bool SORTED, bool ODD>
 __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
     typedef Piece<O> P;
     __shared__ int32_t found[SORTED ? 1 : kFew];
+    __shared__ f32x4 inner_sums[STEPS ? kTile * (STEPS * 8 + 1) : 1];
     const int64_t unit = blockIdx.x % a.units, chunk = blockIdx.x / a.units;
     const Rows16<SORTED> rows(a, unit, found);
     if (rows.n == 0) return;
@@ -272,9 +280,30 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
         const int64_t row = rows.row(tile + in_tile);
         const bool here = tile + in_tile < rows.n;
         Raw8<bf16_t> h[STEPS ? STEPS : 1][3];
-        if constexpr (STEPS > 0)
+        if constexpr (STEPS > 0) {
+            // (by all threads for all waves, along the rows: what the waves' lanes hold are 16 rows side by side, 64 cycles a load.  96 rows of 40
+            // adapters, ten parts: the launch takes 10.2 us where each wave reads its own, 8.0 so)
+            const int quads = (int)a.ranks / 4;
+            __syncthreads();
+            for (int q = (int)threadIdx.x; q < kTile * quads; q += kThreads) {
+                const int r = q / quads, at = q % quads;
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                if (tile + r < rows.n) {
+                    const f32x4 *h0 = reinterpret_cast<const f32x4 *>(a.h + rows.row(tile + r) * a.ranks) + at;
+#pragma unroll 4
+                    for (int s = 0; s < (int)a.splits; ++s) sum += h0[s * a.m * quads];
+                }
+                inner_sums[r * (STEPS * 8 + 1) + at] = sum;
+            }
+            __syncthreads();
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) inner(a, row, s * 32 + part * 8, scale, h[s]);
+            for (int s = 0; s < STEPS; ++s) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = s * 32 + part * 8 + e < a.rank ? inner_sums[in_tile * (STEPS * 8 + 1) + s * 8 + part * 2 + e / 4][e & 3] * scale : 0.f;
+                cut(f, h[s]);
+            }
+        }
         O *out = static_cast<O *>(a.out) + row * a.out_stride;
         constexpr int STRIDE = kWaves * P::kColumns;
         for (int64_t n = from + wave * P::kColumns; n < to; n += STRIDE) {
@@ -443,7 +472,8 @@ __global__ __launch_bounds__(kThreads, STEPS == 1 ? 4 : 1) void adapter_up_tiles
     constexpr int VECTORS = STEPS * 4, EACH = kUpColumns * VECTORS / kThreads, PER = 16 / (int)sizeof(O), WIDTH = 16 * PER, PASSES = kUpColumns / WIDTH;
     __shared__ __align__(16) bf16_t up_tile[kUpColumns * STEPS * 32];
     // neighbouring groups, which have the same adapter, on the same of 8 dies (workgroups go to them in turn)
-    const int64_t each = (a.units + 7) / 8, slot = blockIdx.x % (each * 8), unit = slot % 8 * each + slot / 8, n0 = blockIdx.x / (each * 8) * kUpColumns;
+    const int64_t each = (a.units + 7) / 8, chunks = (a.n + kUpColumns - 1) / kUpColumns, at = blockIdx.x / 8;
+    const int64_t unit = blockIdx.x % 8 * each + at / chunks, n0 = at % chunks * kUpColumns;
     if (unit >= a.units) return;
     const AdapterArgs::Group g = a.groups[unit];
     if (g.n == 0) return;
