@@ -6,6 +6,9 @@ added up), clipping by the norm of all gradients, an update of the fp32 master w
 bf16 weights' bits changed in.  Receiver, two shards: apply, the head's shards rounded to 4-bit matrices, and logits for
 prompts and for single tokens, each shard its rows of the embedding and its columns of the logits.
 
+Behind it a small model learns to draft for the receiver: an embedding, a root mean square norm and a head, from the receiver's top
+logits alone; then it drafts tokens that the receiver verifies, some requests through adapters of their own.
+
     python examples/train_and_serve.py [steps]
 """
 import os
@@ -106,6 +109,74 @@ def serve(shards, tokens):
     return torch.cat([s.logits(x) for s in shards], 1)
 
 
+class Draft:
+    """A small model that learns from the top logits of a large one, and drafts for it."""
+
+    def __init__(self, hidden=64, top=8, seed=1):
+        g = torch.Generator("cuda").manual_seed(seed)
+        self.hidden, self.top, self.scale = hidden, top, hidden ** 0.5
+        self.embedding, self.head = (torch.randn(VOCAB, hidden, generator=g, device="cuda") * 0.02 for _ in range(2))
+        self.norm = torch.ones(hidden, device="cuda")
+
+    def gradients(self, tokens, ids, teacher, temperature=1.0):
+        """(loss of each token, gradients of embedding, norm weight and head)"""
+        n = len(tokens)
+        x, y, rstd = torch.empty(n, self.hidden, device="cuda"), torch.empty(n, self.hidden, device="cuda"), torch.empty(n, device="cuda")
+        R.embedding_lookup(self.embedding, tokens, x, scale=self.scale)
+        R.layer_norm(x, self.norm, y, rstd=rstd, center=False)
+        logits = y @ self.head.t()
+        loss, lse, d_loss = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.full((n,), 1.0 / n, device="cuda")
+        R.distill_loss_grad(logits, ids, teacher, d_loss, loss, lse, logits, R.distill_workspace(n, VOCAB), temperature=temperature)
+        d_y, d_head = logits @ self.head, logits.t() @ y                        # (the gradient has taken the logits' place)
+        d_norm, d_embedding = torch.empty_like(self.norm), torch.empty_like(self.embedding)
+        R.layer_norm_grad(d_y, x, self.norm, rstd, d_y, d_norm, R.layer_norm_grad_workspace(n, self.hidden))
+        R.embedding_grad(d_y, tokens, d_embedding, R.embedding_grad_workspace(VOCAB, self.hidden, n), scale=self.scale)
+        return loss, (d_embedding, d_norm, d_head)
+
+    def learn(self, shards, tokens, rate=20.0):
+        teacher, ids = serve(shards, tokens).topk(self.top, 1)
+        loss, gradients = self.gradients(tokens, ids, teacher)
+        for w, d in zip((self.embedding, self.norm, self.head), gradients):
+            w.sub_(d, alpha=rate)
+        return loss.mean().item()
+
+    def probabilities(self, tokens):
+        x = torch.empty(len(tokens), self.hidden, device="cuda")
+        R.embedding_lookup(self.embedding, tokens, x, scale=self.scale)
+        R.layer_norm(x, self.norm, x, center=False)
+        return torch.softmax(x @ self.head.t(), 1)
+
+
+def answer(shards, draft, tokens, g, length=3, adapters=None, chosen=None):
+    """What the receiver makes of `length` tokens that are drafted behind each of these: (tokens, how many of them were drafted)"""
+    n = len(tokens)
+    last, drafted, q = tokens, [], []
+    for _ in range(length):
+        q.append(draft.probabilities(last))
+        last = torch.multinomial(q[-1], 1, generator=g).view(-1)
+        drafted.append(last)
+    rows = torch.stack([tokens] + drafted, 1).view(-1)                          # each request's tokens, all of which are answered at once
+    logits = serve(shards, rows)
+    if adapters is not None:
+        x = sum(s.rows_of(rows) for s in shards) * shards[0].weights[1]
+        R.adapter_linear(x, adapters, chosen.repeat_interleave(length + 1), logits, R.adapter_linear_workspace(len(rows), adapters))
+    out, accepted = torch.empty(n * (length + 1), dtype=torch.int64, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+    R.draft_verify(torch.softmax(logits, 1), torch.stack(q, 1).view(n * length, VOCAB), torch.stack(drafted, 1).view(-1),
+                   torch.arange(n + 1, device="cuda") * length, torch.rand(len(rows), generator=g, device="cuda"), out, accepted,
+                   R.draft_verify_workspace(n, VOCAB))
+    return out.view(n, length + 1), accepted
+
+
+def draft_and_verify(shards, steps=60, seed=0):
+    g, draft = torch.Generator("cuda").manual_seed(seed + 1), Draft(seed=seed + 1)
+    everyone = torch.arange(VOCAB, device="cuda")
+    losses = [draft.learn(shards, everyone) for _ in range(steps)]
+    down, up = (torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16) * 0.02 for s in ((4, 8, HIDDEN), (4, VOCAB, 8)))
+    tokens, accepted = answer(shards, draft, everyone[:256], g, adapters=R.Adapters(down, up), chosen=(everyone[:256] % 6).int())
+    print("drafting: loss %.3f to %.3f, %.2f of 3 drafted tokens stay" % (losses[0], losses[-1], accepted.float().mean().item()), flush=True)
+    return losses, tokens, accepted, draft
+
+
 def batch(g, following):
     tokens = torch.randint(0, VOCAB, (TOKENS,), generator=g, device="cuda")
     return tokens, following[tokens]
@@ -135,4 +206,4 @@ def main(steps=40, seed=0):
 
 
 if __name__ == "__main__":
-    main(*(int(v) for v in sys.argv[1:2]))
+    draft_and_verify(main(*(int(v) for v in sys.argv[1:2]))[-1])

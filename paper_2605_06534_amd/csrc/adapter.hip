@@ -371,7 +371,7 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
 // ---- many rows of each adapter: tiles of 64 rows whose operands go through LDS.  What a lane of a matrix instruction needs lies in 16 rows
 // of memory next to each other's lanes, and such a load takes 64 cycles for its 16 lines a quarter; so rows are read along their length into
 // LDS, and results are laid out so that lanes next to each other have columns next to each other (8192 rows of 300 each, rank 64: the first
-// product 74 us without LDS, DOWN_US so; the second 164 and UP_US). ----
+// product 74 us without LDS, 33 so; the second 164 and 101). ----
 constexpr int kRows = 64;                           // of a group
 constexpr int kDepth = 64;                          // elements of k at a time: 8 vectors
 constexpr int kUpColumns = 128;                     // of out, a workgroup

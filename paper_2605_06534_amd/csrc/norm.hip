@@ -388,22 +388,26 @@ constexpr int kJoinColumns = 32, kJoinLanes = 32;
 __global__ __launch_bounds__(kJoinColumns * kJoinLanes) void norm_join_kernel(NormGradArgs a, const float *partials, int64_t parts) {
     __shared__ float shared[2][kJoinLanes][kJoinColumns];
     const int c = threadIdx.x % kJoinColumns, lane = threadIdx.x / kJoinColumns;
-    const int64_t col = (int64_t)blockIdx.x * kJoinColumns + c;
-    float dw = 0.f, db = 0.f;
-    if (col < a.cols)
+    for (int64_t first = (int64_t)blockIdx.x * kJoinColumns; first < a.cols; first += (int64_t)gridDim.x * kJoinColumns) {
+        const int64_t col = first + c;
+        float dw = 0.f, db = 0.f;
+        if (col < a.cols)
 #pragma unroll 8
-        for (int64_t p = lane; p < parts; p += kJoinLanes) {
-            dw += partials[2 * p * a.cols + col];
-            db += partials[(2 * p + 1) * a.cols + col];
+            for (int64_t p = lane; p < parts; p += kJoinLanes) {
+                dw += partials[2 * p * a.cols + col];
+                db += partials[(2 * p + 1) * a.cols + col];
+            }
+        shared[0][lane][c] = dw;
+        shared[1][lane][c] = db;
+        __syncthreads();
+        if (lane < 2 && col < a.cols) {
+            float s = 0.f;
+            for (int k = 0; k < kJoinLanes; ++k) s += shared[lane][k][c];
+            float *out = lane ? a.dbias : a.dweight;
+            if (out) out[col] = a.accumulate ? out[col] + s : s;
         }
-    shared[0][lane][c] = dw;
-    shared[1][lane][c] = db;
-    __syncthreads();
-    if (lane > 1 || col >= a.cols) return;
-    float s = 0.f;
-    for (int k = 0; k < kJoinLanes; ++k) s += shared[lane][k][c];
-    float *out = lane ? a.dbias : a.dweight;
-    if (out) out[col] = a.accumulate ? out[col] + s : s;
+        __syncthreads();
+    }
 }
 
 constexpr int64_t kMostParts = 256;
@@ -446,7 +450,8 @@ size_t means_bytes(int64_t rows) { return ((size_t)rows * sizeof(RowMeans) + 255
 
 int join(const NormGradArgs &a, const float *partials, int64_t parts, hipStream_t st) {
     if (!a.dweight && !a.dbias) return 0;
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((a.cols + kJoinColumns - 1) / kJoinColumns)), dim3(kJoinColumns * kJoinLanes), 0, st, a, partials, parts);
+    const int64_t groups = (a.cols + kJoinColumns - 1) / kJoinColumns, most = kMostThreads / (kJoinColumns * kJoinLanes);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(groups < most ? groups : most)), dim3(kJoinColumns * kJoinLanes), 0, st, a, partials, parts);
     return (int)hipGetLastError();
 }
 
