@@ -642,7 +642,8 @@ rose_status rose_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_st
  * rose_distill_grad       d_logits, from the lse that the loss left behind
  * rose_distill_loss_grad  all of them in one call, d_loss being known beforehand (1 / number of tokens)
  * Sums over the columns are fp32, each relative to the largest logit of what it sums; the entries' p and the loss are formed in 64 bits, one
- * rounding each.  Columns of minus infinity have q = 0 (an entry there makes the loss infinite); rows whose logits hold a NaN or an
+ * rounding each.  How a sum is divided, and so its last bits, depends on the form that is called, on rows, columns and `top`, and on how the
+ * rows lie to 16 bytes.  Columns of minus infinity have q = 0 (an entry there makes the loss infinite); rows whose logits hold a NaN or an
  * infinity, or minus infinities only, have no number for loss and gradient.
  * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a temperature that is not above zero or
  * infinite, a workspace that is too small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^22 or more rows, 2^31 or more columns, or more than
