@@ -703,7 +703,7 @@ rose_status rose_draft_verify(const void *target, int64_t target_stride, const v
  * on the sizes, the number of adapters among them.  An infinity in up or down makes what it reaches no number or an infinity.
  * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too small;
  * ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^29 or more rows, 2^31 or more columns, more than ROSE_MOST_ADAPTERS adapters, a rank
- * above ROSE_MOST_RANK, or, of more than 64 rows that are 32 or more for
+ * above ROSE_MOST_RANK, or, of more than 128 rows that are 32 or more for
  * each adapter, 2^24 or more pieces of 64 rows and 32 ranks, or of 64 rows and 128 columns.
  */
 #define ROSE_MOST_ADAPTERS 65536

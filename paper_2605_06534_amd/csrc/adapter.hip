@@ -3,7 +3,7 @@
 //
 // What has to move is x, out (both ways) and the adapters that rows name; memory bounds both.  So that an adapter goes by once for all of its
 // rows, rows of one adapter are taken together, up to 16 (one tile of the matrix instructions) or 64 of them.  Few rows: a workgroup
-// looks through all rows' choices for its adapter's by itself.  Many: a launch in front sorts the rows by adapter.
+// looks through all rows' choices for its own.  More: a launch in front sorts the rows by adapter.
 //
 // h keeps 24 bits on its way through matrix instructions that take bf16: it is cut into three numbers of 8 bits, whose sum it is exactly.
 #include "ops_device.h"
@@ -16,7 +16,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kTile = 16;                           // rows of a tile, and ranks, and columns
-constexpr int kFew = 512;                           // rows that a workgroup looks through by itself, at most
+constexpr int kFew = 128;                           // rows that a workgroup looks through by itself, at most: two a lane
 constexpr int kMostSplit = 16;                      // parts of the sums over k
 constexpr int64_t kSplitRows = 32768;               // rows of partial sums, where there are parts
 constexpr int kSortThreads = 1024;
@@ -32,6 +32,23 @@ __device__ __forceinline__ int64_t adapter_of(const AdapterArgs &a, int64_t row)
 __device__ __forceinline__ f32x4 multiply(const Raw8<bf16_t> &p, const Raw8<bf16_t> &q, f32x4 c) {
     const u32x4 pv = {p.d[0], p.d[1], p.d[2], p.d[3]}, qv = {q.d[0], q.d[1], q.d[2], q.d[3]};
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pv), __builtin_bit_cast(bf16x8, qv), c, 0, 0, 0);
+}
+
+// The last n < 8 elements of a row that ends at `end`, zeros behind: the vector that ends there, moved down, where the row has one.  (Element by
+// element 34 rows of 3261, rank 74, take 25 us, 20 so.)
+__device__ __forceinline__ void load_end(const bf16_t *end, int n, bool long_enough, Raw8<bf16_t> &r) {
+    if (n <= 0) {
+        zero(r);
+    } else if (long_enough) {
+        load(end - 8, r);
+        uint64_t lo = (uint64_t)r.d[1] << 32 | r.d[0], hi = (uint64_t)r.d[3] << 32 | r.d[2];
+        const int by = 16 * (8 - n);                            // 16 .. 112
+        if (by >= 64) lo = hi >> (by - 64), hi = 0;
+        else lo = lo >> by | hi << (64 - by), hi >>= by;
+        r.d[0] = (uint32_t)lo, r.d[1] = (uint32_t)(lo >> 32), r.d[2] = (uint32_t)hi, r.d[3] = (uint32_t)(hi >> 32);
+    } else {
+        load(end - n, n, r);
+    }
 }
 
 // ---- rows sorted by adapter: a workgroup an adapter ----
@@ -82,12 +99,13 @@ __global__ __launch_bounds__(kSortThreads) void adapter_sort_kernel(AdapterArgs 
     }
 }
 
-// The rows of one adapter that a workgroup has: of a group, or found among the choices of all rows (unit u: adapter u, or where there are more
-// adapters than rows that of row u, if no row in front has the same).
+// Up to 16 rows of one adapter that a workgroup has: a group's; or, unsorted, the unit-th of all such groups.  Those begin at rows that
+// have a multiple of 16 rows of the same adapter in front of them, which each wave counts by itself, two rows a lane, bit by bit.  (However the rows are
+// distributed: with a workgroup an adapter, 67 rows that all have one of 16 take 23 us, 12 so.)
 template <bool SORTED>
 struct Rows16 {
-    int64_t id;
-    int32_t n;
+    int64_t id = -1;
+    int32_t n = 0;
     const int32_t *list;
     __device__ __forceinline__ Rows16(const AdapterArgs &a, int64_t unit, int32_t *shared) {
         if constexpr (SORTED) {
@@ -96,26 +114,35 @@ struct Rows16 {
             n = g.n;
             list = a.order + g.first;
         } else {
-            const int lane = threadIdx.x & 63;
-            id = a.adapters <= a.m ? unit : adapter_of(a, unit);
-            n = 0;
             list = shared;
-            if (id < 0) return;
-            constexpr int AHEAD = 2;
-            for (int32_t i = 0; i < a.m; i += 64 * AHEAD) {
-                bool here[AHEAD];
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) here[u] = i + 64 * u + lane < a.m && adapter_of(a, i + 64 * u + lane) == id;
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const uint64_t rows = __ballot(here[u]);
-                    // (every wave writes the same)
-                    if (here[u]) shared[n + __popcll(rows & ((1ull << lane) - 1))] = i + 64 * u + lane;
-                    n += __popcll(rows);
-                }
+            const int lane = threadIdx.x & 63, m = (int)a.m;
+            const int32_t c0 = lane < m ? (int32_t)adapter_of(a, lane) : -1, c1 = lane + 64 < m ? (int32_t)adapter_of(a, lane + 64) : -1;
+            // rows with the same number: those that agree in each of its bits
+            uint64_t same00 = __ballot(c0 >= 0), same11 = __ballot(c1 >= 0), same10 = same00;
+            for (int bit = 0; (a.adapters - 1) >> bit; ++bit) {
+                const bool b0 = (c0 >> bit) & 1, b1 = (c1 >> bit) & 1;
+                const uint64_t set0 = __ballot(b0), set1 = __ballot(b1);
+                same00 &= b0 ? set0 : ~set0;
+                same10 &= b1 ? set0 : ~set0;
+                same11 &= b1 ? set1 : ~set1;
             }
+            const uint64_t below = (1ull << lane) - 1;
+            const int in_front0 = __popcll(same00 & below), in_front1 = __popcll(same10) + __popcll(same11 & below);
+            const uint64_t first0 = __ballot(c0 >= 0 && in_front0 % kTile == 0), first1 = __ballot(c1 >= 0 && in_front1 % kTile == 0);
+            const int many0 = __popcll(first0), many1 = __popcll(first1), u = (int)unit;
+            if (u >= many0 + many1) return;
+            // the row that it begins at: the one with so many beginnings in front
+            const bool high = u >= many0;
+            const uint64_t first = high ? first1 : first0, mine = __ballot(((first >> lane) & 1) && __popcll(first & ((1ull << lane) - 1)) == u - (high ? many0 : 0));
+            const int at = __builtin_amdgcn_readfirstlane(__builtin_ctzll(mine));
+            const int32_t of = __builtin_amdgcn_readlane(high ? c1 : c0, at), from = __builtin_amdgcn_readlane(high ? in_front1 : in_front0, at);
+            const bool here0 = c0 == of && in_front0 >= from && in_front0 < from + kTile, here1 = c1 == of && in_front1 >= from && in_front1 < from + kTile;
+            // (every wave writes the same)
+            if (here0) shared[in_front0 - from] = lane;
+            if (here1) shared[in_front1 - from] = lane + 64;
+            id = of;
+            n = __popcll(__ballot(here0)) + __popcll(__ballot(here1));
             __syncthreads();
-            if (a.adapters > a.m && n > 0 && shared[0] != unit) n = 0;
         }
     }
     __device__ __forceinline__ int64_t row(int64_t i) const { return list[i < n ? i : n - 1]; }
@@ -124,11 +151,12 @@ struct Rows16 {
 // ---- h = down x: a workgroup has RANKS tiles of ranks and a part of k that its waves share ----
 template <int RANKS, bool SORTED>
 __global__ __launch_bounds__(kThreads) void adapter_down_kernel(AdapterArgs a) {
-    __shared__ int32_t found[SORTED ? 1 : kFew];
+    __shared__ int32_t found[kTile];
     __shared__ f32x4 sums[(kWaves - 1) * RANKS * 64];
     const int64_t unit = blockIdx.x % a.units, rest = blockIdx.x / a.units;
     const int64_t split = rest % a.splits, rank0 = rest / a.splits * (RANKS * kTile);
     const Rows16<SORTED> rows(a, unit, found);
+    if (rows.n == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in_tile = lane & 15, part = lane >> 4;
     const int64_t from = split * a.share, to = from + a.share < a.k ? from + a.share : a.k;
     const bf16_t *down[RANKS];
@@ -138,53 +166,55 @@ __global__ __launch_bounds__(kThreads) void adapter_down_kernel(AdapterArgs a) {
         const int64_t r = rank0 + t * kTile + in_tile;
         down[t] = static_cast<const bf16_t *>(a.down) + (rows.id * a.rank + (r < a.rank ? r : a.rank - 1)) * a.k + part * 8;
     }
-    for (int32_t tile = 0; tile < rows.n; tile += kTile) {
-        const int64_t row = rows.row(tile + in_tile);
-        const bf16_t *x = static_cast<const bf16_t *>(a.x) + row * a.x_stride + part * 8;
-        f32x4 c[RANKS];
+    const int64_t row = rows.row(in_tile);
+    const bf16_t *x = static_cast<const bf16_t *>(a.x) + row * a.x_stride + part * 8;
+    f32x4 c[RANKS];
 #pragma unroll
-        for (int t = 0; t < RANKS; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        constexpr int STEP = 64;
-        for (int64_t k = from + wave * STEP; k < to; k += kWaves * STEP) {
-            Raw8<bf16_t> xv[2], dv[2][RANKS];
-            if (k + STEP <= a.k) {
+    for (int t = 0; t < RANKS; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int STEP = 64;
+    for (int64_t k = from + wave * STEP; k < to; k += kWaves * STEP) {
+        Raw8<bf16_t> xv[2], dv[2][RANKS];
+        if (k + STEP <= a.k) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h) {
+                load(x + k + 32 * h, xv[h]);
+#pragma unroll
+                for (int t = 0; t < RANKS; ++t) load(down[t] + k + 32 * h, dv[h][t]);
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t left = a.k - k - 32 * h - part * 8;
+                if (left >= 8) {
                     load(x + k + 32 * h, xv[h]);
 #pragma unroll
                     for (int t = 0; t < RANKS; ++t) load(down[t] + k + 32 * h, dv[h][t]);
-                }
-            } else {
+                } else {
+                    load_end(x + a.k - part * 8, (int)left, a.k >= 8, xv[h]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t left = a.k - k - 32 * h - part * 8;
-                    const int n = left < 0 ? 0 : left < 8 ? (int)left : 8;
-                    load(x + k + 32 * h, n, xv[h]);
-#pragma unroll
-                    for (int t = 0; t < RANKS; ++t) load(down[t] + k + 32 * h, n, dv[h][t]);
+                    for (int t = 0; t < RANKS; ++t) load_end(down[t] + a.k - part * 8, (int)left, a.k >= 8, dv[h][t]);
                 }
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int t = 0; t < RANKS; ++t) c[t] = multiply(dv[h][t], xv[h], c[t]);
         }
-        __syncthreads();
-        if (wave > 0)
 #pragma unroll
-            for (int t = 0; t < RANKS; ++t) sums[((wave - 1) * RANKS + t) * 64 + lane] = c[t];
-        __syncthreads();
-        if (wave > 0) continue;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int w = 0; w < kWaves - 1; ++w)
+            for (int t = 0; t < RANKS; ++t) c[t] = multiply(dv[h][t], xv[h], c[t]);
+    }
+    if (wave > 0)
 #pragma unroll
-            for (int t = 0; t < RANKS; ++t) c[t] += sums[(w * RANKS + t) * 64 + lane];
-        if (tile + in_tile < rows.n) {
-            float *h = a.h + (split * a.m + row) * a.ranks + rank0 + part * 4;
+        for (int t = 0; t < RANKS; ++t) sums[((wave - 1) * RANKS + t) * 64 + lane] = c[t];
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-            for (int t = 0; t < RANKS; ++t)
-                if (rank0 + t * kTile < a.ranks) *reinterpret_cast<f32x4 *>(h + t * kTile) = c[t];
-        }
+    for (int w = 0; w < kWaves - 1; ++w)
+#pragma unroll
+        for (int t = 0; t < RANKS; ++t) c[t] += sums[(w * RANKS + t) * 64 + lane];
+    if (in_tile < rows.n) {
+        float *h = a.h + (split * a.m + row) * a.ranks + rank0 + part * 4;
+#pragma unroll
+        for (int t = 0; t < RANKS; ++t)
+            if (rank0 + t * kTile < a.ranks) *reinterpret_cast<f32x4 *>(h + t * kTile) = c[t];
     }
 }
 
@@ -267,7 +297,7 @@ struct Piece<bf16_t> {
 template <class O, int STEPS, bool SORTED, bool ODD>
 __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
     typedef Piece<O> P;
-    __shared__ int32_t found[SORTED ? 1 : kFew];
+    __shared__ int32_t found[kTile];
     __shared__ f32x4 inner_sums[STEPS ? kTile * (STEPS * 8 + 1) : 1];
     const int64_t unit = blockIdx.x % a.units, chunk = blockIdx.x / a.units;
     const Rows16<SORTED> rows(a, unit, found);
@@ -276,94 +306,91 @@ __global__ __launch_bounds__(kThreads) void adapter_up_kernel(AdapterArgs a) {
     const float scale = a.scales ? a.scales[rows.id] : 1.f;
     const bf16_t *up = static_cast<const bf16_t *>(a.up);
     const int64_t from = chunk * a.columns, to = from + a.columns < a.n ? from + a.columns : a.n;
-    for (int32_t tile = 0; tile < rows.n; tile += kTile) {
-        const int64_t row = rows.row(tile + in_tile);
-        const bool here = tile + in_tile < rows.n;
-        Raw8<bf16_t> h[STEPS ? STEPS : 1][3];
-        if constexpr (STEPS > 0) {
-            // (by all threads for all waves, along the rows: what the waves' lanes hold are 16 rows side by side, 64 cycles a load.  96 rows of 40
-            // adapters, ten parts: the launch takes 10.2 us where each wave reads its own, 8.0 so)
-            const int quads = (int)a.ranks / 4;
-            __syncthreads();
-            for (int q = (int)threadIdx.x; q < kTile * quads; q += kThreads) {
-                const int r = q / quads, at = q % quads;
-                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-                if (tile + r < rows.n) {
-                    const f32x4 *h0 = reinterpret_cast<const f32x4 *>(a.h + rows.row(tile + r) * a.ranks) + at;
+    const int64_t row = rows.row(in_tile);
+    const bool here = in_tile < rows.n;
+    Raw8<bf16_t> h[STEPS ? STEPS : 1][3];
+    if constexpr (STEPS > 0) {
+        // (by all threads for all waves, along the rows: what the waves' lanes hold are 16 rows side by side, 64 cycles a load.  96 rows of 40
+        // adapters, ten parts: the launch takes 10.2 us where each wave reads its own, 8.0 so)
+        const int quads = (int)a.ranks / 4;
+        for (int q = (int)threadIdx.x; q < kTile * quads; q += kThreads) {
+            const int r = q / quads, at = q % quads;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            if (r < rows.n) {
+                const f32x4 *h0 = reinterpret_cast<const f32x4 *>(a.h + rows.row(r) * a.ranks) + at;
 #pragma unroll 4
-                    for (int s = 0; s < (int)a.splits; ++s) sum += h0[s * a.m * quads];
-                }
-                inner_sums[r * (STEPS * 8 + 1) + at] = sum;
+                for (int s = 0; s < (int)a.splits; ++s) sum += h0[s * a.m * quads];
             }
-            __syncthreads();
+            inner_sums[r * (STEPS * 8 + 1) + at] = sum;
+        }
+        __syncthreads();
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                float f[8];
+        for (int s = 0; s < STEPS; ++s) {
+            float f[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = s * 32 + part * 8 + e < a.rank ? inner_sums[in_tile * (STEPS * 8 + 1) + s * 8 + part * 2 + e / 4][e & 3] * scale : 0.f;
-                cut(f, h[s]);
+            for (int e = 0; e < 8; ++e) f[e] = s * 32 + part * 8 + e < a.rank ? inner_sums[in_tile * (STEPS * 8 + 1) + s * 8 + part * 2 + e / 4][e & 3] * scale : 0.f;
+            cut(f, h[s]);
+        }
+    }
+    O *out = static_cast<O *>(a.out) + row * a.out_stride;
+    constexpr int STRIDE = kWaves * P::kColumns;
+    for (int64_t n = from + wave * P::kColumns; n < to; n += STRIDE) {
+        const bool whole = n + P::kColumns <= a.n;
+        Raw<O, P::kPer> old[P::kVectors];
+        if (whole && here)
+#pragma unroll
+            for (int v = 0; v < P::kVectors; ++v) load(out + n + v * 4 * P::kPer + part * P::kPer, old[v]);
+        f32x4 c[P::kTiles];
+#pragma unroll
+        for (int t = 0; t < P::kTiles; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        int64_t at[P::kTiles];
+#pragma unroll
+        for (int t = 0; t < P::kTiles; ++t) {
+            const int64_t column = n + P::column(t, in_tile);
+            at[t] = (rows.id * a.n + (column < a.n ? column : a.n - 1)) * a.rank;
+        }
+        if constexpr (STEPS > 0) {
+            Raw8<bf16_t> uv[STEPS][P::kTiles];
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int t = 0; t < P::kTiles; ++t) read_up<ODD>(a, up, at[t], s * 32 + part * 8, uv[s][t]);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+#pragma unroll
+                    for (int t = 0; t < P::kTiles; ++t) c[t] = multiply(uv[s][t], h[s][i], c[t]);
+        } else {
+            for (int64_t r = 0; r < a.rank; r += 32) {
+                inner(a, row, r + part * 8, scale, h[0]);
+#pragma unroll
+                for (int t = 0; t < P::kTiles; ++t) {
+                    Raw8<bf16_t> uv;
+                    read_up<ODD>(a, up, at[t], r + part * 8, uv);
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) c[t] = multiply(uv, h[0][i], c[t]);
+                }
             }
         }
-        O *out = static_cast<O *>(a.out) + row * a.out_stride;
-        constexpr int STRIDE = kWaves * P::kColumns;
-        for (int64_t n = from + wave * P::kColumns; n < to; n += STRIDE) {
-            const bool whole = n + P::kColumns <= a.n;
-            Raw<O, P::kPer> old[P::kVectors];
-            if (whole && here)
+        if (!here) continue;
+        if (whole) {
 #pragma unroll
-                for (int v = 0; v < P::kVectors; ++v) load(out + n + v * 4 * P::kPer + part * P::kPer, old[v]);
-            f32x4 c[P::kTiles];
+            for (int v = 0; v < P::kVectors; ++v) {
+                float f[P::kPer];
+                widen(old[v], f);
 #pragma unroll
-            for (int t = 0; t < P::kTiles; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-            int64_t at[P::kTiles];
-#pragma unroll
-            for (int t = 0; t < P::kTiles; ++t) {
-                const int64_t column = n + P::column(t, in_tile);
-                at[t] = (rows.id * a.n + (column < a.n ? column : a.n - 1)) * a.rank;
+                for (int e = 0; e < P::kPer; ++e) f[e] += c[v * P::kPer / 4 + e / 4][e & 3];
+                store(out + n + v * 4 * P::kPer + part * P::kPer, f);
             }
-            if constexpr (STEPS > 0) {
-                Raw8<bf16_t> uv[STEPS][P::kTiles];
+        } else {
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
+            for (int t = 0; t < P::kTiles; ++t)
 #pragma unroll
-                    for (int t = 0; t < P::kTiles; ++t) read_up<ODD>(a, up, at[t], s * 32 + part * 8, uv[s][t]);
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-                    for (int i = 0; i < 3; ++i)
-#pragma unroll
-                        for (int t = 0; t < P::kTiles; ++t) c[t] = multiply(uv[s][t], h[s][i], c[t]);
-            } else {
-                for (int64_t r = 0; r < a.rank; r += 32) {
-                    inner(a, row, r + part * 8, scale, h[0]);
-#pragma unroll
-                    for (int t = 0; t < P::kTiles; ++t) {
-                        Raw8<bf16_t> uv;
-                        read_up<ODD>(a, up, at[t], r + part * 8, uv);
-#pragma unroll
-                        for (int i = 0; i < 3; ++i) c[t] = multiply(uv, h[0][i], c[t]);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t column = n + P::column(t, part * 4 + e);
+                    if (column < a.n) out[column] = from_f32<O>(to_f32(out[column]) + c[t][e]);
                 }
-            }
-            if (!here) continue;
-            if (whole) {
-#pragma unroll
-                for (int v = 0; v < P::kVectors; ++v) {
-                    float f[P::kPer];
-                    widen(old[v], f);
-#pragma unroll
-                    for (int e = 0; e < P::kPer; ++e) f[e] += c[v * P::kPer / 4 + e / 4][e & 3];
-                    store(out + n + v * 4 * P::kPer + part * P::kPer, f);
-                }
-            } else {
-#pragma unroll
-                for (int t = 0; t < P::kTiles; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int64_t column = n + P::column(t, part * 4 + e);
-                        if (column < a.n) out[column] = from_f32<O>(to_f32(out[column]) + c[t][e]);
-                    }
-            }
         }
     }
 }
@@ -402,16 +429,23 @@ __global__ __launch_bounds__(kThreads) void adapter_down_tiles_kernel(AdapterArg
     }
     Raw8<bf16_t> xv[XS], dv[D_EACH];
     auto ask = [&](int64_t k) {
+        if (k + kDepth <= a.k) {
+#pragma unroll
+            for (int i = 0; i < XS; ++i) load(x[i] + k, xv[i]);
+#pragma unroll
+            for (int i = 0; i < D_EACH; ++i) load(down[i] + k, dv[i]);
+            return;
+        }
         const int64_t left = a.k - k - thread % VECTORS * 8;
         const int n = left < 0 ? 0 : left < 8 ? (int)left : 8;
 #pragma unroll
         for (int i = 0; i < XS; ++i)
             if (n == 8) load(x[i] + k, xv[i]);
-            else load(x[i] + k, n, xv[i]);
+            else load_end(x[i] + a.k - thread % VECTORS * 8, n, a.k >= 8, xv[i]);
 #pragma unroll
         for (int i = 0; i < D_EACH; ++i)
             if (n == 8) load(down[i] + k, dv[i]);
-            else load(down[i] + k, n, dv[i]);
+            else load_end(down[i] + a.k - thread % VECTORS * 8, n, a.k >= 8, dv[i]);
     };
     auto put = [&](bf16_t *tile, int q, const Raw8<bf16_t> &v) {
         const int row = q / VECTORS;
@@ -657,9 +691,9 @@ int launch_adapter_linear(const AdapterArgs &args, bool out_f32, void *stream) {
     hipStream_t st = static_cast<hipStream_t>(stream);
     a.ranks = padded(a.rank);
     a.h = reinterpret_cast<float *>(a.workspace);
-    // Few rows, and few of each adapter: no launch that sorts.
-    if (a.m <= 64 || (a.m <= kFew && a.m <= 8 * a.adapters)) {
-        a.units = a.adapters <= a.m ? a.adapters : a.m;
+    // Few rows: no launch that sorts.  (As many groups as there can be: one of each adapter that a row has, and one for each 16 rows.)
+    if (a.m <= kFew) {
+        a.units = (a.adapters <= a.m ? a.adapters : a.m) + a.m / kTile;
         return both<false>(a, out_f32, st);
     }
     char *at = a.workspace + whole((size_t)split_rows(a.m) * a.ranks * 4);

@@ -313,7 +313,7 @@ namespace {
 rose_status check_adapters(int64_t m, int64_t n, int64_t k, int64_t adapters, int64_t rank) {
     if (m < 0 || n < 0 || k < 0 || adapters < 0 || rank < 0) return ROSE_ERR_ARG;
     // (rows that go in groups of 64: those times pieces of ranks, or of columns, are workgroups)
-    if (m > 64 && m >= 32 * adapters && m < (1 << 29) && n < kMost && rank <= ROSE_MOST_RANK) {
+    if (m > 128 && m >= 32 * adapters && m < (1 << 29) && n < kMost && rank <= ROSE_MOST_RANK) {
         const int64_t groups = m / 64 + adapters + 8;
         if (groups * ((rank + 31) / 32) >= (1 << 24) || groups * ((n + 127) / 128) >= (1 << 24)) return ROSE_ERR_UNSUPPORTED;
     }

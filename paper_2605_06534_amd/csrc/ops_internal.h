@@ -153,7 +153,7 @@ struct AdapterArgs {
     float *h;
     int64_t ranks, splits, share;       // ranks in whole tiles; parts of k, and elements of one
     int64_t columns;                    // of a workgroup
-    int64_t units, group;               // groups, or adapters to look for; rows of a group, at most
+    int64_t units, group;               // groups of rows, at most; rows of one, at most
     bf16_t *cut;                        // scale * h in three numbers of 8 bits
     int32_t *order;
     struct Group {
