@@ -642,7 +642,7 @@ rose_status rose_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_st
  * rose_distill_grad       d_logits, from the lse that the loss left behind
  * rose_distill_loss_grad  all of them in one call, d_loss being known beforehand (1 / number of tokens)
  * Sums over the columns are fp32, each relative to the largest logit of what it sums; the entries' p and the loss are formed in 64 bits, one
- * rounding each.  How a sum is divided, and so its last bits, depends on the form that is called, on rows, columns and `top`, and on how the
+ * rounding each (p to 24 bits where the gradient alone is wanted).  How a sum is divided, and so its last bits, depends on the form that is called, on rows, columns and `top`, and on how the
  * rows lie to 16 bytes.  Columns of minus infinity have q = 0 (an entry there makes the loss infinite); rows whose logits hold a NaN or an
  * infinity, or minus infinities only, have no number for loss and gradient.
  * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a temperature that is not above zero or

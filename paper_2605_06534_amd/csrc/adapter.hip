@@ -20,7 +20,10 @@ constexpr int kFew = 128;                           // rows that a workgroup loo
 constexpr int kMostSplit = 16;                      // parts of the sums over k
 constexpr int64_t kSplitRows = 32768;               // rows of partial sums, where there are parts
 constexpr int kSortThreads = 1024;
-constexpr int64_t kLarge = 32;                      // rows of each adapter on average from which on 64 go together
+// Rows of each adapter on average, and rows times ranks (of up to 64), from which on 64 rows go together and not 16 (4096 columns both ways, 64
+// against 16 together: 4096 rows of 64 adapters, rank 16, 35.5 us and 43.3, of 256 adapters 55.9 and 48.1; 1024 rows of 16, rank 64, 29.5 and 32.0,
+// rank 16 20.1 and 18.3).
+constexpr int64_t kLarge = 32, kLargeWork = 65536;
 
 __device__ __forceinline__ int64_t adapter_of(const AdapterArgs &a, int64_t row) {
     const int64_t id = a.wide ? static_cast<const int64_t *>(a.chosen)[row] : static_cast<const int32_t *>(a.chosen)[row];
@@ -279,7 +282,7 @@ __device__ __forceinline__ void read_up(const AdapterArgs &a, const bf16_t *up, 
     }
 }
 
-// Columns of a wave at a time: 64 for bf16, 32 for fp32, whole lines of out; STEPS: 32 ranks each, 0: any number, cut again for each columns.
+// Columns of a wave at a time: 64 for bf16, 32 for fp32, whole lines of out; STEPS: 32 ranks each; 0: any number, cut anew for each of these.
 // Which row of a tile is which column is chosen so that a lane's results are 16 neighbouring bytes of out.
 template <class O>
 struct Piece;
@@ -700,7 +703,7 @@ int launch_adapter_linear(const AdapterArgs &args, bool out_f32, void *stream) {
     a.order = reinterpret_cast<int32_t *>(at);
     a.groups = reinterpret_cast<AdapterArgs::Group *>(at + whole((size_t)a.m * 4));
     a.cut = reinterpret_cast<bf16_t *>(at + whole((size_t)a.m * 4) + whole((size_t)(a.m / kTile + a.adapters) * sizeof(AdapterArgs::Group)));
-    const bool large = a.m >= kLarge * a.adapters;
+    const bool large = a.m >= kLarge * a.adapters && a.m * (a.rank < 64 ? a.rank : 64) >= kLargeWork;
     a.group = large ? kRows : kTile;
     a.units = a.m / a.group + a.adapters;
     hipLaunchKernelGGL(adapter_sort_kernel, dim3((unsigned)a.adapters), dim3(kSortThreads), 0, st, a);

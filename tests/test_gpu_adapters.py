@@ -169,3 +169,28 @@ def test_nothing_to_do():
         out = torch.full((m, n), 3.0, device="cuda")
         R.adapter_linear(torch.zeros(m, k, dtype=torch.bfloat16, device="cuda"), w, torch.zeros(m, dtype=torch.int32, device="cuda"), out, R.adapter_linear_workspace(m, w))
         assert (out == 3).all()
+
+
+@pytest.mark.parametrize("out", DTYPES)
+@pytest.mark.parametrize("rank,m", [(1, 66000), (3, 22000), (8, 8300), (15, 4400), (17, 3900), (33, 2000), (50, 1400), (64, 1100), (65, 1100), (100, 1100), (129, 1100),
+                                    (200, 1100), (1024, 1100)])
+def test_many_rows_by_rank(rank, m, out):
+    """Enough rows and ranks for groups of 64."""
+    check(m, 130, 257, rank, 2, out, pad=3, seed=21)
+    check(m, 96, 128, rank, 5, out, run=50, pad=8, seed=22, index=torch.int64, scales=False)
+
+
+@pytest.mark.parametrize("out", DTYPES)
+@pytest.mark.parametrize("n,k", [(1, 1), (1, 64), (64, 1), (7, 9), (15, 31), (17, 33), (63, 65), (100, 1000), (129, 2050), (1000, 100), (4099, 4083)])
+def test_many_rows_by_columns(n, k, out):
+    check(1111, n, k, 64, 3, out, 1, pad=3 if n % 2 else 0, seed=23)
+    check(1111, n, k, 60, 4, out, 300, seed=24)
+
+
+@pytest.mark.parametrize("m", [1, 15, 16, 17, 63, 64, 65, 100, 127, 128, 129])
+def test_few_rows_however_they_are_distributed(m):
+    """All of one adapter, each its own, two in turn, one row apart: groups of 16 that begin anywhere."""
+    place = torch.arange(m, device="cuda")
+    for chosen in (place * 0 + 3, place, place % 2, (place > m // 2).long() * 7 - 1, torch.where(place == m // 3, 2, 6), place // 17, place * 0 - 1):
+        check(m, 70, 90, 10, 130, "f32", chosen=chosen, seed=25)
+        check(m, 70, 90, 10, 8, "bf16", chosen=chosen, seed=26)
