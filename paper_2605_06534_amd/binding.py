@@ -578,7 +578,7 @@ def _list(t, n, dtypes, what):
     """The address of n contiguous elements on the GPU, None for None."""
     if t is None:
         return None
-    if not (t.is_cuda and t.is_contiguous()) or t.numel() != n or t.dtype not in dtypes:
+    if t.dtype not in dtypes or t.numel() != n or not (t.is_cuda and t.is_contiguous()):
         raise RoseError(ERR_SHAPE, "%s: %d contiguous elements of %s on the GPU are wanted"
                         % (what, n, " or ".join(str(d)[6:] for d in dtypes)))
     return t.data_ptr()
@@ -593,8 +593,16 @@ def _bytes(name, what, *sizes, device="cuda"):
     return torch.empty(v.value, dtype=torch.uint8, device=device)
 
 
+_gpus = None
+
+
 def _one_device(what, stream, *tensors):
-    """Everything on one GPU, the current one unless a stream says otherwise."""
+    """Everything on one GPU, the current one unless a stream says otherwise.  (That it is no host memory others see to.)"""
+    global _gpus
+    if _gpus is None:
+        _gpus = torch.cuda.device_count()
+    if _gpus == 1:
+        return
     here = tensors[0].get_device() if stream is not None else torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != here:
