@@ -604,8 +604,10 @@ rose_status rose_mx4_linear(const void *x, int32_t x_dtype, int64_t m, int64_t x
  *   center       nonzero: mean is the row's; 0: it is zero (root mean square norm), and a bias is refused
  *   weight, bias cols elements of weight_dtype; bias may be NULL
  *   mean, rstd   device, one fp32 a row, what the gradient needs; either may be NULL
- * Sums are fp32, of deviations from the mean; one rounding to out's type.  out may be x (same address, type and stride).  Rows
- * with an infinity or a NaN follow the formula.
+ * Sums are fp32, of deviations from the mean, which is itself corrected by what they sum to: a row of equal values has that mean and no
+ * deviation.  One rounding to out's type.  out may be x (same address, type and stride).  Rows with an infinity or a NaN follow the
+ * formula.  So do finite rows while their sum, and that of their squared deviations, is below 2^128; beyond, a mean is infinite
+ * and its row no number, or rstd 0.  (Squares below 2^-149 count as zero.)
  * Its gradient for g = dy * weight, xhat = (x - mean) * rstd:
  *   dx      = rstd * (g - mean of g - xhat * mean of (g * xhat));  mean == NULL: not centred, without the mean of g
  *   dweight = sum over the rows of dy * xhat, dbias = sum over the rows of dy  (accumulate != 0: added to what is there)

@@ -39,8 +39,14 @@ __device__ __forceinline__ void write(T *p, const float (&f)[W]) {
     else store(p, f);
 }
 
+// A mean of n numbers and the sum of the deviations from it: the mean that they have.  (Infinities, and what is no number, stay as the sum has them.)
+__device__ __forceinline__ float refined(float mean, float deviations, float n) {
+    return fabsf(mean) < INFINITY && n > 0.f ? mean + deviations / n : mean;
+}
+
 // ---- rows that stay in registers: read once, LANES lanes a row, V vectors a lane; what is behind the last whole vector an element a lane ----
-// HBM bounds them where rows are many: 16384 x 5120 in bf16 59 us, 5.7 TB/s, centred and with a bias 69 (three times through the caches, as below, 180).
+// HBM bounds them where rows are many: 16384 x 5120 in bf16 59 us, 5.7 TB/s, centred and with a bias 73 (69 without correcting the mean;
+// three times through the caches, as below, 180).
 template <class X, class Y, int LANES, int V>
 __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows_kernel(NormArgs a) {
     constexpr int W = kPer<X, Y>, THREADS = LANES < kThreads ? kThreads : LANES;
@@ -58,8 +64,10 @@ __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows
         if (v * LANES + lane < vectors) load(x + (v * LANES + lane) * W, raw[v]);
     }
     const float tail = lane < rest ? to_f32(x[vectors * W + lane]) : 0.f;
-    // Each 16 lanes, or each wave of a longer row, find their own mean and the squares of the deviations from it; waves then join theirs in one
-    // exchange:  sum (x - mean)^2 = sum over the waves of squares + n (mean - the wave's)^2.
+    // Each 16 lanes, or each wave of a longer row, find their own mean, in two steps: that of the sum, and what the deviations from it say that it
+    // is off by.  (A sum of equal numbers gives a mean that is a few units off, and squares of deviations that are not there: 10000.1 5121 times
+    // had a variance of 1e-4, -1e30 an infinite one.)  Then the squares of the deviations; waves join theirs in one exchange:
+    //   sum (x - mean)^2 = sum over the waves of squares + 2 d left + n d^2,   d = the wave's mean - mean,   left = sum (x - the wave's mean).
     auto total = [](float v) { return LANES == 16 ? sum16(v) : wave_sum(v); };
     const int wave = LANES > 64 ? (int)threadIdx.x >> 6 : 0;
     float n = (float)a.cols;
@@ -72,7 +80,7 @@ __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows
         }
         n = (float)mine;
     }
-    float sum = 0.f, mean = 0.f;
+    float mean = 0.f, left = 0.f;
     if (a.center) {
         float s = tail;
 #pragma unroll
@@ -82,8 +90,19 @@ __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows
 #pragma unroll
             for (int e = 0; e < W; ++e) s += f[e];
         }
-        sum = total(s);
-        mean = n > 0.f ? sum / n : 0.f;
+        const float sum = total(s), first = n > 0.f ? sum / n : 0.f;
+        s = lane < rest ? tail - first : 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float f[W], t = 0.f;
+            widen(raw[v], f);
+#pragma unroll
+            for (int e = 0; e < W; ++e) t += f[e] - first;
+            s += v * LANES + lane < vectors ? t : 0.f;
+        }
+        left = total(s);
+        mean = refined(first, left, n);
+        left = fmaf(n, first - mean, left);
     }
     float s = lane < rest ? (tail - mean) * (tail - mean) : 0.f;
 #pragma unroll
@@ -97,20 +116,18 @@ __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows
     float squares = total(s);
     if constexpr (LANES > 64) {
         constexpr int WAVES = LANES / 64;
-        if ((threadIdx.x & 63) == 0) shared[0][wave] = squares, shared[1][wave] = sum, shared[2][wave] = mean, shared[3][wave] = n;
+        if ((threadIdx.x & 63) == 0) shared[0][wave] = squares, shared[1][wave] = left, shared[2][wave] = mean, shared[3][wave] = n;
         __syncthreads();
+        // (each of 16 lanes has a wave's)
+        const int w = threadIdx.x & 15;
+        const float its_squares = w < WAVES ? shared[0][w] : 0.f, its_left = w < WAVES ? shared[1][w] : 0.f;
+        const float its_mean = w < WAVES ? shared[2][w] : 0.f, its_n = w < WAVES ? shared[3][w] : 0.f;
         if (a.center) {
-            sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += shared[1][w];
-            mean = sum / (float)a.cols;
+            const float first = sum16(its_mean * its_n) / (float)a.cols;
+            mean = refined(first, sum16(fmaf(its_mean - first, its_n, its_left)), (float)a.cols);
         }
-        squares = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float d = a.center ? shared[2][w] - mean : 0.f;
-            squares += fmaf(d * shared[3][w], d, shared[0][w]);
-        }
+        const float d = its_mean - mean;
+        squares = sum16(fmaf(d, fmaf(d, its_n, 2.f * its_left), its_squares));
     }
     const float rstd = 1.f / sqrtf(squares / (float)a.cols + a.eps);
     if (!there) return;
@@ -145,15 +162,17 @@ __global__ __launch_bounds__(LANES < kThreads ? kThreads : LANES) void norm_rows
 template <class X, class Y>
 __global__ __launch_bounds__(kThreads) void layer_norm_kernel(NormArgs a) {
     __shared__ float shared[kWaves];
+    __shared__ double sums[kWaves];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const X *x = static_cast<const X *>(a.x) + row * a.x_stride;
         Y *out = static_cast<Y *>(a.out) + row * a.out_stride;
         float mean = 0.f;
         if (a.center) {
-            float s[1] = {0.f};
-            for (int64_t i = threadIdx.x; i < a.cols; i += kThreads) s[0] += to_f32(x[i]);
-            block_sum<kWaves>(s, shared);
-            mean = s[0] / (float)a.cols;
+            // (in 64 bits, so that equal numbers have exactly their mean without another pass)
+            double s[1] = {0.};
+            for (int64_t i = threadIdx.x; i < a.cols; i += kThreads) s[0] += (double)to_f32(x[i]);
+            block_sum<kWaves>(s, sums);
+            mean = (float)(s[0] / (double)a.cols);
         }
         float s[1] = {0.f};
         for (int64_t i = threadIdx.x; i < a.cols; i += kThreads) {

@@ -130,8 +130,10 @@ __device__ __forceinline__ float moved(float v) {
 __device__ __forceinline__ float of_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 
 // Sums over 16 neighbouring lanes, and over the lanes of a wave, the same in each: pairs, fours, and mirrored halves of 8 and of 16, all in the
-// additions themselves (through LDS, as shuffles go, and with two exchanges between the waves a centred norm of 16384 x 5120 took 79 us, now 69).
+// additions themselves (through LDS, as shuffles go, and with two exchanges between the waves a centred norm of 16384 x 5120 took 79 us, 69 so).
+// (A product that is summed stays one by itself: taken into the first addition as a fused one, each lane's would be rounded in another place.)
 __device__ __forceinline__ float sum16(float v) {
+#pragma clang fp contract(off)
     v += moved<0xB1>(v);
     v += moved<0x4E>(v);
     v += moved<0x141>(v);
