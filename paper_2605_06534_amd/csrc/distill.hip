@@ -172,8 +172,9 @@ struct Q {
     __device__ __forceinline__ float operator()(float z) const {
         if constexpr (!FROM_LSE) return exp2_of((z - ref) * c) * factor;
         if constexpr (sizeof(T) == 2) return exp2_of(fmaf(z, high, -ref) * kLog2E) * factor;
-        z = fmaxf(z, kLowest);              // (times a low part of zero)
-        return exp2_of(fmaf(z, low, fmaf(z, high, -ref)) * kLog2E) * factor;
+        // (minus infinity in the high part alone: times a low part of zero it would be no number, and as the lowest of numbers in both no
+        // less likely than that, where a row holds nothing more)
+        return exp2_of(fmaf(fmaxf(z, kLowest), low, fmaf(z, high, -ref)) * kLog2E) * factor;
     }
 };
 template <class T, bool FROM_LSE>
