@@ -647,8 +647,8 @@ rose_status rose_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_st
  * rounding each (p to 24 bits where the gradient alone is wanted).  How a sum is divided, and so its last bits, depends on the form that is called, on rows, columns and `top`, and on how the
  * rows lie to 16 bytes.  Columns of minus infinity have q = 0 (an entry there makes the loss infinite); rows whose logits hold a NaN or an
  * infinity, or minus infinities only, have no number for loss and gradient.
- * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a temperature that is not above zero or
- * infinite, a workspace that is too small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^22 or more rows, 2^31 or more columns, or more than
+ * ROSE_ERR_ARG for null pointers, negative sizes, no columns, strides below cols, unknown types, a temperature that is not within 2^-126 and
+ * 2^126, a workspace that is too small; ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^22 or more rows, 2^31 or more columns, or more than
  * ROSE_DISTILL_MOST_TOP entries.
  */
 #define ROSE_DISTILL_MOST_TOP 1024

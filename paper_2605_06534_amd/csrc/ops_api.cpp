@@ -221,12 +221,13 @@ extern "C" rose_status rose_layer_norm_grad(const void *dy, int32_t dy_dtype, in
 
 namespace {
 
-// What the three forms of the distillation have in common.
+// What the three forms of the distillation have in common.  (1 / temperature, times log2(e), is a normal number of fp32: infinite or zero it would
+// make logits no numbers.)
 rose_status check_distill(const void *logits, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const void *ids, int32_t id_bytes,
                           const float *teacher, int64_t top, double temperature) {
     const rose_status s = check_matrix(logits, dtype, rows, cols, stride);
     if (s != ROSE_OK) return s;
-    if ((id_bytes != 4 && id_bytes != 8) || top < 0 || cols == 0 || !(temperature > 0.) || !(1. / temperature > 0.)) return ROSE_ERR_ARG;
+    if ((id_bytes != 4 && id_bytes != 8) || top < 0 || cols == 0 || !(temperature >= 0x1p-126 && temperature <= 0x1p126)) return ROSE_ERR_ARG;
     if (rows >= (1 << 22) || top > ROSE_DISTILL_MOST_TOP) return ROSE_ERR_UNSUPPORTED;
     if (rows > 0 && top > 0 && (!ids || !teacher)) return ROSE_ERR_ARG;
     return aligned(ids, (size_t)id_bytes) && aligned(teacher, 4) ? ROSE_OK : ROSE_ERR_ALIGN;
