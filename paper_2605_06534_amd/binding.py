@@ -596,14 +596,23 @@ def _bytes(name, what, *sizes, device="cuda"):
 _gpus = None
 
 
+def _device_of(stream):
+    """The GPU that a call on this stream runs on."""
+    if stream is None:
+        return torch._C._cuda_getDevice()
+    v = _i32()
+    _check(OK if _lib.hipStreamGetDevice(_stream(stream), ctypes.byref(v)) == 0 else ERR_HIP, "stream")
+    return v.value
+
+
 def _one_device(what, stream, *tensors):
-    """Everything on one GPU, the current one unless a stream says otherwise.  (That it is no host memory others see to.)"""
+    """Everything on the GPU that the call runs on: the stream's, or without one the current.  (That it is no host memory others see to.)"""
     global _gpus
     if _gpus is None:
         _gpus = torch.cuda.device_count()
     if _gpus == 1:
         return
-    here = tensors[0].get_device() if stream is not None else torch._C._cuda_getDevice()
+    here = _device_of(stream)
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise RoseError(ERR_SHAPE, "%s: all tensors on the GPU that the call runs on are wanted" % what)
