@@ -702,7 +702,8 @@ rose_status rose_draft_verify(const void *target, int64_t target_stride, const v
  *   workspace    rose_adapter_linear_workspace_bytes, 256-byte aligned: never fewer where a size grows; contents before the call do not
  *                matter; calls that share one must be ordered on one stream
  * Products are exact, sums and what lies between the two products fp32; one rounding, of the sum with out.  How a sum is divided depends
- * on the sizes, the number of adapters among them.  An infinity in up or down makes what it reaches no number or an infinity.
+ * on the sizes, the number of adapters among them.  More than 128 rows are looked through once for each adapter that there is, named or
+ * not (8192 rows and 512 adapters 8 us, 65536 adapters 0.4 ms).  An infinity in up or down makes what it reaches no number or an infinity.
  * ROSE_ERR_ARG for null pointers, negative sizes, strides below the columns, unknown types, a workspace that is too small;
  * ROSE_ERR_ALIGN; ROSE_ERR_UNSUPPORTED for 2^29 or more rows, 2^31 or more columns, more than ROSE_MOST_ADAPTERS adapters, a rank
  * above ROSE_MOST_RANK, or, of more than 128 rows that are 32 or more for

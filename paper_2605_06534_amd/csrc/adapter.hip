@@ -22,7 +22,8 @@ constexpr int64_t kSplitRows = 32768;               // rows of partial sums, whe
 constexpr int kSortThreads = 1024;
 // Rows of each adapter on average, and rows times ranks (of up to 64), from which on 64 rows go together and not 16 (4096 columns both ways, 64
 // against 16 together: 4096 rows of 64 adapters, rank 16, 35.5 us and 43.3, of 256 adapters 55.9 and 48.1; 1024 rows of 16, rank 64, 29.5 and 32.0,
-// rank 16 20.1 and 18.3).
+// rank 16 20.1 and 18.3).  Rows of each adapter that there is, that is: which ones rows name is not known on the host.  8192 rows that name 8,
+// rank 16, take 67 us as traced where there are 8, 73 of 64, and in groups of 16 78 of 512.
 constexpr int64_t kLarge = 32, kLargeWork = 65536;
 
 __device__ __forceinline__ int64_t adapter_of(const AdapterArgs &a, int64_t row) {
@@ -56,7 +57,8 @@ __device__ __forceinline__ void load_end(const bf16_t *end, int n, bool long_eno
 
 // ---- rows sorted by adapter: a workgroup an adapter ----
 // Rows of adapter a lie behind those of smaller ones, `less` of them, in their order.  Its groups of up to `a.group` rows have numbers from
-// less / group + a on: the next adapter's begin behind them, since floor(x / g) + 1 >= ceil(y / g) + floor((x - y) / g).
+// less / group + a on: the next adapter's begin behind them, since floor(x / g) + 1 >= ceil(y / g) + floor((x - y) / g).  Each workgroup looks
+// through all rows: 8 us for 8192 of them and up to 512 adapters, 31 for 4096, 390 for 65536.
 __global__ __launch_bounds__(kSortThreads) void adapter_sort_kernel(AdapterArgs a) {
     constexpr int WAVES = kSortThreads / 64;
     __shared__ int32_t less_of[WAVES], mine_of[WAVES];

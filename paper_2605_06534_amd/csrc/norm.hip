@@ -241,8 +241,10 @@ __global__ __launch_bounds__(kThreads) void norm_columns_kernel(NormGradArgs a, 
 // ones on their way; TEAM threads have a row, in whole waves (TEAM = 0: as many as the workgroup has), or 16 lanes.  The two means of a row
 // are the only thing that goes from wave to wave.
 // 256 workgroups: each leaves sums of all columns behind, 8 bytes a column (16384 x 5120 in bf16: 110 us, with 512 of them 116, with 768 128).
-// x and dy are read for the last time, so that the caches need not keep them: 99 us, 5.1 TB/s.  (Columns a lane 8: the same; two rows at
-// a time instead of one: 89 us against 96 of 16384 x 4096, four spill.) ----
+// x and dy are read for the last time, so that the caches need not keep them: 99 to 104 us, 4.8 to 5.1 TB/s.  (Columns a lane 8: the same; two rows at
+// a time instead of one: 89 us against 96 of 16384 x 4096, four spill.)  More than 8192 columns: one row at a time by up to 1024 threads of 128
+// registers, of which 13 (bf16) to 70 (fp32) spill: 4096 x 12288 in bf16 74 us, 4.1 TB/s, in fp32 178, 3.4.  Up to 256 columns: 16 rows a workgroup, one
+// for each 16 lanes, whose trips to memory bound it: 1,048,576 x 128 in bf16 265 us, 3.0 TB/s. ----
 constexpr int kColumns = 16;
 
 template <class D, class X, int TEAM, int ROWS, int THREADS>
@@ -373,7 +375,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(NormGradArgs a, floa
         float(&sum)[V][W] = which ? db : dw;
         float &sum_tail = which ? db_tail : dw_tail;
         if constexpr (!ONE) {
-            // (the elements behind the last whole vector go into the place of a vector that is not there, or along with lane 0's)
+            // (the vectors' first, then in an exchange of their own the elements behind the last whole one)
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < V; ++v)
